@@ -302,6 +302,91 @@ FIRA_API fira_status fira_profile_begin(fira_ctx* ctx, int max_steps);
 FIRA_API fira_status fira_profile_end(fira_ctx* ctx, double* ms_sum, int* steps);
 FIRA_API const char* fira_kernel_name(int k);
 
+/* ---- Operators around the step ---------------------------------------------------------------------------
+ * A training step around fira_step: what the low-rank update is not for (embeddings and norms, forwards and
+ * backwards) and the norm of all gradients together.  These calls have no context.  Conventions beyond those at the top:
+ *   - They enqueue on hip_stream (a hipStream_t, NULL = default stream) of the current device, return without synchronising,
+ *     allocate nothing, keep nothing from one call for the next, and can be captured in a HIP graph.
+ *   - Matrices are row-major with leading dimension ld >= the width (elements); rows start at any element, every pointer is aligned to
+ *     its element.  What lies between the end of a row and the next one is neither read nor written.
+ *   - Arguments may be zero rows, tokens or tensors, with null pointers then; results that are sums are zero.
+ *   - Sums, means and deviations are held in fp32 or fp64 and results rounded once, to nearest even.  All
+ *     sums are taken in an order that depends on the sizes only: the same inputs give the same bits.
+ *   - Results must not overlap inputs unless a call says so.
+ *   - fira_last_error(NULL) has the message of the last failure on this thread.  A call refused for its arguments enqueues nothing.
+ *   - dev_workspace: device scratch of at least what the matching *_workspace_bytes call says (0 for invalid arguments), 256-byte
+ *     aligned, its contents arbitrary, owned by the caller and free to reuse once the stream has passed the call.
+ * Limits: tokens, vocabularies and rows below 2^31; widths below 2^31. */
+
+typedef enum { FIRA_I32 = 0, FIRA_I64 = 1 } fira_index_type;
+
+/* An embedding table E (rows x dim) and the rows looked up in it. */
+typedef struct {
+  int64_t rows, dim, ld;   /* ld: leading dimension of the table, or of its gradient in fira_embed_gradient */
+  int32_t dtype;           /* fira_dtype of the table and of its gradient */
+  int32_t row_dtype;       /* fira_dtype of the rows looked up and of their gradients */
+  int32_t id_type;         /* fira_index_type of the tokens */
+  double scale;            /* finite, as fp32 */
+} fira_embed_desc;
+
+/* out[t] = scale E[id_t] for `count` tokens; an id outside [0, rows) (padding) gives a row of zeros. */
+FIRA_API fira_status fira_embed_lookup(const fira_embed_desc* d, const void* dev_table, const void* dev_ids, int64_t count,
+                                       void* dev_out, int64_t ld_out, void* hip_stream);
+
+/* The table's gradient, every row of it: dE[v] = scale * sum of dout[t] over the tokens with id_t = v, zeros where there is none; ids
+ * outside [0, rows) are left out.  accumulate != 0 adds to what dev_dtable holds (micro-batches) and leaves rows without a token as they are.
+ * A row's result depends on its own tokens and their order only. */
+FIRA_API size_t fira_embed_gradient_workspace_bytes(const fira_embed_desc* d, int64_t count);
+FIRA_API fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, int64_t ld_dout, const void* dev_ids, int64_t count,
+                                         void* dev_dtable, int accumulate, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* FIRA_LAYER_NORM: mu = mean x, rstd = (mean (x - mu)^2 + eps)^(-1/2), y = weight (x - mu) rstd + bias, per row.
+ * FIRA_RMS_NORM: the same with mu = 0. */
+typedef enum { FIRA_LAYER_NORM = 0, FIRA_RMS_NORM = 1 } fira_layer_norm_kind;
+typedef struct {
+  int64_t rows, dim;
+  int32_t dtype;           /* fira_dtype of x, y and their gradients */
+  int32_t param_dtype;     /* fira_dtype of weight, bias and their gradients */
+  int32_t kind;            /* fira_layer_norm_kind */
+  double eps;              /* >= 0 */
+} fira_layer_norm_desc;
+
+/* weight, bias: dim values each, NULL for ones and zeros.  dev_mean, dev_rstd: fp32, `rows` values each, for the backward
+ * pass; either may be NULL, and dev_mean is not written by FIRA_RMS_NORM. */
+FIRA_API fira_status fira_layer_norm(const fira_layer_norm_desc* d, const void* dev_x, int64_t ld_x, const void* dev_weight,
+                                     const void* dev_bias, void* dev_y, int64_t ld_y, float* dev_mean, float* dev_rstd, void* hip_stream);
+
+/* With h = (x - mu) rstd and g = weight dy:  dx = rstd (g - mean g - h mean(g h)) per row, without `mean g` for FIRA_RMS_NORM;
+ * dweight = sum over rows of dy h;  dbias = sum over rows of dy.  Any of the three results may be NULL.  dev_mean (NULL for
+ * FIRA_RMS_NORM) and dev_rstd are those of the forward pass.  accumulate != 0 adds dweight and dbias to what their buffers hold. */
+FIRA_API size_t fira_layer_norm_gradient_workspace_bytes(const fira_layer_norm_desc* d);
+FIRA_API fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* dev_dy, int64_t ld_dy, const void* dev_x, int64_t ld_x,
+                                              const void* dev_weight, const float* dev_mean, const float* dev_rstd, void* dev_dx, int64_t ld_dx,
+                                              void* dev_dweight, void* dev_dbias, int accumulate, void* dev_workspace, size_t workspace_bytes,
+                                              void* hip_stream);
+
+/* One gradient of a list: any tensor as a matrix (a vector has one row). */
+typedef struct {
+  int64_t rows, cols, ld;
+  int32_t dtype;           /* fira_dtype */
+  int32_t out_dtype;       /* fira_dtype of the clipped gradient; not looked at without dev_out */
+  int64_t ld_out;          /* its leading dimension; not looked at without dev_out */
+} fira_gradient_desc;
+
+/* *dev_norm (fp32) = sqrt of the sum of the squares of all values of all `count` gradients; the squares are summed in fp64, so that no
+ * finite gradient overflows on the way.  d and dev_G are host arrays of length count. */
+FIRA_API size_t fira_gradient_workspace_bytes(const fira_gradient_desc* d, int count);
+FIRA_API fira_status fira_gradient_norm(const fira_gradient_desc* d, int count, const void* const* dev_G, float* dev_norm,
+                                        void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient clipping by that norm n: every gradient times min(1, max_norm / n), *dev_norm = n, the norm before.  dev_out[i] (host array) is where
+ * gradient i goes, converted to out_dtype; it may be dev_G[i] itself with the same type and leading dimension.  dev_out NULL: all in place, and
+ * then gradients that need no cut are read once and not written.  A norm that is not finite leaves the values as they are (the caller sees
+ * it in *dev_norm), as the norm-growth limiter of fira_step leaves such a step.  max_norm >= 0, +inf for no limit.  The tensors must
+ * not overlap one another. */
+FIRA_API fira_status fira_clip_gradients(const fira_gradient_desc* d, int count, void* const* dev_G, void* const* dev_out, double max_norm,
+                                         float* dev_norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
 FIRA_API const char* fira_last_error(const fira_ctx* ctx);
 
 FIRA_API void fira_destroy(fira_ctx* ctx);

@@ -17,10 +17,12 @@ HIPCC_FLAGS = [
 ]
 
 
+SOURCES = ("fira.hip", "fira_training.hip")   # the optimizer step; the operators around it
+
+
 def build_library(verbose: bool = True, extra_flags=()) -> str:
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
-    src = os.path.join(CSRC, "fira.hip")
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, src, "-o", LIB_PATH]
+    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, *(os.path.join(CSRC, name) for name in SOURCES), "-o", LIB_PATH]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "fira_device.h"
+#include "fira_error.h"
 #include "fira_elementwise.h"
 #include "fira_refresh.h"
 #include "fira_gemm.h"
@@ -25,6 +26,11 @@ namespace {
 thread_local std::string g_last_error;
 
 }  // namespace
+
+fira_status fira_fail_without_context(fira_status st, const char* msg) noexcept {
+  try { g_last_error = msg; } catch (...) { g_last_error.clear(); }
+  return st;
+}
 
 // Scratch of fira_refresh_projectors_static: device memory that exists from the moment the library is
 // loaded, so that the call needs no allocation.  Every GPU the library runs on holds its own copy at its own

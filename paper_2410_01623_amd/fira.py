@@ -27,6 +27,8 @@ FIRA_F32, FIRA_BF16 = 0, 1
 FIRA_SCALE_COLUMN, FIRA_SCALE_MATRIX, FIRA_SCALE_NONE = 0, 1, 2
 FIRA_VARIANT_FULL, FIRA_VARIANT_ONLY_SCALING = 0, 1
 FIRA_NORM_RESIDUAL, FIRA_NORM_GRAM = 0, 1
+FIRA_I32, FIRA_I64 = 0, 1
+FIRA_LAYER_NORM, FIRA_RMS_NORM = 0, 1
 FIRA_NUM_KERNELS = 6
 FIRA_STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -37,6 +39,9 @@ EXPORTS = (
     "fira_get_factors", "fira_get_lowrank", "fira_get_projector", "fira_refresh_workspace_bytes",
     "fira_refresh_projectors", "fira_refresh_projectors_static", "fira_profile_begin", "fira_profile_end", "fira_kernel_name",
     "fira_last_error", "fira_destroy",
+    "fira_embed_lookup", "fira_embed_gradient_workspace_bytes", "fira_embed_gradient",
+    "fira_layer_norm", "fira_layer_norm_gradient_workspace_bytes", "fira_layer_norm_gradient",
+    "fira_gradient_workspace_bytes", "fira_gradient_norm", "fira_clip_gradients",
 )
 
 
@@ -48,6 +53,21 @@ class fira_hparams(ctypes.Structure):
 class fira_matrix_desc(ctypes.Structure):
     _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("ld", ctypes.c_int64),
                 ("r", ctypes.c_int32), ("wg_dtype", ctypes.c_int32)]
+
+
+class fira_embed_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("row_dtype", ctypes.c_int32), ("id_type", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class fira_layer_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("eps", ctypes.c_double)]
+
+
+class fira_gradient_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("ld_out", ctypes.c_int64)]
 
 
 class FiraError(RuntimeError):
@@ -129,6 +149,26 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fira_last_error.argtypes = [vp]
     lib.fira_destroy.restype = None
     lib.fira_destroy.argtypes = [vp]
+    c64, cz = ctypes.c_int64, ctypes.c_size_t
+    embed, norm, grad = (ctypes.POINTER(t) for t in (fira_embed_desc, fira_layer_norm_desc, fira_gradient_desc))
+    lib.fira_embed_lookup.restype = ci
+    lib.fira_embed_lookup.argtypes = [embed, vp, vp, c64, vp, c64, vp]
+    lib.fira_embed_gradient_workspace_bytes.restype = cz
+    lib.fira_embed_gradient_workspace_bytes.argtypes = [embed, c64]
+    lib.fira_embed_gradient.restype = ci
+    lib.fira_embed_gradient.argtypes = [embed, vp, c64, vp, c64, vp, ci, vp, cz, vp]
+    lib.fira_layer_norm.restype = ci
+    lib.fira_layer_norm.argtypes = [norm, vp, c64, vp, vp, vp, c64, vp, vp, vp]
+    lib.fira_layer_norm_gradient_workspace_bytes.restype = cz
+    lib.fira_layer_norm_gradient_workspace_bytes.argtypes = [norm]
+    lib.fira_layer_norm_gradient.restype = ci
+    lib.fira_layer_norm_gradient.argtypes = [norm, vp, c64, vp, c64, vp, vp, vp, vp, c64, vp, vp, ci, vp, cz, vp]
+    lib.fira_gradient_workspace_bytes.restype = cz
+    lib.fira_gradient_workspace_bytes.argtypes = [grad, ci]
+    lib.fira_gradient_norm.restype = ci
+    lib.fira_gradient_norm.argtypes = [grad, ci, ctypes.POINTER(vp), vp, vp, cz, vp]
+    lib.fira_clip_gradients.restype = ci
+    lib.fira_clip_gradients.argtypes = [grad, ci, ctypes.POINTER(vp), ctypes.POINTER(vp), cd, vp, vp, cz, vp]
     if path is None:
         _lib = lib
     return lib

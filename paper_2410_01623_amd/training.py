@@ -1,0 +1,313 @@
+"""The operators around the optimizer step, by the names of their C entry points (include/fira.h): embedding lookup, layer norm
+and root-mean-square norm, each with its gradient, and the norm and clipping of a list of gradients.
+
+As in `fira`, this is argument marshalling: tensors become pointers, sizes and leading dimensions, everything is computed by
+libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.  `stream` is the torch stream to enqueue on (default: the
+current one of that GPU); the caller orders it after whatever made the inputs.  Results and workspaces that are not given
+are allocated on that stream.  Of a tensor with more than two dimensions all but the last are its rows.  An input whose rows cannot
+be told from one leading dimension (an expanded or permuted view) is copied first; a result given by the caller has
+to be such a matrix.  What the library refuses raises fira.FiraError with its status, and so does a tensor that does not fit the others."""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from . import fira
+from .fira import FiraError, FIRA_BF16, FIRA_ERR_DTYPE, FIRA_ERR_INVALID_ARG, FIRA_ERR_SHAPE, FIRA_F32, FIRA_I32, FIRA_I64
+
+_DTYPE = {torch.float32: FIRA_F32, torch.bfloat16: FIRA_BF16}
+_IDS = {torch.int32: FIRA_I32, torch.int64: FIRA_I64}
+
+
+def _refuse(status: int, message: str):
+    raise FiraError(status, message)
+
+
+def _dtype(t, name: str) -> int:
+    dt = _DTYPE.get(t.dtype if isinstance(t, torch.Tensor) else t)
+    if dt is None:
+        _refuse(FIRA_ERR_DTYPE, f"{name} is neither bf16 nor fp32")
+    return dt
+
+
+def _device(*tensors) -> torch.device:
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        _refuse(FIRA_ERR_INVALID_ARG, "tensors are not on a GPU")
+    for t in tensors[1:]:
+        if t is not None and t.device != dev:
+            _refuse(FIRA_ERR_INVALID_ARG, f"tensors on {dev} and {t.device}")
+    return dev
+
+
+@contextlib.contextmanager
+def _on_device_and_stream(dev, stream):
+    with torch.cuda.device(dev), (torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()):
+        yield
+
+
+class _Call:
+    """The device and the stream of one call: entered only where they are not the current ones, for they cost as much as a launch."""
+
+    __slots__ = ("handle", "guard")
+
+    def __init__(self, dev: torch.device, stream: Optional[torch.cuda.Stream]):
+        if stream is not None and stream.device != dev:
+            _refuse(FIRA_ERR_INVALID_ARG, f"tensors on {dev}, stream on {stream.device}")
+        current = torch.cuda.current_stream(dev)
+        self.guard = None
+        if dev.index != torch.cuda.current_device() or (stream is not None and stream != current):
+            self.guard = _on_device_and_stream(dev, stream)
+        self.handle = (stream or current).cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _ld(t: torch.Tensor) -> Optional[int]:
+    """Leading dimension of t seen as rows of its last dimension, or None if it has no such."""
+    shape, strides = t.shape, t.stride()
+    cols = shape[-1]
+    if t.is_contiguous():
+        return cols
+    if cols > 1 and strides[-1] != 1:
+        return None
+    ld = None
+    need = None            # stride that the next dimension outwards has to have
+    for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if size == 1:
+            continue
+        if need is None:
+            ld = stride
+        elif stride != need:
+            return None
+        need = stride * size
+    if ld is None:
+        return cols
+    return ld if ld >= cols else None
+
+
+def _input(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    ld = _ld(t)
+    if ld is None:
+        t = t.contiguous()
+        ld = t.shape[-1]
+    return t, ld
+
+
+def _result(given: Optional[torch.Tensor], shape, dtype, dev, name: str) -> Tuple[torch.Tensor, int]:
+    if given is None:
+        return torch.empty(shape, dtype=dtype, device=dev), shape[-1]
+    if tuple(given.shape) != tuple(shape):
+        _refuse(FIRA_ERR_SHAPE, f"{name} is {tuple(given.shape)}, not {tuple(shape)}")
+    if given.dtype != dtype:
+        _refuse(FIRA_ERR_DTYPE, f"{name} is {given.dtype}, not {dtype}")
+    ld = _ld(given)
+    if ld is None:
+        _refuse(FIRA_ERR_SHAPE, f"{name} has no single leading dimension")
+    return given, ld
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        _refuse(FIRA_ERR_SHAPE, f"{name} is not a dense vector of {n}")
+    return t.data_ptr()
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, dev) -> torch.Tensor:
+    if given is not None:
+        if given.device != dev or given.dtype != torch.uint8 or not given.is_contiguous():
+            _refuse(FIRA_ERR_INVALID_ARG, f"workspace is not a dense byte tensor on {dev}")
+        return given
+    return torch.empty(need, dtype=torch.uint8, device=dev)
+
+
+def _ids(ids: torch.Tensor) -> torch.Tensor:
+    if ids.dtype not in _IDS:
+        _refuse(FIRA_ERR_DTYPE, "ids are neither int32 nor int64")
+    return ids.contiguous()
+
+
+def _check(status: int):
+    if status:
+        fira._check(fira.load_library(), None, status)
+
+
+def fira_embed_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
+                      out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """scale * table[ids], of shape ids.shape + (width,) and type `dtype` (default: out's, else the table's).  ids (int32 or int64) outside the
+    table, such as -1 for padding, give zeros."""
+    lib = fira.load_library()
+    if table.dim() != 2:
+        _refuse(FIRA_ERR_SHAPE, "the table is no matrix")
+    dev = _device(table, ids, out)
+    dtype = dtype or (out.dtype if out is not None else table.dtype)
+    dt, rdt = _dtype(table, "table"), _dtype(dtype, "result")
+    with _Call(dev, stream) as call:
+        ids = _ids(ids)
+        table, ld = _input(table)
+        out, ld_out = _result(out, (*ids.shape, table.shape[1]), dtype, dev, "out")
+        d = fira.fira_embed_desc(table.shape[0], table.shape[1], ld, dt, rdt, _IDS[ids.dtype], scale)
+        _check(lib.fira_embed_lookup(d, table.data_ptr(), ids.data_ptr(), ids.numel(), out.data_ptr(), ld_out, call.handle))
+    return out
+
+
+def fira_embed_gradient(dout: torch.Tensor, ids: torch.Tensor, rows: int, *, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
+                        out: Optional[torch.Tensor] = None, accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of fira_embed_lookup's table of `rows` rows: dout is the gradient of its result (ids.shape + (width,)).  The result has type `dtype`
+    (default: out's, else dout's).  accumulate adds to `out`."""
+    lib = fira.load_library()
+    dev = _device(dout, ids, out)
+    dtype = dtype or (out.dtype if out is not None else dout.dtype)
+    dt, rdt = _dtype(dtype, "result"), _dtype(dout, "dout")
+    if dout.dim() < 1 or dout.shape[:-1] != ids.shape:
+        _refuse(FIRA_ERR_SHAPE, f"dout is {tuple(dout.shape)} for ids of {tuple(ids.shape)}")
+    if accumulate and out is None:
+        _refuse(FIRA_ERR_INVALID_ARG, "accumulate without out")
+    with _Call(dev, stream) as call:
+        ids = _ids(ids)
+        dout, ld_dout = _input(dout)
+        out, ld = _result(out, (rows, dout.shape[-1]), dtype, dev, "out")
+        d = fira.fira_embed_desc(rows, dout.shape[-1], ld, dt, rdt, _IDS[ids.dtype], scale)
+        count = ids.numel()
+        workspace = _workspace(workspace, lib.fira_embed_gradient_workspace_bytes(d, count), dev)
+        _check(lib.fira_embed_gradient(d, dout.data_ptr(), ld_dout, ids.data_ptr(), count, out.data_ptr(), bool(accumulate),
+                                       workspace.data_ptr(), workspace.numel(), call.handle))
+    return out
+
+
+def fira_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, eps: float = 1e-5,
+                    rms: bool = False, out: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor]:
+    """Layer norm (rms: root-mean-square norm) over x's last dimension -> (y, mean, rstd); y is of x's type, mean (None with rms) and rstd are
+    fp32 of shape x.shape[:-1], for fira_layer_norm_gradient.  weight and bias, of one type, default to ones and zeros."""
+    lib = fira.load_library()
+    if x.dim() < 1:
+        _refuse(FIRA_ERR_SHAPE, "x has no dimension")
+    dev = _device(x, weight, bias, out)
+    dt = _dtype(x, "x")
+    pdt = _param_dtype(dt, weight, bias)
+    with _Call(dev, stream) as call:
+        x, ld_x = _input(x)
+        dim, shape = x.shape[-1], x.shape[:-1]
+        out, ld_y = _result(out, x.shape, x.dtype, dev, "out")
+        mean = None if rms else torch.empty(shape, dtype=torch.float32, device=dev)
+        rstd = torch.empty(shape, dtype=torch.float32, device=dev)
+        d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, eps)
+        _check(lib.fira_layer_norm(d, x.data_ptr(), ld_x, _vector(weight, dim, "weight"), _vector(bias, dim, "bias"), out.data_ptr(), ld_y,
+                                   None if rms else mean.data_ptr(), rstd.data_ptr(), call.handle))
+    return out, mean, rstd
+
+
+def _param_dtype(default: int, *params) -> int:
+    dts = {_dtype(p, "parameter") for p in params if p is not None}
+    if len(dts) > 1:
+        _refuse(FIRA_ERR_DTYPE, "parameters of two types")
+    return dts.pop() if dts else default
+
+
+def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: Optional[torch.Tensor], rstd: torch.Tensor, *,
+                             rms: bool = False, bias: bool = True, param_dtype: Optional[torch.dtype] = None, dx: Optional[torch.Tensor] = None,
+                             dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                             workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Gradients of fira_layer_norm -> (dx, dweight, dbias); dbias is None without `bias`.  mean and rstd are the forward pass's.  dweight and dbias
+    are of weight's type (without weight: param_dtype, default x's).  accumulate adds them to what the given dweight and dbias hold."""
+    lib = fira.load_library()
+    if x.dim() < 1 or dy.shape != x.shape:
+        _refuse(FIRA_ERR_SHAPE, f"dy is {tuple(dy.shape)} for x of {tuple(x.shape)}")
+    dev = _device(x, dy, weight, mean, rstd, dx, dweight, dbias)
+    dt = _dtype(x, "x")
+    if dy.dtype != x.dtype:
+        _refuse(FIRA_ERR_DTYPE, "dy is not of x's type")
+    ptype = weight.dtype if weight is not None else param_dtype or (dweight.dtype if dweight is not None else x.dtype)
+    pdt = _dtype(ptype, "parameter")
+    if not rms and mean is None:
+        _refuse(FIRA_ERR_INVALID_ARG, "a layer norm's gradient needs its mean")
+    for t, name in ((rstd, "rstd"),) if rms else ((mean, "mean"), (rstd, "rstd")):
+        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+            _refuse(FIRA_ERR_SHAPE, f"{name} is not a dense fp32 tensor of {tuple(x.shape[:-1])}")
+    if accumulate and (dweight is None or (bias and dbias is None)):
+        _refuse(FIRA_ERR_INVALID_ARG, "accumulate without dweight and dbias")
+    with _Call(dev, stream) as call:
+        x, ld_x = _input(x)
+        dy, ld_dy = _input(dy)
+        dim = x.shape[-1]
+        dx, ld_dx = _result(dx, x.shape, x.dtype, dev, "dx")
+        dweight, _ = _result(dweight, (dim,), ptype, dev, "dweight")
+        if bias:
+            dbias, _ = _result(dbias, (dim,), ptype, dev, "dbias")
+        else:
+            dbias = None
+        d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, 0.0)
+        workspace = _workspace(workspace, lib.fira_layer_norm_gradient_workspace_bytes(d), dev)
+        _check(lib.fira_layer_norm_gradient(d, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, _vector(weight, dim, "weight"),
+                                            None if rms else mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), ld_dx, _vector(dweight, dim, "dweight"),
+                                            _vector(dbias, dim, "dbias"), bool(accumulate), workspace.data_ptr(), workspace.numel(), call.handle))
+    return dx, dweight, dbias
+
+
+class GradientList:
+    """Gradients that are measured and clipped together, marshalled once: any tensors of bf16 and fp32 on one GPU that can be seen as
+    matrices.  outs, one per gradient and of its shape, take the clipped gradients in their own type; without them clipping is in place.  The
+    workspace is the list's own, so that its calls belong on one stream at a time."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, device: Optional[torch.device] = None):
+        self.lib = fira.load_library()
+        grads = list(grads)
+        if not grads and device is None:
+            _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
+        self.device = _device(*grads, *(outs or ())) if grads else torch.device(device)
+        if outs is not None and len(outs) != len(grads):
+            _refuse(FIRA_ERR_INVALID_ARG, f"{len(outs)} results for {len(grads)} gradients")
+        n = self.count = len(grads)
+        self.descs = (fira.fira_gradient_desc * n)()
+        for i, g in enumerate(grads):
+            o = outs[i] if outs is not None else g
+            if o.shape != g.shape:
+                _refuse(FIRA_ERR_SHAPE, f"result {i} is {tuple(o.shape)}, not {tuple(g.shape)}")
+            (rows, cols, ld), (_, _, ld_out) = self._matrix(g, f"gradient {i}"), self._matrix(o, f"result {i}")
+            self.descs[i] = fira.fira_gradient_desc(rows, cols, ld, _dtype(g, f"gradient {i}"), _dtype(o, f"result {i}"), ld_out)
+        pointers = ctypes.c_void_p * n
+        self.G = pointers(*[g.data_ptr() for g in grads])
+        self.outs = pointers(*[o.data_ptr() for o in outs]) if outs is not None else None
+        self.bytes = self.lib.fira_gradient_workspace_bytes(self.descs, n)
+        self.workspace = torch.empty(max(self.bytes, 256), dtype=torch.uint8, device=self.device)
+        self._keep = (grads, list(outs) if outs is not None else None)
+
+    @staticmethod
+    def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
+        if t.dim() == 0:
+            return 1, 1, 1
+        ld = _ld(t)
+        if ld is None:
+            _refuse(FIRA_ERR_SHAPE, f"{name} has no single leading dimension")
+        cols = t.shape[-1]
+        return (t.numel() // cols if cols else 0), cols, ld
+
+    def fira_gradient_norm(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The norm of all gradients together, an fp32 scalar on the GPU."""
+        with _Call(self.device, stream) as call:
+            norm = torch.empty((), dtype=torch.float32, device=self.device)
+            _check(self.lib.fira_gradient_norm(self.descs, self.count, self.G, norm.data_ptr(), self.workspace.data_ptr(), self.bytes, call.handle))
+        return norm
+
+    def fira_clip_gradients(self, max_norm: float, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Scales all gradients by min(1, max_norm / norm) -> the norm before, an fp32 scalar on the GPU.  A norm that is not finite leaves
+        them as they are."""
+        with _Call(self.device, stream) as call:
+            norm = torch.empty((), dtype=torch.float32, device=self.device)
+            _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), self.workspace.data_ptr(),
+                                                self.bytes, call.handle))
+        return norm

@@ -1,0 +1,92 @@
+"""What the operators around the step refuse, and that they enqueue nothing then (C ABI, no GPU)."""
+import ctypes
+import math
+
+import pytest
+
+from paper_2410_01623_amd import fira
+
+P = ctypes.c_void_p(4096)          # never looked at: every call here is refused on the host, or has nothing to do
+ODD = ctypes.c_void_p(4097)
+N = None
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return fira.load_library()
+
+
+def embed(rows=10, dim=8, ld=8, dtype=0, row_dtype=1, id_type=1, scale=1.0):
+    return fira.fira_embed_desc(rows, dim, ld, dtype, row_dtype, id_type, scale)
+
+
+def norm(rows=10, dim=8, dtype=0, param_dtype=1, kind=0, eps=1e-5):
+    return fira.fira_layer_norm_desc(rows, dim, dtype, param_dtype, kind, eps)
+
+
+def test_embedding(lib):
+    for d, count, want in ((None, 1, -1), (embed(rows=0), 1, -2), (embed(rows=1 << 31), 1, -2), (embed(dim=0), 1, -2), (embed(ld=7), 1, -2), (embed(ld=1 << 62), 1, -2),
+                           (embed(), -1, -2), (embed(), 1 << 31, -2), (embed(dtype=2), 1, -4), (embed(row_dtype=-1), 1, -4), (embed(id_type=2), 1, -4),
+                           (embed(scale=math.nan), 1, -1), (embed(scale=1e300), 1, -1)):
+        assert lib.fira_embed_lookup(d, P, P, count, P, 8, N) == want
+        assert lib.fira_embed_gradient_workspace_bytes(d, count) == 0
+        assert lib.fira_embed_gradient(d, P, 8, P, count, P, 0, P, BIG, N) == want
+    d = embed()
+    for args, want in (((N, P, 3, P, 8), -1), ((P, N, 3, P, 8), -1), ((P, P, 3, N, 8), -1), ((P, P, 3, P, 7), -2), ((ODD, P, 3, P, 8), -1), ((P, P, 3, ODD, 8), -1)):
+        assert lib.fira_embed_lookup(d, *args, N) == want
+        assert len(lib.fira_last_error(None)) > 0
+    assert lib.fira_embed_lookup(d, N, N, 0, N, 0, N) == 0
+    need = lib.fira_embed_gradient_workspace_bytes(d, 3)
+    assert need > 0
+    for args, want in (((N, 8, P, 3, P, 0, P, need), -1), ((P, 7, P, 3, P, 0, P, need), -2), ((P, 8, N, 3, P, 0, P, need), -1), ((P, 8, P, 3, N, 0, P, need), -1),
+                       ((P, 8, P, 3, P, 0, P, need - 1), -5), ((P, 8, P, 3, P, 0, N, need), -5), ((P, 8, P, 3, P, 0, ctypes.c_void_p(4096 + 128), need), -5)):
+        assert lib.fira_embed_gradient(d, *args, N) == want
+    assert lib.fira_embed_gradient(d, N, 0, N, 0, P, 1, P, need, N) == 0      # nothing to add
+
+
+def test_norms(lib):
+    for d, want in ((None, -1), (norm(rows=-1), -2), (norm(rows=1 << 31), -2), (norm(dim=0), -2), (norm(dim=1 << 31), -2), (norm(dtype=3), -4), (norm(param_dtype=2), -4),
+                    (norm(kind=2), -1), (norm(eps=-1e-9), -1), (norm(eps=math.nan), -1), (norm(eps=math.inf), -1)):
+        assert lib.fira_layer_norm(d, P, 8, P, P, P, 8, P, P, N) == want
+        assert lib.fira_layer_norm_gradient_workspace_bytes(d) == 0
+        assert lib.fira_layer_norm_gradient(d, P, 8, P, 8, P, P, P, P, 8, P, P, 0, P, BIG, N) == want
+    d = norm()
+    for args, want in (((N, 8, P, P, P, 8, P, P), -1), ((P, 7, P, P, P, 8, P, P), -2), ((P, 8, P, P, N, 8, P, P), -1), ((P, 8, P, P, P, 7, P, P), -2), ((P, 8, ODD, P, P, 8, P, P), -1),
+                       ((P, 8, P, P, P, 8, ODD, P), -1)):
+        assert lib.fira_layer_norm(d, *args, N) == want
+    assert lib.fira_layer_norm(norm(rows=0), N, 0, N, N, N, 0, N, N, N) == 0
+    need = lib.fira_layer_norm_gradient_workspace_bytes(d)
+    assert need > 0
+    ok = [P, 8, P, 8, P, P, P, P, 8, P, P, 0, P, need]
+    for at, bad, want in ((0, N, -1), (1, 7, -2), (2, N, -1), (3, 7, -2), (5, N, -1), (6, N, -1), (7, ODD, -1), (8, 7, -2), (9, ODD, -1), (10, ODD, -1), (12, N, -5), (13, need - 1, -5)):
+        args = list(ok)
+        args[at] = bad
+        assert lib.fira_layer_norm_gradient(d, *args, N) == want, at
+
+
+def test_gradients(lib):
+    def one(rows=4, cols=8, ld=8, dtype=0, out_dtype=0, ld_out=8):
+        return (fira.fira_gradient_desc * 1)(fira.fira_gradient_desc(rows, cols, ld, dtype, out_dtype, ld_out))
+
+    def list_of(p):
+        return (ctypes.c_void_p * 1)(p.value if p is not None else None)
+
+    g = list_of(P)
+    for d, want in ((one(rows=-1), -2), (one(cols=-1), -2), (one(ld=7), -2), (one(dtype=2), -4)):
+        assert lib.fira_gradient_workspace_bytes(d, 1) == 0
+        assert lib.fira_gradient_norm(d, 1, g, P, P, BIG, N) == want
+        assert lib.fira_clip_gradients(d, 1, g, None, 1.0, P, P, BIG, N) == want
+    for d, want in ((one(out_dtype=9), -4), (one(ld_out=7), -2)):
+        assert lib.fira_clip_gradients(d, 1, g, g, 1.0, P, P, BIG, N) == want
+    d = one()
+    need = lib.fira_gradient_workspace_bytes(d, 1)
+    assert need > 0
+    assert lib.fira_gradient_norm(d, -1, g, P, P, need, N) == -1
+    assert lib.fira_gradient_norm(None, 1, g, P, P, need, N) == -1
+    for args, want in (((None, P, P, need), -1), ((list_of(None), P, P, need), -1), ((list_of(ODD), P, P, need), -1), ((g, N, P, need), -1), ((g, P, P, need - 1), -5), ((g, P, N, need), -5)):
+        assert lib.fira_gradient_norm(d, 1, *args, N) == want
+    for args, want in (((g, list_of(None), 1.0, P, P, need), -1), ((g, None, -1.0, P, P, need), -1), ((g, None, math.nan, P, P, need), -1), ((g, None, 1.0, N, P, need), -1)):
+        assert lib.fira_clip_gradients(d, 1, *args, N) == want
+    assert lib.fira_clip_gradients(one(out_dtype=1), 1, g, g, 1.0, P, P, need, N) == -1       # in place with another type
+    assert lib.fira_clip_gradients(one(ld_out=9), 1, g, g, 1.0, P, P, need, N) == -1          # ... or leading dimension
