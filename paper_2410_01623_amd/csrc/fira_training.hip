@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <type_traits>
 
 #include "fira_error.h"
 #include "fira_embed.h"
@@ -66,7 +67,7 @@ void with_types(int32_t a, int32_t b, F f) {
 
 fira_status check_embed(const fira_embed_desc* d, int64_t count) {
   if (!d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
-  if (d->rows < 1 || d->rows > kMost || d->dim < 1 || d->dim > kMost) return refuse(FIRA_ERR_SHAPE, "embedding table of %lld x %lld", (long long)d->rows, (long long)d->dim);
+  if (d->rows < 1 || d->rows > kMostEmbedRows || d->dim < 1 || d->dim > kMost) return refuse(FIRA_ERR_SHAPE, "embedding table of %lld x %lld", (long long)d->rows, (long long)d->dim);
   FIRA_LEADING(d->ld, d->dim, d->rows);
   if (count < 0 || count > kMost) return refuse(FIRA_ERR_SHAPE, "%lld tokens", (long long)count);
   if (!known(d->dtype) || !known(d->row_dtype)) return refuse(FIRA_ERR_DTYPE, "embedding types %d and %d", d->dtype, d->row_dtype);
@@ -77,6 +78,34 @@ fira_status check_embed(const fira_embed_desc* d, int64_t count) {
 
 FiraEmbed embed_of(const fira_embed_desc* d, int64_t count, int64_t ld_rows) {
   return FiraEmbed{(int)d->rows, d->dim, d->ld, count, ld_rows, (float)d->scale, d->id_type == FIRA_I64};
+}
+
+// The gradient's workspace.
+struct EmbedSort {
+  FiraEmbedSort s;
+  int64_t pieces;     // at most so many: rows in pieces have more than kPieceTokens tokens each
+  size_t bytes;
+};
+EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
+  EmbedSort r{};
+  FiraEmbedSort& s = r.s;
+  char* const begin = at;
+  auto take = [&](auto*& p, int64_t n) { p = (std::remove_reference_t<decltype(p)>)at; at += up256(n * sizeof *p); };
+  s.chunk = (int)std::max<int64_t>(1024, up256((count + kMostChunks - 1) / kMostChunks));
+  s.chunks = (int)std::max<int64_t>(1, (count + s.chunk - 1) / s.chunk);
+  s.bins = (int)((d->rows + kBuckets - 1) / kBuckets);
+  while (1 << s.bits < s.bins) ++s.bits;
+  r.pieces = count > kPieceTokens ? 2 * (count / kPieceTokens) : 0;
+  take(s.sorted, (int64_t)s.chunks * s.chunk);
+  take(s.part, (int64_t)kBuckets * s.chunks);
+  take(s.order, count);
+  take(s.rows, (int64_t)kBuckets * s.bins);
+  take(s.counters, 3);
+  take(s.pieces, r.pieces);
+  take(s.cut, r.pieces);
+  take(s.partial, r.pieces * d->dim);
+  r.bytes = at - begin;
+  return r;
 }
 
 fira_status check_norm(const fira_layer_norm_desc* d) {
@@ -197,7 +226,9 @@ fira_status fira_embed_lookup(const fira_embed_desc* d, const void* dev_table, c
   return launched("embedding lookup");
 }
 
-size_t fira_embed_gradient_workspace_bytes(const fira_embed_desc* d, int64_t count) { return check_embed(d, count) ? 0 : 256; }
+size_t fira_embed_gradient_workspace_bytes(const fira_embed_desc* d, int64_t count) {
+  return check_embed(d, count) ? 0 : embed_sort(d, count, nullptr).bytes;
+}
 
 fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, int64_t ld_dout, const void* dev_ids, int64_t count,
                                 void* dev_dtable, int accumulate, void* dev_workspace, size_t workspace_bytes, void* hip_stream) {
@@ -208,14 +239,30 @@ fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, 
     FIRA_POINTER(dev_ids, d->id_type == FIRA_I64 ? 8 : 4);
   }
   FIRA_POINTER(dev_dtable, size_of(d->dtype));
-  if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, fira_embed_gradient_workspace_bytes(d, count))) return st;
+  const EmbedSort sort = embed_sort(d, count, (char*)dev_workspace);
+  if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, sort.bytes)) return st;
   if (!count && accumulate) return FIRA_OK;
   const FiraEmbed e = embed_of(d, count, ld_dout);
+  const FiraEmbedSort& s = sort.s;
+  const hipStream_t q = (hipStream_t)hip_stream;
+  // (with no tokens there is one empty chunk)
+  hipLaunchKernelGGL(fira_embed_chunk_kernel, dim3(s.chunks), dim3(256), 0, q, e, dev_ids, s);
+  const int waves = std::min(16, kCounters / s.bins);
+  hipLaunchKernelGGL(fira_embed_bucket_kernel, dim3(kBuckets), dim3(64 * waves), 4 * waves * s.bins, q, e, s);
   with_types(d->dtype, d->row_dtype, [&](auto t, auto r) {
     typedef decltype(t) T;
     typedef decltype(r) R;
-    hipLaunchKernelGGL((fira_embed_gradient_kernel<T, R>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(64), 0, (hipStream_t)hip_stream, e,
-                       (const typename R::raw*)dev_dout, dev_ids, (typename T::raw*)dev_dtable, accumulate);
+    auto sum = [&](auto lanes) {
+      constexpr int LANES = decltype(lanes)::value;
+      const int64_t tiles = (d->dim + LANES * kVec - 1) / (LANES * kVec), groups = (sort.pieces + d->rows) * tiles, per = 256 / LANES;
+      hipLaunchKernelGGL((fira_embed_sum_kernel<T, R, LANES>), dim3(std::min<int64_t>((groups + per - 1) / per, 1 << 20)), dim3(256), 0, q, e,
+                         (const typename R::raw*)dev_dout, (typename T::raw*)dev_dtable, accumulate, s);
+    };
+    if (d->dim <= 64) sum(std::integral_constant<int, 8>{});
+    else if (d->dim <= 128) sum(std::integral_constant<int, 16>{});
+    else if (d->dim <= 256) sum(std::integral_constant<int, 32>{});
+    else sum(std::integral_constant<int, 64>{});
+    if (sort.pieces) hipLaunchKernelGGL(fira_embed_join_kernel<T>, dim3(std::min<int64_t>(sort.pieces, 512)), dim3(1024), 0, q, e, (typename T::raw*)dev_dtable, accumulate, s);
   });
   return launched("embedding gradient");
 }

@@ -83,6 +83,17 @@ def test_embed_gradient(tokens, vocab, dim, pad, dtype, rows_dtype):
             assert torch.equal(got[missing], old[missing])
 
 
+@pytest.mark.parametrize("tokens,vocab,dim", [(300001, 1000, 8), (20000, 300000, 8), (5000, 1 << 21, 3), (70000, 50257, 20), (40000, 7, 64)])
+def test_embed_gradient_of_many(tokens, vocab, dim):
+    """More tokens than 256 chunks of the smallest size, more rows of a bucket than it has counters for all its wavefronts, the largest table."""
+    gen = generator(tokens)
+    _, dout = matrix(tokens, dim, 0, BF16, gen)
+    ids = _skewed(tokens, vocab, gen)
+    got = training.fira_embed_gradient(dout, ids, vocab, dtype=F32)
+    want, bound = ref.embed_gradient(dout, ids, vocab, 1.0, None, F32)
+    ref.within(got, want, bound)
+
+
 @pytest.mark.parametrize("fill", [0, 499, -1, 500, 1 << 40, -(1 << 62)])
 def test_embed_gradient_of_one_id(fill):
     """All tokens the same row, or all of them padding; an id that is a row only in its low 32 bits is outside too."""

@@ -26,7 +26,7 @@ def norm(rows=10, dim=8, dtype=0, param_dtype=1, kind=0, eps=1e-5):
 
 
 def test_embedding(lib):
-    for d, count, want in ((None, 1, -1), (embed(rows=0), 1, -2), (embed(rows=1 << 31), 1, -2), (embed(dim=0), 1, -2), (embed(ld=7), 1, -2), (embed(ld=1 << 62), 1, -2),
+    for d, count, want in ((None, 1, -1), (embed(rows=0), 1, -2), (embed(rows=(1 << 21) + 1), 1, -2), (embed(rows=1 << 31), 1, -2), (embed(dim=0), 1, -2), (embed(ld=7), 1, -2), (embed(ld=1 << 62), 1, -2),
                            (embed(), -1, -2), (embed(), 1 << 31, -2), (embed(dtype=2), 1, -4), (embed(row_dtype=-1), 1, -4), (embed(id_type=2), 1, -4),
                            (embed(scale=math.nan), 1, -1), (embed(scale=1e300), 1, -1)):
         assert lib.fira_embed_lookup(d, P, P, count, P, 8, N) == want
