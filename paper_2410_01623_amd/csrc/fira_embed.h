@@ -20,18 +20,35 @@ __device__ __forceinline__ int token_row(const FiraEmbed& e, const void* ids, lo
   return v >= 0 && v < e.vocab ? v : -1;
 }
 
-// out[t] = scale * table[id_t], zeros for an id outside the table.  One workgroup per token.
-template <typename T, typename R>
+// out[t] = scale * table[id_t], zeros for an id outside the table.  A wavefront takes TOKENS tokens at a time, 64 / LANES of them side by side, and
+// NV vectors of each per lane.
+template <typename T, typename R, int W, int LANES, int NV, int TOKENS>
 __global__ __launch_bounds__(256) void fira_embed_lookup_kernel(FiraEmbed e, const typename T::raw* table, const void* ids, typename R::raw* out) {
-  for (long long t = blockIdx.x; t < e.count; t += gridDim.x) {
-    const int v = token_row(e, ids, t);
-    for (long long c = threadIdx.x * kVec; c < e.dim; c += 256 * kVec) {
-      float x[kVec] = {};
-      if (v >= 0) load_some<T>(table + v * e.ld + c, e.dim - c, x);
+  constexpr int SIDE = 64 / LANES, EACH = TOKENS / SIDE;
+  const int lane = threadIdx.x & 63;
+  const unsigned tiles = (unsigned)((e.dim + NV * LANES * W - 1) / (NV * LANES * W));
+  const long long all = (e.count + TOKENS - 1) / TOKENS * tiles;
+  for (long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += gridDim.x * 4LL) {
+    const long long unit = i / tiles, c0 = (i - unit * tiles) * (NV * LANES * W) + lane % LANES * W, t0 = unit * TOKENS + lane / LANES;
+    int row[EACH];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) x[i] *= e.scale;
-      store_some<R>(out + t * e.ld_rows + c, e.dim - c, x);
-    }
+    for (int k = 0; k < EACH; ++k) row[k] = token_row(e, ids, min(t0 + k * SIDE, e.count - 1));
+    Raw<T, W> x[EACH][NV];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) x[k][v].load(table + max(row[k], 0) * e.ld + Columns<W>(c0 + v * (LANES * W), e.dim).at);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const Columns<W> c(c0 + v * (LANES * W), e.dim);
+        const long long t = t0 + k * SIDE;
+        float y[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) y[j] = row[k] >= 0 ? e.scale * x[k][v].get(j) : 0.0f;
+        if (c.any && t < e.count) store_w<R, W>(out + t * e.ld_rows + c.at, y);
+      }
   }
 }
 
@@ -58,9 +75,9 @@ struct FiraEmbedSort {       // the sort's part of the workspace
   u32x2* part;               // [kBuckets][chunks]    first entry and number of entries of a bucket in a chunk
   unsigned* order;           // [count]               tokens by row
   u32x2* rows;               // [kBuckets][bins]      first entry in `order` and number of entries of a row
-  int* counters;             // entries of `order` handed out, pieces, rows in pieces
-  u32x2* pieces;             // (row, piece of it)
-  u32x2* cut;                // rows in pieces: (row, their first piece)
+  int* counters;             // pieces, rows in pieces
+  u32x4* pieces;             // (row, first entry of `order`, number of entries)
+  u32x4* cut;                // rows in pieces: (row, first piece, number of pieces)
   float* partial;            // [pieces][dim]
 };
 
@@ -68,8 +85,8 @@ struct FiraEmbedSort {       // the sort's part of the workspace
 __device__ __forceinline__ unsigned long long lanes_alike(unsigned key, int bits, bool in) {
   unsigned long long m = __ballot(in);
   for (int b = 0; b < bits; ++b) {
-    const unsigned long long one = __ballot((key >> b) & 1);
-    m &= (key >> b) & 1 ? one : ~one;
+    const int mine = (int)(key << (31 - b)) >> 31;      // all ones where the bit is set
+    m &= ~(__ballot(mine) ^ (unsigned long long)(long long)mine);
   }
   return m;
 }
@@ -92,27 +109,22 @@ __global__ __launch_bounds__(256) void fira_embed_chunk_kernel(FiraEmbed e, cons
   __shared__ int count[4][kBuckets];
   __shared__ int part[17];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (blockIdx.x == 0 && threadIdx.x < 3) *as_global(s.counters + threadIdx.x) = 0;   // for the next kernel
+  if (blockIdx.x == 0 && threadIdx.x < 2) *as_global(s.counters + threadIdx.x) = 0;   // for the next kernel
   for (int w = 0; w < 4; ++w) count[w][threadIdx.x] = 0;
   __syncthreads();
   const long long begin = (long long)blockIdx.x * s.chunk, end = min(begin + s.chunk, e.count);
   const long long mine = begin + wave * (s.chunk / 4), until = min(mine + s.chunk / 4, end);
-  // (a wavefront's counters are its own, and of the lanes with one bucket only the first one writes)
-  auto each = [&](auto f) {
-    for (long long t0 = mine; t0 < until; t0 += 64) {
-      const long long t = t0 + lane;
-      const int v = t < until ? token_row(e, ids, t) : -1;
-      const unsigned long long alike = lanes_alike(v & (kBuckets - 1), 8, v >= 0);
-      const unsigned long long below = alike & ((1ull << lane) - 1);
-      volatile int* const c = &count[wave][v & (kBuckets - 1)];
-      const int before = *c + __popcll(below);
-      __builtin_amdgcn_wave_barrier();
-      if (v >= 0 && !below) *c = before + __popcll(alike);
-      __builtin_amdgcn_wave_barrier();
-      if (v >= 0) f(v, t, before);
-    }
+  int id[2];                                             // a wavefront's ids, where there are so few
+  auto load = [&](long long t0) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) { const long long t = t0 + k * 64 + lane; id[k] = t < until ? token_row(e, ids, t) : -1; }
   };
-  each([](int, long long, int) {});
+  for (long long t0 = mine; t0 < until; t0 += 128) {
+    load(t0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (id[k] >= 0) atomicAdd(&count[wave][id[k] & (kBuckets - 1)], 1);
+  }
   __syncthreads();
   int sum = 0;
   for (int w = 0; w < 4; ++w) sum += count[w][threadIdx.x];
@@ -121,53 +133,88 @@ __global__ __launch_bounds__(256) void fira_embed_chunk_kernel(FiraEmbed e, cons
   *as_global(s.part + (long long)threadIdx.x * s.chunks + blockIdx.x) = u32x2{(unsigned)first, (unsigned)sum};
   for (int w = 0; w < 4; ++w) { const int c = count[w][threadIdx.x]; count[w][threadIdx.x] = first; first += c; }
   __syncthreads();
-  each([&](int v, long long t, int at) { *as_global(s.sorted + begin + at) = u32x2{(unsigned)v >> 8, (unsigned)t}; });
+  // (a wavefront's counters are its own, and of the lanes with one bucket only the first one writes)
+  for (long long t0 = mine; t0 < until; t0 += 128) {
+    if (until - mine > 128) load(t0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int v = id[k];
+      const unsigned long long alike = lanes_alike(v & (kBuckets - 1), 8, v >= 0);
+      const unsigned long long below = alike & ((1ull << lane) - 1);
+      volatile int* const c = &count[wave][v & (kBuckets - 1)];
+      const int at = *c + __popcll(below);
+      __builtin_amdgcn_wave_barrier();
+      if (v >= 0 && !below) *c = at + __popcll(alike);
+      __builtin_amdgcn_wave_barrier();
+      if (v >= 0) *as_global(s.sorted + begin + at) = u32x2{(unsigned)v >> 8, (unsigned)(t0 + k * 64 + lane)};
+    }
+  }
 }
 
+// Tokens of a piece of a row with n tokens: at most 256 pieces, which the join has to read one after the other.
+__device__ __forceinline__ int piece_tokens(int n) {
+  int len = kPieceTokens;
+  while (n > 256 * len) len *= 2;
+  return len;
+}
+
+// A wavefront takes the bucket's entries of neighbouring chunks, in groups of 64 lanes: as many chunks side by side as leave each the lanes for
+// its entries (an ordinary bucket has two or three in a chunk, the one with a text's most frequent token a tenth of the chunk).  One pass over
+// them finds each entry's place among the wavefront's own with the same row, which stays in registers until the rows' first places are known.
 // (dynamic LDS: a counter per wavefront and row of the bucket)
 __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, FiraEmbedSort s) {
+  constexpr int KEPT = 16;                              // groups whose entries stay in registers; where there are more, they are read again
   extern __shared__ int count[];
-  __shared__ int first_of[kMostChunks], at_of[kMostChunks];
+  __shared__ int at_of[kMostChunks], n_of[kMostChunks];
   __shared__ int part[17];
-  __shared__ int base_s;
+  __shared__ unsigned long long given;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, bucket = blockIdx.x;
-  int n = 0;                                            // tokens of this bucket
-  for (int c0 = 0; c0 < s.chunks; c0 += blockDim.x) {
-    const int c = c0 + threadIdx.x;
-    const u32x2 p = c < s.chunks ? *as_global(s.part + (long long)bucket * s.chunks + c) : u32x2{0, 0};
-    int total;
-    const int before = n + block_scan((int)p.y, part, &total);
-    if (c < s.chunks) { first_of[c] = before; at_of[c] = (int)p.x; }
-    n += total;
+  int before = 0;                                       // entries of the buckets before this one
+  for (int c = threadIdx.x; c < s.chunks; c += blockDim.x) {
+    const u32x2 p = *as_global(s.part + (long long)bucket * s.chunks + c);
+    at_of[c] = (int)p[0];
+    n_of[c] = (int)p[1];
+    before += (int)p[0];
   }
+  int base;
+  block_scan(before, part, &base);
   for (int i = threadIdx.x; i < waves * s.bins; i += blockDim.x) count[i] = 0;
-  // where in `order` does not matter to any result
-  if (threadIdx.x == 0) base_s = n ? atomicAdd(s.counters, n) : 0;
   __syncthreads();
-  const int base = base_s;
-  const int per = ((n + waves - 1) / waves + 63) / 64 * 64;
-  const int mine = min(wave * per, n), until = min(mine + per, n);
+  const int per = (s.chunks + waves - 1) / waves, c_mine = wave * per, c_until = min(c_mine + per, s.chunks);
+  int most = 0;                                         // entries of any of them
+  for (int c = c_mine + lane; c < c_until; c += 64) most = max(most, n_of[c]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
+  int share = 4;                                        // lanes to a chunk
+  while (share < 64 && share < most) share *= 2;
+  const int side = 64 / share, rounds = max((most + 63) / 64, 1), groups = c_mine < c_until ? (per + side - 1) / side * rounds : 0;
   volatile int* const own = count + wave * s.bins;
-  auto each = [&](auto f) {
-    for (int i0 = mine; i0 < until; i0 += 64) {
-      const int i = i0 + lane;
-      u32x2 entry{0, 0};
-      if (i < until) {
-        int c = 0;                                       // the last chunk whose first entry is not after i
-        for (int step = kMostChunks / 2; step; step >>= 1)
-          if (c + step < s.chunks && first_of[c + step] <= i) c += step;
-        entry = *as_global(s.sorted + (long long)c * s.chunk + at_of[c] + (i - first_of[c]));
-      }
-      const unsigned long long alike = lanes_alike(entry.x, s.bits, i < until);
-      const unsigned long long below = alike & ((1ull << lane) - 1);
-      const int before = own[entry.x] + __popcll(below);
-      __builtin_amdgcn_wave_barrier();
-      if (i < until && !below) own[entry.x] = before + __popcll(alike);
-      __builtin_amdgcn_wave_barrier();
-      if (i < until) f(entry.y, before);
-    }
+  // group g: round g % rounds of the chunks from c_mine + g / rounds * side on
+  auto load = [&](int g, u32x2& entry) {
+    const int c = c_mine + g / rounds * side + lane / share, j = g % rounds * 64 + lane % share;
+    entry = u32x2{~0u, 0};
+    if (g < groups && c < c_until && j < n_of[c]) entry = *as_global(s.sorted + (long long)c * s.chunk + at_of[c] + j);
   };
-  each([](unsigned, int) {});
+  auto place = [&](u32x2 entry) {                       // (of the lanes with one row only the first one writes)
+    const bool in = entry[0] != ~0u;
+    const unsigned key = in ? entry[0] : 0;
+    const unsigned long long alike = lanes_alike(key, s.bits, in);
+    const unsigned long long below = alike & ((1ull << lane) - 1);
+    const int at = own[key] + __popcll(below);
+    __builtin_amdgcn_wave_barrier();
+    if (in && !below) own[key] = at + __popcll(alike);
+    __builtin_amdgcn_wave_barrier();
+    return at;
+  };
+  u32x2 entry[KEPT];
+  int at[KEPT];
+  for (int g0 = 0; g0 < groups; g0 += KEPT) {
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) load(g0 + k, entry[k]);
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+      if (g0 + k < groups) at[k] = place(entry[k]);
+  }
   __syncthreads();
   int start = 0;
   for (int b0 = 0; b0 < s.bins; b0 += blockDim.x) {
@@ -175,107 +222,282 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
     int sum = 0;
     if (b < s.bins)
       for (int w = 0; w < waves; ++w) sum += count[w * s.bins + b];
-    int total;
-    int first = start + block_scan(sum, part, &total);
-    start += total;
-    if (b >= s.bins) continue;                          // (the barriers are behind; the next round's are in block_scan, which needs all)
-    *as_global(s.rows + (long long)bucket * s.bins + b) = u32x2{(unsigned)(base + first), (unsigned)sum};
-    if (sum > kPieceTokens) {
-      const int pieces = (sum + kPieceTokens - 1) / kPieceTokens, p = atomicAdd(s.counters + 1, pieces);
-      const unsigned row = (unsigned)b * kBuckets + bucket;
-      for (int k = 0; k < pieces; ++k) *as_global(s.pieces + p + k) = u32x2{row, (unsigned)k};
-      *as_global(s.cut + atomicAdd(s.counters + 2, 1)) = u32x2{row, (unsigned)p};
+    int here;
+    int first = start + block_scan(sum, part, &here);
+    start += here;
+    // rows in pieces: one addition per workgroup hands out the places for all of them, as those of all workgroups wait for one another
+    // (two for every such row took half of the kernel's time); which places does not matter to any result
+    const int len = piece_tokens(sum), pieces = sum > kPieceTokens ? (sum + len - 1) / len : 0;
+    if (__syncthreads_or(pieces)) {
+      int all_pieces, all_rows;
+      const int my_pieces = block_scan(pieces, part, &all_pieces), my_row = block_scan(pieces > 0, part, &all_rows);
+      if (threadIdx.x == 0) given = atomicAdd((unsigned long long*)s.counters, (unsigned long long)all_rows << 32 | (unsigned)all_pieces);
+      __syncthreads();
+      const unsigned row = (unsigned)b * kBuckets + bucket, p = (unsigned)given + my_pieces;
+      if (pieces) *as_global(s.cut + (given >> 32) + my_row) = u32x4{row, p, (unsigned)pieces, 0};
+      for (unsigned long long m = __ballot(pieces > 0); m; m &= m - 1) {      // a wavefront lists one row's pieces after the other
+        const int l = __builtin_ctzll(m), n = __builtin_amdgcn_readlane(pieces, l), size = __builtin_amdgcn_readlane(len, l);
+        const int from = base + __builtin_amdgcn_readlane(first, l), all = __builtin_amdgcn_readlane(sum, l);
+        u32x4* const to = s.pieces + (unsigned)__builtin_amdgcn_readlane((int)p, l);
+        for (int k = lane; k < n; k += 64)
+          *as_global(to + k) = u32x4{(unsigned)__builtin_amdgcn_readlane((int)row, l), (unsigned)(from + k * size), (unsigned)min(size, all - k * size), 0};
+      }
     }
+    if (b >= s.bins) continue;                          // (no barrier before the next round's)
+    *as_global(s.rows + (long long)bucket * s.bins + b) = u32x2{(unsigned)(base + first), (unsigned)sum};
     for (int w = 0; w < waves; ++w) { const int c = count[w * s.bins + b]; count[w * s.bins + b] = first; first += c; }
   }
   __syncthreads();
-  each([&](unsigned t, int at) { *as_global(s.order + base + at) = t; });
+  if (groups <= KEPT) {                                 // the first place of each row and wavefront, and the place among them
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k)
+      if (k < groups && entry[k][0] != ~0u) *as_global(s.order + base + own[entry[k][0]] + at[k]) = entry[k][1];
+  } else {
+    for (int g0 = 0; g0 < groups; g0 += KEPT) {
+#pragma unroll
+      for (int k = 0; k < KEPT; ++k) load(g0 + k, entry[k]);
+#pragma unroll
+      for (int k = 0; k < KEPT; ++k)
+        if (g0 + k < groups) {
+          const int to = place(entry[k]);
+          if (entry[k][0] != ~0u) *as_global(s.order + base + to) = entry[k][1];
+        }
+    }
+  }
 }
 
 __device__ __forceinline__ u32x2 tokens_of_row(const FiraEmbedSort& s, unsigned row) {
   return *as_global(s.rows + (long long)(row & (kBuckets - 1)) * s.bins + (row >> 8));
 }
 
-// sum += dout[order[first + i]] for i < n, columns c to c + 7, in order of i; eight rows are on their way at a time.
-template <typename R>
-__device__ __forceinline__ void sum_of_tokens(const FiraEmbed& e, const typename R::raw* dout, const unsigned* order, unsigned n, long long c, float (&sum)[kVec]) {
-  const long long left = e.dim - c;
-  for (unsigned i0 = 0; i0 < n; i0 += 8) {
-    float x[8][kVec];
+template <typename T, int W, bool ADD>
+__device__ __forceinline__ void write_gradient(const FiraEmbed& e, typename T::raw* dtable, unsigned row, const Columns<W>& c, const float (&sum)[W]) {
+  typename T::raw* const to = dtable + row * e.ld + c.at;
+  float y[W];
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (i0 + k < n) load_some<R>(dout + *as_global(order + i0 + k) * e.ld_rows + c, left, x[k]);
+  for (int j = 0; j < W; ++j) y[j] = e.scale * sum[j];
+  if constexpr (ADD) {
+    Raw<T, W> old;
+    old.load(to);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (i0 + k < n)
+    for (int j = 0; j < W; ++j) y[j] += old.get(j);
+    if (c.skip) {                                        // (the neighbour may be another wavefront, before its own reading)
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum[j] += x[k][j];
+      for (int j = 1; j < W; ++j)
+        if (j >= c.skip) store1<T>(to + j, y[j]);
+      return;
+    }
   }
-}
-template <typename T>
-__device__ __forceinline__ void write_gradient(const FiraEmbed& e, typename T::raw* dtable, unsigned row, long long c, int accumulate, float (&sum)[kVec]) {
-  typename T::raw* to = dtable + row * e.ld + c;
-  float old[kVec] = {};
-  if (accumulate) load_some<T>(to, e.dim - c, old);
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) sum[j] = old[j] + e.scale * sum[j];
-  store_some<T>(to, e.dim - c, sum);
+  store_w<T, W>(to, y);
 }
 
-// LANES lanes to a row, or to 512 columns of one; the pieces first, as they take longest.
-template <typename T, typename R, int LANES>
-__global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const typename R::raw* dout, typename T::raw* dtable, int accumulate, FiraEmbedSort s) {
-  const int lane = threadIdx.x % LANES;
-  const long long tiles = (e.dim + LANES * kVec - 1) / (LANES * kVec);
-  const long long pieces = *as_global(s.counters + 1) * tiles, all = pieces + e.vocab * tiles;
+// Loads of N rows are put on their way together, without a branch between them; beyond the last row it is loaded again.  (One copy of the loop's
+// body: with blocks of 8, 4, 2 and 1 for the remainder the wavefronts of fira_embed_sum_kernel waited for instructions half of their time.)
+
+// Widths up to 256: LANES lanes to a row; four tokens' rows are on their way at a time.  The pieces come first, as they take longest.
+template <typename T, typename R, int W, int LANES, bool ADD>
+__global__ __launch_bounds__(256) void fira_embed_sum_narrow_kernel(FiraEmbed e, const typename R::raw* dout, typename T::raw* dtable, FiraEmbedSort s) {
+  constexpr int N = 4;
+  const Columns<W> c(threadIdx.x % LANES * W, e.dim);
+  if (!c.any) return;
+  const long long pieces = *as_global(s.counters), all = pieces + e.vocab;
   for (long long i = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; i < all; i += (long long)gridDim.x * (256 / LANES)) {
     const bool piece = i < pieces;
-    const long long k = piece ? i / tiles : (i - pieces) / tiles;
-    const long long c = ((piece ? i : i - pieces) - k * tiles) * (LANES * kVec) + lane * kVec;
-    if (c >= e.dim) continue;
-    float sum[kVec] = {};
+    u32x2 r{0, 0};
     if (piece) {
-      const u32x2 p = *as_global(s.pieces + k), r = tokens_of_row(s, p.x);
-      sum_of_tokens<R>(e, dout, s.order + r.x + p.y * kPieceTokens, min((unsigned)kPieceTokens, r.y - p.y * kPieceTokens), c, sum);
-      store_some<FiraStoredF32>(s.partial + k * e.dim + c, e.dim - c, sum);
+      const u32x4 p = *as_global(s.pieces + i);
+      r = u32x2{p[1], p[2]};
     } else {
-      const u32x2 r = tokens_of_row(s, (unsigned)k);
-      if (r.y > kPieceTokens || (r.y == 0 && accumulate)) continue;
-      sum_of_tokens<R>(e, dout, s.order + r.x, r.y, c, sum);
-      write_gradient<T>(e, dtable, (unsigned)k, c, accumulate, sum);
+      r = tokens_of_row(s, (unsigned)(i - pieces));
+      if (r[1] > kPieceTokens || (ADD && r[1] == 0)) continue;
+    }
+    float sum[W] = {};
+    const unsigned* const order = s.order + r[0];
+    for (unsigned first = 0; first < r[1]; first += N) {
+      unsigned t[N];
+      Raw<R, W> x[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) t[k] = *as_global(order + min(first + k, r[1] - 1));
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k].load(dout + t[k] * e.ld_rows + c.at);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (first + k < r[1])
+#pragma unroll
+          for (int j = 0; j < W; ++j) sum[j] += x[k].get(j);
+    }
+    if (piece) store_w<FiraStoredF32, W>(s.partial + i * e.dim + c.at, sum);
+    else write_gradient<T, W, ADD>(e, dtable, (unsigned)(i - pieces), c, sum);
+  }
+}
+
+// Wider ones: a wavefront takes 512 columns of kBatch neighbouring rows of a bucket (whose tokens it finds with one load), or of a piece.
+// The tokens of all its rows make one sequence, of which eight are on their way at a time, whatever row they belong to: most rows have one
+// token or none, and one row after the other would wait for its place, its tokens and their rows in turn.
+constexpr int kBatch = 8;
+template <typename T, typename R, bool ADD>
+__global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const typename R::raw* dout, typename T::raw* dtable, FiraEmbedSort s) {
+  constexpr int W = kVec, N = 8;
+  const int lane = threadIdx.x & 63;
+  const unsigned tiles = (unsigned)((e.dim + 64 * W - 1) / (64 * W)), batches = (s.bins + kBatch - 1) / kBatch;
+  const long long pieces = (long long)*as_global(s.counters) * tiles, all = pieces + (long long)batches * kBuckets * tiles;
+  for (long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += gridDim.x * 4LL) {
+    const bool piece = i < pieces;
+    const long long unit = (piece ? i : i - pieces) / tiles;
+    const Columns<W> c(((piece ? i : i - pieces) - unit * tiles) * (64 * W) + lane * W, e.dim);
+    // lane k < kBatch: first token and number of tokens of row k
+    unsigned row0 = 0;
+    u32x2 r{0, 0};
+    if (piece) {
+      const u32x4 p = *as_global(s.pieces + unit);
+      if (lane == 0) r = u32x2{p[1], p[2]};
+    } else {
+      const unsigned bucket = (unsigned)unit & (kBuckets - 1), key0 = (unsigned)(unit >> 8) * kBatch;
+      row0 = key0 * kBuckets + bucket;                   // row k is row0 + k * kBuckets
+      if (lane < kBatch && key0 + lane < (unsigned)s.bins) r = *as_global(s.rows + (long long)bucket * s.bins + key0 + lane);
+    }
+    const int n = r[1] > kPieceTokens ? 0 : (int)r[1];
+    int upto = n;                                        // tokens of the rows up to this lane's
+#pragma unroll
+    for (int d = 1; d < kBatch; d <<= 1) { const int y = __shfl_up(upto, d, 64); upto += lane >= d ? y : 0; }
+    const int total = __builtin_amdgcn_readlane(upto, kBatch - 1);
+    float sum[W] = {};
+    if (!ADD && !piece) {
+      const bool none = r[1] == 0 && lane < kBatch && row0 + lane * kBuckets < (unsigned)e.vocab;
+      for (unsigned long long m = __ballot(none); m; m &= m - 1)
+        if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + __builtin_ctzll(m) * kBuckets, c, sum);
+    }
+    int row = -1;                                        // the one that is being summed
+    for (int j0 = 0; j0 < total; j0 += 64) {
+      // token and row of place j0 + lane in the sequence
+      const int at = min(j0 + lane, total - 1);
+      int of = 0;
+#pragma unroll
+      for (int k = 0; k < kBatch - 1; ++k) of += at >= __builtin_amdgcn_readlane(upto, k);
+      const int before = __shfl(upto, of, 64) - __shfl(n, of, 64);
+      const unsigned token = *as_global(s.order + (__shfl(r[0], of, 64) + at - before));
+      for (int first = 0; first < 64 && j0 + first < total; first += N) {
+        Raw<R, W> x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k].load(dout + (unsigned)__builtin_amdgcn_readlane(token, first + k) * e.ld_rows + c.at);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          if (j0 + first + k >= total) break;
+          const int next = __builtin_amdgcn_readlane(of, first + k);
+          if (next != row) {
+            if (row >= 0) {
+              if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + row * kBuckets, c, sum);
+#pragma unroll
+              for (int j = 0; j < W; ++j) sum[j] = 0.0f;
+            }
+            row = next;
+          }
+#pragma unroll
+          for (int j = 0; j < W; ++j) sum[j] += x[k].get(j);
+        }
+      }
+    }
+    if (row >= 0 && c.any) {
+      if (piece) store_w<FiraStoredF32, W>(s.partial + unit * e.dim + c.at, sum);
+      else write_gradient<T, W, ADD>(e, dtable, row0 + row * kBuckets, c, sum);
     }
   }
 }
 
-// 512 columns of a row in pieces per workgroup: its wavefronts take every 16th piece each, and their sums are added in turn.
-template <typename T>
-__global__ __launch_bounds__(1024) void fira_embed_join_kernel(FiraEmbed e, typename T::raw* dtable, int accumulate, FiraEmbedSort s) {
-  __shared__ float part[16][64 * kVec];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long tiles = (e.dim + 64 * kVec - 1) / (64 * kVec), all = *as_global(s.counters + 2) * tiles;
+// 32 W columns of a row in pieces per workgroup: its eight half wavefronts take every eighth piece each, and their sums are added in turn.  (With
+// 64 W columns and sixteen wavefronts the chip holds fewer rows at a time than a text of 131072 tokens has, and a row is mostly latency.)
+template <typename T, int W, bool ADD>
+__global__ __launch_bounds__(256) void fira_embed_join_kernel(FiraEmbed e, typename T::raw* dtable, FiraEmbedSort s) {
+  constexpr int PARTS = 8, N = 8;
+  __shared__ float part[PARTS][32 * W];
+  const int lane = threadIdx.x & 31, mine = threadIdx.x >> 5;
+  const long long tiles = (e.dim + 32 * W - 1) / (32 * W), all = *as_global(s.counters + 1) * tiles;
   for (long long i = blockIdx.x; i < all; i += gridDim.x) {
-    const u32x2 row = *as_global(s.cut + i / tiles);
-    const long long c = i % tiles * (64 * kVec) + lane * kVec;
-    const unsigned pieces = (tokens_of_row(s, row.x).y + kPieceTokens - 1) / kPieceTokens;
-    float sum[kVec] = {};
-    if (c < e.dim)
-#pragma unroll 4
-      for (unsigned k = wave; k < pieces; k += 16) {
-        float x[kVec];
-        load_some<FiraStoredF32>(s.partial + (long long)(row.y + k) * e.dim + c, e.dim - c, x);
+    const u32x4 row = *as_global(s.cut + i / tiles);
+    const Columns<W> c(i % tiles * (32 * W) + lane * W, e.dim);
+    const int pieces = (int)row[2];
+    const float* const from = s.partial + (long long)row[1] * e.dim + c.at;
+    float sum[W] = {};
+    for (int first = mine; first < pieces; first += PARTS * N) {
+      Raw<FiraStoredF32, W> x[N];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum[j] += x[j];
+      for (int k = 0; k < N; ++k) x[k].load(from + (long long)min(first + PARTS * k, pieces - 1) * e.dim);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (first + PARTS * k < pieces)
+#pragma unroll
+          for (int j = 0; j < W; ++j) sum[j] += x[k].get(j);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < W; ++j) part[mine][j * 32 + lane] = sum[j];
+    __syncthreads();
+    if (mine == 0 && c.any) {
+#pragma unroll
+      for (int w = 1; w < PARTS; ++w)
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] += part[w][j * 32 + lane];
+      write_gradient<T, W, ADD>(e, dtable, row[0], c, sum);
+    }
+  }
+}
+
+// Few tokens: no sort, every wavefront looks through all ids for kBatch neighbouring rows of the table and 64 W columns.
+constexpr int kFewTokens = 512;
+template <typename T, typename R, int W, bool ADD>
+__global__ __launch_bounds__(256) void fira_embed_few_kernel(FiraEmbed e, const typename R::raw* dout, const void* ids, typename T::raw* dtable) {
+  constexpr int N = 8;
+  __shared__ short found[4][kFewTokens];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned tiles = (unsigned)((e.dim + 64 * W - 1) / (64 * W));
+  const long long all = (e.vocab + kBatch - 1LL) / kBatch * tiles;
+  int id[kFewTokens / 64];
+#pragma unroll
+  for (int g = 0; g < kFewTokens / 64; ++g) id[g] = g * 64 + lane < e.count ? token_row(e, ids, g * 64 + lane) : -1;
+  volatile short* const mine = found[wave];
+  for (long long i = (long long)blockIdx.x * 4 + wave; i < all; i += gridDim.x * 4LL) {
+    const long long unit = i / tiles;
+    const Columns<W> c((i - unit * tiles) * (64 * W) + lane * W, e.dim);
+    const int row0 = (int)unit * kBatch, rows = min(kBatch, e.vocab - row0);
+    unsigned named = 0;                                  // rows of these with a token
+#pragma unroll
+    for (int g = 0; g < kFewTokens / 64; ++g) {
+      unsigned long long m = __ballot((unsigned)(id[g] - row0) < (unsigned)rows && id[g] >= 0);
+      for (; m; m &= m - 1) named |= 1u << (__builtin_amdgcn_readlane(id[g], __builtin_ctzll(m)) - row0);
+    }
+    for (int k = 0; k < rows; ++k) {
+      float sum[W] = {};
+      if (named >> k & 1) {
+        int total = 0;                                   // its tokens, in order
+#pragma unroll
+        for (int g = 0; g < kFewTokens / 64; ++g) {
+          const bool is = id[g] == row0 + k;
+          const unsigned long long m = __ballot(is);
+          if (is) mine[total + __popcll(m & ((1ull << lane) - 1))] = (short)(g * 64 + lane);
+          total += __popcll(m);
+        }
+        __builtin_amdgcn_wave_barrier();
+        for (int p0 = 0; p0 < total; p0 += kPieceTokens) {     // in pieces as by the other kernels
+          float piece[W] = {};
+          const int until = min(p0 + kPieceTokens, total);
+          const int token = mine[min(p0 + (lane & (kPieceTokens - 1)), until - 1)];
+          for (int first = 0; p0 + first < until; first += N) {
+            Raw<R, W> x[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) x[u].load(dout + (long long)__builtin_amdgcn_readlane(token, first + u) * e.ld_rows + c.at);
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+              if (p0 + first + u < until)
+#pragma unroll
+                for (int j = 0; j < W; ++j) piece[j] += x[u].get(j);
+          }
+#pragma unroll
+          for (int j = 0; j < W; ++j) sum[j] += piece[j];
+        }
+      } else if (ADD) {
+        continue;
       }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) part[wave][lane * kVec + j] = sum[j];
-    __syncthreads();
-    if (wave == 0 && c < e.dim) {
-#pragma unroll 1
-      for (int w = 1; w < 16; ++w)
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) sum[j] += part[w][lane * kVec + j];
-      write_gradient<T>(e, dtable, row.x, c, accumulate, sum);
+      if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + k, c, sum);
     }
   }
 }

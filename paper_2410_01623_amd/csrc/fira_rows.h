@@ -57,6 +57,44 @@ __device__ __forceinline__ void store_some(typename T::raw* p, long long n, cons
     if (i < n) store1<T>(p + i, v[i]);
 }
 
+// W neighbouring values (8, or 1 for rows shorter than 8) as they are stored: what is on its way is held like this, in half the
+// registers where it is bf16.  One load each, without a branch, so that many stay on their way.
+template <typename T, int W>
+struct Raw;
+template <>
+struct Raw<FiraStoredF32, 8> {
+  f32x4 a, b;
+  __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+  __device__ __forceinline__ void load(const float* p) { a = *(gptr<const f32x4_a4>)as_global(p); b = *(gptr<const f32x4_a4>)as_global(p + 4); }
+};
+template <>
+struct Raw<FiraStoredBf16, 8> {
+  u32x4 a;
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? a[i / 2] & 0xffff0000u : a[i / 2] << 16); }
+  __device__ __forceinline__ void load(const bf16_raw* p) { a = *(gptr<const u32x4_a2>)as_global(p); }
+};
+template <typename T>
+struct Raw<T, 1> {
+  float a;
+  __device__ __forceinline__ float get(int) const { return a; }
+  __device__ __forceinline__ void load(const typename T::raw* p) { a = load1<T>(p); }
+};
+template <typename T, int W>
+__device__ __forceinline__ void store_w(typename T::raw* p, const float (&v)[W]) {
+  if constexpr (W == 8) store8<T>(p, v);
+  else store1<T>(p, v[0]);
+}
+
+// A lane's W columns of rows that are `dim` >= W wide, by rights those from `c` on.  At the end of a row they start earlier, so that they are
+// whole: the first `skip` of them are a neighbour's as well, who computes the same for them.  A lane beyond the end has none of its own.
+template <int W>
+struct Columns {
+  long long at;
+  int skip;
+  bool any;
+  __device__ __forceinline__ Columns(long long c, long long dim) : at(min(c, dim - W)), skip((int)(c - min(c, dim - W))), any(c < dim) {}
+};
+
 // Sum over the 64 lanes of a wavefront, in every lane.
 template <typename F>
 __device__ __forceinline__ F wave_sum(F x) {

@@ -33,6 +33,9 @@ fira_status launched(const char* what) {
   return e == hipSuccess ? FIRA_OK : refuse(FIRA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 bool known(int32_t dtype) { return dtype == FIRA_F32 || dtype == FIRA_BF16; }
 size_t size_of(int32_t dtype) { return dtype == FIRA_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -65,6 +68,13 @@ void with_types(int32_t a, int32_t b, F f) {
   else { if (b == FIRA_F32) f(FiraStoredBf16{}, FiraStoredF32{}); else f(FiraStoredBf16{}, FiraStoredBf16{}); }
 }
 
+// Calls f with `flag` as a constant.
+template <typename F>
+void with_flag(bool flag, F f) {
+  if (flag) f(std::true_type{});
+  else f(std::false_type{});
+}
+
 fira_status check_embed(const fira_embed_desc* d, int64_t count) {
   if (!d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
   if (d->rows < 1 || d->rows > kMostEmbedRows || d->dim < 1 || d->dim > kMost) return refuse(FIRA_ERR_SHAPE, "embedding table of %lld x %lld", (long long)d->rows, (long long)d->dim);
@@ -89,18 +99,19 @@ struct EmbedSort {
 EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
   EmbedSort r{};
   FiraEmbedSort& s = r.s;
+  if (count <= kFewTokens) { r.bytes = 256; return r; }      // no sort
   char* const begin = at;
   auto take = [&](auto*& p, int64_t n) { p = (std::remove_reference_t<decltype(p)>)at; at += up256(n * sizeof *p); };
-  s.chunk = (int)std::max<int64_t>(1024, up256((count + kMostChunks - 1) / kMostChunks));
+  s.chunk = (int)std::max<int64_t>(512, up256((count + kMostChunks - 1) / kMostChunks));
   s.chunks = (int)std::max<int64_t>(1, (count + s.chunk - 1) / s.chunk);
   s.bins = (int)((d->rows + kBuckets - 1) / kBuckets);
   while (1 << s.bits < s.bins) ++s.bits;
-  r.pieces = count > kPieceTokens ? 2 * (count / kPieceTokens) : 0;
+  r.pieces = 2 * (count / kPieceTokens);
   take(s.sorted, (int64_t)s.chunks * s.chunk);
   take(s.part, (int64_t)kBuckets * s.chunks);
   take(s.order, count);
   take(s.rows, (int64_t)kBuckets * s.bins);
-  take(s.counters, 3);
+  take(s.counters, 2);
   take(s.pieces, r.pieces);
   take(s.cut, r.pieces);
   take(s.partial, r.pieces * d->dim);
@@ -220,8 +231,17 @@ fira_status fira_embed_lookup(const fira_embed_desc* d, const void* dev_table, c
   with_types(d->dtype, d->row_dtype, [&](auto t, auto r) {
     typedef decltype(t) T;
     typedef decltype(r) R;
-    hipLaunchKernelGGL((fira_embed_lookup_kernel<T, R>), dim3(std::min<int64_t>(count, 1 << 20)), dim3(256), 0, (hipStream_t)hip_stream, e,
-                       (const typename T::raw*)dev_table, dev_ids, (typename R::raw*)dev_out);
+    auto launch = [&](auto w, auto lanes, auto nv, auto tokens) {
+      constexpr int W = decltype(w)::value, LANES = decltype(lanes)::value, NV = decltype(nv)::value, TOKENS = decltype(tokens)::value;
+      const int64_t units = (count + TOKENS - 1) / TOKENS * ((d->dim + NV * LANES * W - 1) / (NV * LANES * W));
+      hipLaunchKernelGGL((fira_embed_lookup_kernel<T, R, W, LANES, NV, TOKENS>), dim3(std::min<int64_t>((units + 3) / 4, 1 << 20)), dim3(256), 0,
+                         (hipStream_t)hip_stream, e, (const typename T::raw*)dev_table, dev_ids, (typename R::raw*)dev_out);
+    };
+    if (d->dim < kVec) launch(Int<1>{}, Int<8>{}, Int<1>{}, Int<8>{});
+    else if (d->dim <= 64) launch(Int<kVec>{}, Int<8>{}, Int<1>{}, Int<16>{});
+    else if (d->dim <= 128) launch(Int<kVec>{}, Int<16>{}, Int<1>{}, Int<8>{});
+    else if (d->dim <= 256) launch(Int<kVec>{}, Int<32>{}, Int<1>{}, Int<4>{});
+    else launch(Int<kVec>{}, Int<64>{}, Int<1>{}, Int<4>{});
   });
   return launched("embedding lookup");
 }
@@ -243,26 +263,45 @@ fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, 
   if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, sort.bytes)) return st;
   if (!count && accumulate) return FIRA_OK;
   const FiraEmbed e = embed_of(d, count, ld_dout);
-  const FiraEmbedSort& s = sort.s;
+  const FiraEmbedSort& s = sort.s;   // (not made for few tokens)
   const hipStream_t q = (hipStream_t)hip_stream;
-  // (with no tokens there is one empty chunk)
-  hipLaunchKernelGGL(fira_embed_chunk_kernel, dim3(s.chunks), dim3(256), 0, q, e, dev_ids, s);
-  const int waves = std::min(16, kCounters / s.bins);
-  hipLaunchKernelGGL(fira_embed_bucket_kernel, dim3(kBuckets), dim3(64 * waves), 4 * waves * s.bins, q, e, s);
   with_types(d->dtype, d->row_dtype, [&](auto t, auto r) {
     typedef decltype(t) T;
     typedef decltype(r) R;
-    auto sum = [&](auto lanes) {
-      constexpr int LANES = decltype(lanes)::value;
-      const int64_t tiles = (d->dim + LANES * kVec - 1) / (LANES * kVec), groups = (sort.pieces + d->rows) * tiles, per = 256 / LANES;
-      hipLaunchKernelGGL((fira_embed_sum_kernel<T, R, LANES>), dim3(std::min<int64_t>((groups + per - 1) / per, 1 << 20)), dim3(256), 0, q, e,
-                         (const typename R::raw*)dev_dout, (typename T::raw*)dev_dtable, accumulate, s);
-    };
-    if (d->dim <= 64) sum(std::integral_constant<int, 8>{});
-    else if (d->dim <= 128) sum(std::integral_constant<int, 16>{});
-    else if (d->dim <= 256) sum(std::integral_constant<int, 32>{});
-    else sum(std::integral_constant<int, 64>{});
-    if (sort.pieces) hipLaunchKernelGGL(fira_embed_join_kernel<T>, dim3(std::min<int64_t>(sort.pieces, 512)), dim3(1024), 0, q, e, (typename T::raw*)dev_dtable, accumulate, s);
+    const typename R::raw* const dout = (const typename R::raw*)dev_dout;
+    typename T::raw* const dtable = (typename T::raw*)dev_dtable;
+    const int64_t dim = d->dim;
+    auto grid = [](int64_t units, int64_t per) { return dim3(std::min<int64_t>((units + per - 1) / per, 1 << 20)); };
+    with_flag(accumulate, [&](auto add) {
+      constexpr bool ADD = decltype(add)::value;
+      if (count <= kFewTokens) {
+        auto few = [&](auto w) {
+          constexpr int W = decltype(w)::value;
+          hipLaunchKernelGGL((fira_embed_few_kernel<T, R, W, ADD>), grid((d->rows + kBatch - 1) / kBatch * ((dim + 64 * W - 1) / (64 * W)), 4), dim3(256), 0, q, e,
+                             dout, dev_ids, dtable);
+        };
+        if (dim < kVec) few(Int<1>{});
+        else few(Int<kVec>{});
+        return;
+      }
+      hipLaunchKernelGGL(fira_embed_chunk_kernel, dim3(s.chunks), dim3(256), 0, q, e, dev_ids, s);
+      const int waves = std::min(16, kCounters / s.bins);
+      hipLaunchKernelGGL(fira_embed_bucket_kernel, dim3(kBuckets), dim3(64 * waves), 4 * waves * s.bins, q, e, s);
+      auto narrow = [&](auto w, auto lanes) {
+        constexpr int W = decltype(w)::value, LANES = decltype(lanes)::value;
+        hipLaunchKernelGGL((fira_embed_sum_narrow_kernel<T, R, W, LANES, ADD>), grid(sort.pieces + d->rows, 256 / LANES), dim3(256), 0, q, e, dout, dtable, s);
+      };
+      const int64_t batches = (int64_t)((s.bins + kBatch - 1) / kBatch) * kBuckets;
+      if (dim < kVec) narrow(Int<1>{}, Int<8>{});
+      else if (dim <= 64) narrow(Int<kVec>{}, Int<8>{});
+      else if (dim <= 128) narrow(Int<kVec>{}, Int<16>{});
+      else if (dim <= 256) narrow(Int<kVec>{}, Int<32>{});
+      else hipLaunchKernelGGL((fira_embed_sum_kernel<T, R, ADD>), grid((sort.pieces + batches) * ((dim + 64 * kVec - 1) / (64 * kVec)), 4), dim3(256), 0, q, e, dout, dtable, s);
+      // (a row in pieces has kPieceTokens + 1 tokens at least)
+      const dim3 joins(std::min<int64_t>(count / (kPieceTokens + 1) * ((dim + 32 * kVec - 1) / (32 * kVec)), 4096));
+      if (dim < kVec) hipLaunchKernelGGL((fira_embed_join_kernel<T, 1, ADD>), joins, dim3(256), 0, q, e, dtable, s);
+      else hipLaunchKernelGGL((fira_embed_join_kernel<T, kVec, ADD>), joins, dim3(256), 0, q, e, dtable, s);
+    });
   });
   return launched("embedding gradient");
 }
