@@ -48,29 +48,6 @@ __device__ __forceinline__ float bias_correction(const FiraHp& hp, int t) {
   return (float)(sqrt(lane_value(p, 0)) / lane_value(p, 32));
 }
 
-// x of lane l ^ OFF, and x plus that, between registers (a shuffle goes through LDS, ten times as far): sums over the lanes of a factor
-// are chains of them.  Called by whole wavefronts.
-typedef unsigned u32x2_s __attribute__((__vector_size__(2 * sizeof(unsigned))));
-template <int CTRL>
-__device__ __forceinline__ float dpp_move(float x) { return __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xf, 0xf, true)); }
-template <int OFF>
-__device__ __forceinline__ float lane_xor(float x) {
-  static_assert(OFF == 1 || OFF == 2 || OFF == 4 || OFF == 8, "inside a row of 16 lanes");
-  if (OFF == 1) return dpp_move<0xb1>(x);                       // quad_perm 1 0 3 2
-  if (OFF == 2) return dpp_move<0x4e>(x);                       // quad_perm 2 3 0 1
-  if (OFF == 4) return dpp_move<0x1b>(dpp_move<0x141>(x));      // l ^ 7 (row_half_mirror), then ^ 3 (quad_perm 3 2 1 0)
-  return dpp_move<0x128>(x);                                    // row_ror 8
-}
-template <int OFF>
-__device__ __forceinline__ float add_xor(float x) {
-  if constexpr (OFF < 16) {
-    return x + lane_xor<OFF>(x);
-  } else {      // the swap leaves both lanes' values in every lane
-    const unsigned u = __float_as_uint(x);
-    const u32x2_s s = OFF == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-}
 // Sum over the LPR lanes that share a factor's row.
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x) {

@@ -8,27 +8,253 @@ struct FiraNorm {
   long long ld_dx;
   float eps;
   int rms;                   // 1: no mean
-  int accumulate;            // backward: the weight's and the bias's gradients are added to what is there
 };
 
-// mu = mean x, rstd = (mean (x - mu)^2 + eps)^-1/2, y = w (x - mu) rstd + b.  One workgroup per row; mean before deviation, as their
-// difference of large sums would cancel.
+// A row is held in registers by THREADS threads, NV vectors of W values to a thread (all but the last one of them inside the row), a part of a
+// wavefront, a wavefront or a workgroup as its width asks for, so that it is read once and its sums are taken of what is there.
+// kNormWidest: widest row that is held; wider ones are read again for every sum.
+constexpr int kNormWidest = 1024 * 2 * kVec;
+
+// Sums of two values over a row's threads, in all of them.  part: LDS, two sets in turn, so that one barrier a row is enough.
+template <int THREADS>
+__device__ __forceinline__ void row_sums(float& a, float& b, float (*part)[16][2], int turn) {
+  a = lanes_sum<THREADS < 64 ? THREADS : 64>(a);
+  b = lanes_sum<THREADS < 64 ? THREADS : 64>(b);
+  if constexpr (THREADS > 64) {
+    if ((threadIdx.x & 63) == 0) { part[turn & 1][threadIdx.x >> 6][0] = a; part[turn & 1][threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      const int wave = THREADS < 256 ? threadIdx.x / THREADS * (THREADS / 64) + w : w;
+      a += part[turn & 1][wave][0];
+      b += part[turn & 1][wave][1];
+    }
+  }
+}
+
+// mu = mean x, rstd = (mean (x - mu)^2 + eps)^-1/2, y = w (x - mu) rstd + b.  The deviation is taken from x - mu: E x^2 - mu^2 would cancel.
+template <typename T, typename P, int W, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm_kernel(FiraNorm n, const typename T::raw* x, const typename P::raw* w,
+                                                                                        const typename P::raw* b, typename T::raw* y, float* mean, float* rstd) {
+  constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
+  __shared__ float part[2][16][2];
+  const int me = threadIdx.x % THREADS;
+  int turn = 0;
+  for (long long row0 = (long long)blockIdx.x * GROUPS; row0 < n.rows; row0 += (long long)gridDim.x * GROUPS) {
+    const long long row = row0 + threadIdx.x / THREADS;
+    const bool here = row < n.rows;
+    const typename T::raw* const xr = x + (here ? row : n.rows - 1) * n.ld_x;
+    Raw<T, W> xs[NV];
+    Raw<P, W> ws[NV], bs[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) xs[v].load(xr + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+    if (w)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) ws[v].load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+    if (b)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) bs[v].load(b + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+    const Columns<W> last((long long)((NV - 1) * THREADS + me) * W, n.dim);
+    const int skip = last.any ? last.skip : W;           // values of the last vector that are not this thread's
+    float mu = 0.0f, none = 0.0f;
+    if (!n.rms) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) mu += v < NV - 1 || j >= skip ? xs[v].get(j) : 0.0f;
+      row_sums<THREADS>(mu, none, part, turn++);
+      mu /= (float)n.dim;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float d = xs[v].get(j) - mu;
+        s += v < NV - 1 || j >= skip ? d * d : 0.0f;
+      }
+    row_sums<THREADS>(s, none, part, turn++);
+    const float r = 1.0f / sqrtf(s / (float)n.dim + n.eps);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        o[j] = (xs[v].get(j) - mu) * r;
+        if (w) o[j] *= ws[v].get(j);
+        if (b) o[j] += bs[v].get(j);
+      }
+      if (here && c.any) store_w<T, W>(y + row * n.ld_y + c.at, o);
+    }
+    if (here && me == 0) {
+      if (mean) *as_global(mean + row) = mu;
+      if (rstd) *as_global(rstd + row) = r;
+    }
+  }
+}
+
+// g = w dy, h = (x - mu) rstd:  dx = rstd (g - mean g - h mean(g h)), without mean g where there is no mean;  dw = sum over rows of dy h,
+// db = sum over rows of dy.  One pass: a workgroup takes every gridDim.x-th row (or set of rows side by side), the next one's values on their way
+// while it works on one, and adds up dy h and dy of its columns in registers; fira_layer_norm_join_kernel adds up the workgroups' sums.
+// partial: [2][gridDim.x][dim].
+template <typename T, typename P, int W, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm_gradient_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x,
+                                                                                                 const typename P::raw* w, const float* mean, const float* rstd,
+                                                                                                 typename T::raw* dx, float* partial_w, float* partial_b) {
+  constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
+  constexpr int BUFS = THREADS * NV > 1024 ? 1 : 2;      // (there are no registers for two rows then)
+  __shared__ float part[2][16][2];
+  __shared__ float joined[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? THREADS * W : 1];
+  const int me = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
+  Raw<P, W> ws[NV];
+  if (w)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) ws[v].load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+  const Columns<W> last((long long)((NV - 1) * THREADS + me) * W, n.dim);
+  const int skip = last.any ? last.skip : W;
+  float sw[NV][W] = {}, sb[NV][W] = {};
+  Raw<T, W> xs[BUFS][NV], gs[BUFS][NV];
+  float mus[BUFS], rs[BUFS];
+  const long long step = (long long)gridDim.x * GROUPS;
+  auto load = [&](int to, long long row) {
+    row = min(row, n.rows - 1);
+    mus[to] = n.rms ? 0.0f : *as_global(mean + row);
+    rs[to] = *as_global(rstd + row);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const long long c = Columns<W>((long long)(v * THREADS + me) * W, n.dim).at;
+      xs[to][v].load(x + row * n.ld_x + c);
+      gs[to][v].load(dy + row * n.ld_y + c);
+    }
+  };
+  int turn = 0;
+  auto work = [&](int of, long long row0) {
+    const long long row = row0 + group;
+    const bool here = row < n.rows;
+    const float mu = mus[of], r = here ? rs[of] : 0.0f;
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float d = here ? gs[of][v].get(j) : 0.0f, h = (xs[of][v].get(j) - mu) * r, g = w ? d * ws[v].get(j) : d;
+        const bool mine = v < NV - 1 || j >= skip;
+        s1 += mine ? g : 0.0f;
+        s2 += mine ? g * h : 0.0f;
+        sw[v][j] += here ? d * h : 0.0f;
+        sb[v][j] += d;
+      }
+    row_sums<THREADS>(s1, s2, part, turn++);
+    s1 = n.rms ? 0.0f : s1 / (float)n.dim;
+    s2 = s2 / (float)n.dim;
+    if (dx && here)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+        float o[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float h = (xs[of][v].get(j) - mu) * r, g = w ? gs[of][v].get(j) * ws[v].get(j) : gs[of][v].get(j);
+          o[j] = r * (g - s1 - h * s2);
+        }
+        if (c.any) store_w<T, W>(dx + row * n.ld_dx + c.at, o);
+      }
+  };
+  // (two rows a turn, so that which registers hold which is known to the compiler)
+  long long row0 = (long long)blockIdx.x * GROUPS;
+  if constexpr (BUFS == 1) {
+    for (; row0 < n.rows; row0 += step) { load(0, row0 + group); work(0, row0); }
+  } else {
+    load(0, row0 + group);
+    for (; row0 < n.rows; row0 += 2 * step) {
+      load(1, row0 + step + group);
+      work(0, row0);
+      if (row0 + step >= n.rows) break;
+      load(0, row0 + 2 * step + group);
+      work(1, row0 + step);
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* const partial = which ? partial_b : partial_w;
+    if (!partial) continue;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float (&s)[W] = which ? sb[v] : sw[v];
+      if constexpr (GROUPS > 1) {
+        __syncthreads();
+        if (group)
+#pragma unroll
+          for (int j = 0; j < W; ++j) joined[group - 1][j * THREADS + me] = s[j];
+        __syncthreads();
+        if (group) continue;
+#pragma unroll 4
+        for (int k = 0; k < GROUPS - 1; ++k)
+#pragma unroll
+          for (int j = 0; j < W; ++j) s[j] += joined[k][j * THREADS + me];
+      }
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      if (c.any) store_w<FiraStoredF32, W>(partial + (long long)blockIdx.x * n.dim + c.at, s);
+    }
+  }
+}
+
+// Sums of the parts: a workgroup takes 32 columns of dw (blockIdx.y 0) or db (1), a part of the parts to each of its 32 sets of eight lanes.
+template <typename P>
+__global__ __launch_bounds__(256) void fira_layer_norm_join_kernel(const float* partial_w, const float* partial_b, int parts, long long dim, typename P::raw* dw,
+                                                                   typename P::raw* db, int accumulate) {
+  constexpr int SETS = 32, N = 8;
+  __shared__ float sums[SETS][33];
+  const float* const partial = blockIdx.y ? partial_b : partial_w;
+  typename P::raw* const to = blockIdx.y ? db : dw;
+  if (!to) return;
+  const int lane = threadIdx.x % 8, set = threadIdx.x / 8;
+  const long long c0 = blockIdx.x * 32LL;
+  const int cols = (int)min(32LL, dim - c0);
+  float s[4] = {};
+  for (int p0 = set; p0 < parts; p0 += SETS * N) {
+    float x[N][4];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float* const from = partial + (long long)min(p0 + SETS * k, parts - 1) * dim + c0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[k][j] = *as_global(from + min(j * 8 + lane, cols - 1));
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (p0 + SETS * k < parts)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += x[k][j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sums[set][j * 8 + lane] = s[j];
+  __syncthreads();
+  if (threadIdx.x >= cols) return;
+  float all = 0.0f;
+#pragma unroll
+  for (int k = 0; k < SETS; ++k) all += sums[k][threadIdx.x];
+  store1<P>(to + c0 + threadIdx.x, accumulate ? load1<P>(to + c0 + threadIdx.x) + all : all);
+}
+
+// Rows wider than kNormWidest: one workgroup per row, which reads it for each sum and for the result.
 template <typename T, typename P>
-__global__ __launch_bounds__(256) void fira_layer_norm_kernel(FiraNorm n, const typename T::raw* x, const typename P::raw* w, const typename P::raw* b,
-                                                              typename T::raw* y, float* mean, float* rstd) {
-  __shared__ float part[4];
+__global__ __launch_bounds__(1024) void fira_layer_norm_wide_kernel(FiraNorm n, const typename T::raw* x, const typename P::raw* w, const typename P::raw* b,
+                                                                    typename T::raw* y, float* mean, float* rstd) {
+  __shared__ float part[16];
   for (long long row = blockIdx.x; row < n.rows; row += gridDim.x) {
     const typename T::raw* xr = x + row * n.ld_x;
     float mu = 0.0f;
     if (!n.rms) {
       float s = 0.0f;
-      for (long long c = threadIdx.x; c < n.dim; c += 256) s += load1<T>(xr + c);
+      for (long long c = threadIdx.x; c < n.dim; c += 1024) s += load1<T>(xr + c);
       mu = block_sum(s, part) / (float)n.dim;
     }
     float s = 0.0f;
-    for (long long c = threadIdx.x; c < n.dim; c += 256) { const float d = load1<T>(xr + c) - mu; s += d * d; }
+    for (long long c = threadIdx.x; c < n.dim; c += 1024) { const float d = load1<T>(xr + c) - mu; s += d * d; }
     const float r = 1.0f / sqrtf(block_sum(s, part) / (float)n.dim + n.eps);
-    for (long long c = threadIdx.x; c < n.dim; c += 256) {
+    for (long long c = threadIdx.x; c < n.dim; c += 1024) {
       const float h = (load1<T>(xr + c) - mu) * r;
       store1<T>(y + row * n.ld_y + c, (w ? load1<P>(w + c) : 1.0f) * h + (b ? load1<P>(b + c) : 0.0f));
     }
@@ -38,49 +264,39 @@ __global__ __launch_bounds__(256) void fira_layer_norm_kernel(FiraNorm n, const 
     }
   }
 }
-
-// g = w dy, h = (x - mu) rstd:  dx = rstd (g - mean g - h mean(g h)), without mean g where there is no mean.
 template <typename T, typename P>
-__global__ __launch_bounds__(256) void fira_layer_norm_dx_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x, const typename P::raw* w,
-                                                                 const float* mean, const float* rstd, typename T::raw* dx) {
-  __shared__ float part[4];
+__global__ __launch_bounds__(1024) void fira_layer_norm_wide_dx_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x, const typename P::raw* w,
+                                                                       const float* mean, const float* rstd, typename T::raw* dx) {
+  __shared__ float part[16];
   for (long long row = blockIdx.x; row < n.rows; row += gridDim.x) {
     const float mu = n.rms ? 0.0f : *as_global(mean + row), r = *as_global(rstd + row);
     float s1 = 0.0f, s2 = 0.0f;
-    for (long long c = threadIdx.x; c < n.dim; c += 256) {
+    for (long long c = threadIdx.x; c < n.dim; c += 1024) {
       const float g = load1<T>(dy + row * n.ld_y + c) * (w ? load1<P>(w + c) : 1.0f);
       s1 += g;
       s2 += g * (load1<T>(x + row * n.ld_x + c) - mu) * r;
     }
     s1 = n.rms ? 0.0f : block_sum(s1, part) / (float)n.dim;
     s2 = block_sum(s2, part) / (float)n.dim;
-    for (long long c = threadIdx.x; c < n.dim; c += 256) {
+    for (long long c = threadIdx.x; c < n.dim; c += 1024) {
       const float g = load1<T>(dy + row * n.ld_y + c) * (w ? load1<P>(w + c) : 1.0f);
       const float h = (load1<T>(x + row * n.ld_x + c) - mu) * r;
       store1<T>(dx + row * n.ld_dx + c, r * (g - s1 - h * s2));
     }
   }
 }
-
-// dw = sum over rows of dy h, db = sum over rows of dy.  One workgroup per 64 columns, a quarter of the rows to each wavefront.
-template <typename T, typename P>
-__global__ __launch_bounds__(256) void fira_layer_norm_dw_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x, const float* mean,
-                                                                 const float* rstd, typename P::raw* dw, typename P::raw* db) {
-  __shared__ float part[2][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long c = blockIdx.x * 64LL + lane;
+// ... and the sums over rows, gridDim.y-th part of them: 256 columns per workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void fira_layer_norm_wide_dw_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x, const float* mean,
+                                                                      const float* rstd, float* partial_w, float* partial_b) {
+  const long long c = blockIdx.x * 256LL + threadIdx.x;
+  if (c >= n.dim) return;
   float sw = 0.0f, sb = 0.0f;
-  if (c < n.dim)
-    for (long long row = wave; row < n.rows; row += 4) {
-      const float g = load1<T>(dy + row * n.ld_y + c);
-      sb += g;
-      sw += g * (load1<T>(x + row * n.ld_x + c) - (n.rms ? 0.0f : *as_global(mean + row))) * *as_global(rstd + row);
-    }
-  part[0][wave][lane] = sw;
-  part[1][wave][lane] = sb;
-  __syncthreads();
-  if (wave || c >= n.dim) return;
-  for (int k = 1; k < 4; ++k) { sw += part[0][k][lane]; sb += part[1][k][lane]; }
-  if (dw) store1<P>(dw + c, (n.accumulate ? load1<P>(dw + c) : 0.0f) + sw);
-  if (db) store1<P>(db + c, (n.accumulate ? load1<P>(db + c) : 0.0f) + sb);
+  for (long long row = blockIdx.y; row < n.rows; row += gridDim.y) {
+    const float g = load1<T>(dy + row * n.ld_y + c);
+    sb += g;
+    sw += g * (load1<T>(x + row * n.ld_x + c) - (n.rms ? 0.0f : *as_global(mean + row))) * *as_global(rstd + row);
+  }
+  if (partial_w) *as_global(partial_w + blockIdx.y * n.dim + c) = sw;
+  if (partial_b) *as_global(partial_b + blockIdx.y * n.dim + c) = sb;
 }

@@ -95,6 +95,14 @@ struct Columns {
   __device__ __forceinline__ Columns(long long c, long long dim) : at(min(c, dim - W)), skip((int)(c - min(c, dim - W))), any(c < dim) {}
 };
 
+// Sum over each LANES neighbouring lanes, in all of them, between registers.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+  if constexpr (LANES >= 64) x = add_xor<32>(x);
+  if constexpr (LANES >= 32) x = add_xor<16>(x);
+  if constexpr (LANES >= 16) x = add_xor<8>(x);
+  return add_xor<1>(add_xor<2>(add_xor<4>(x)));
+}
 // Sum over the 64 lanes of a wavefront, in every lane.
 template <typename F>
 __device__ __forceinline__ F wave_sum(F x) {

@@ -128,6 +128,32 @@ fira_status check_norm(const fira_layer_norm_desc* d) {
   return FIRA_OK;
 }
 
+// Calls f with the constants that a row of `dim` <= kNormWidest values is held by: values of a vector, threads, vectors of a thread.
+template <typename F>
+void with_row_shape(int64_t dim, F f) {
+  const Int<kVec> w{};
+  if (dim < kVec) f(Int<1>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 64) f(w, Int<8>{}, Int<1>{});
+  else if (dim <= 128) f(w, Int<16>{}, Int<1>{});
+  else if (dim <= 256) f(w, Int<32>{}, Int<1>{});
+  else if (dim <= 512) f(w, Int<64>{}, Int<1>{});
+  else if (dim <= 1024) f(w, Int<128>{}, Int<1>{});
+  else if (dim <= 2048) f(w, Int<256>{}, Int<1>{});
+  else if (dim <= 4096) f(w, Int<512>{}, Int<1>{});
+  else if (dim <= 8192) f(w, Int<1024>{}, Int<1>{});
+  else f(w, Int<1024>{}, Int<2>{});
+}
+// Workgroups of the norm's gradient, each of which leaves its sums over rows: at most as many as the chip holds, and rows for all.
+int64_t norm_parts(const fira_layer_norm_desc* d) {
+  if (d->dim > kNormWidest) return std::min<int64_t>(d->rows, 64);
+  int64_t parts = 1;
+  with_row_shape(d->dim, [&](auto, auto threads, auto) {
+    constexpr int THREADS = decltype(threads)::value, GROUPS = std::max(1, 256 / THREADS);
+    parts = std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 256 * 1024 / std::max(256, THREADS));
+  });
+  return parts;
+}
+
 fira_status check_gradients(const fira_gradient_desc* d, int count, bool outs) {
   if (count < 0) return refuse(FIRA_ERR_INVALID_ARG, "%d gradients", count);
   if (count && !d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptors");
@@ -316,18 +342,31 @@ fira_status fira_layer_norm(const fira_layer_norm_desc* d, const void* dev_x, in
   FIRA_POINTER(dev_y, size_of(d->dtype));
   if (!aligned(dev_weight, size_of(d->param_dtype)) || !aligned(dev_bias, size_of(d->param_dtype)) || !aligned(dev_mean, 4) || !aligned(dev_rstd, 4))
     return refuse(FIRA_ERR_INVALID_ARG, "weight, bias, mean or rstd is not aligned to its elements");
-  const FiraNorm n{d->rows, d->dim, ld_x, ld_y, 0, (float)d->eps, d->kind == FIRA_RMS_NORM, 0};
+  const FiraNorm n{d->rows, d->dim, ld_x, ld_y, 0, (float)d->eps, d->kind == FIRA_RMS_NORM};
   with_types(d->dtype, d->param_dtype, [&](auto t, auto p) {
     typedef decltype(t) T;
     typedef decltype(p) P;
-    hipLaunchKernelGGL((fira_layer_norm_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(256), 0, (hipStream_t)hip_stream, n,
-                       (const typename T::raw*)dev_x, (const typename P::raw*)dev_weight, (const typename P::raw*)dev_bias, (typename T::raw*)dev_y,
-                       n.rms ? nullptr : dev_mean, dev_rstd);
+    const typename T::raw* const x = (const typename T::raw*)dev_x;
+    const typename P::raw *const w = (const typename P::raw*)dev_weight, *const b = (const typename P::raw*)dev_bias;
+    typename T::raw* const y = (typename T::raw*)dev_y;
+    float* const mean = n.rms ? nullptr : dev_mean;
+    const hipStream_t q = (hipStream_t)hip_stream;
+    if (d->dim > kNormWidest) {
+      hipLaunchKernelGGL((fira_layer_norm_wide_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, x, w, b, y, mean, dev_rstd);
+      return;
+    }
+    with_row_shape(d->dim, [&](auto width, auto threads, auto nv) {
+      constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
+      hipLaunchKernelGGL((fira_layer_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)),
+                         dim3(std::max(256, THREADS)), 0, q, n, x, w, b, y, mean, dev_rstd);
+    });
   });
   return launched("layer norm");
 }
 
-size_t fira_layer_norm_gradient_workspace_bytes(const fira_layer_norm_desc* d) { return check_norm(d) ? 0 : 256; }
+size_t fira_layer_norm_gradient_workspace_bytes(const fira_layer_norm_desc* d) {
+  return check_norm(d) ? 0 : up256(std::max<int64_t>(1, 2 * norm_parts(d) * d->dim * 4));
+}
 
 fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* dev_dy, int64_t ld_dy, const void* dev_x, int64_t ld_x,
                                      const void* dev_weight, const float* dev_mean, const float* dev_rstd, void* dev_dx, int64_t ld_dx,
@@ -347,16 +386,30 @@ fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* 
   if (!aligned(dev_weight, size_of(d->param_dtype)) || !aligned(dev_dweight, size_of(d->param_dtype)) || !aligned(dev_dbias, size_of(d->param_dtype)))
     return refuse(FIRA_ERR_INVALID_ARG, "weight, dweight or dbias is not aligned to its elements");
   if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, fira_layer_norm_gradient_workspace_bytes(d))) return st;
-  const FiraNorm n{d->rows, d->dim, ld_x, ld_dy, ld_dx, (float)d->eps, d->kind == FIRA_RMS_NORM, accumulate};
+  const FiraNorm n{d->rows, d->dim, ld_x, ld_dy, ld_dx, (float)d->eps, d->kind == FIRA_RMS_NORM};
   with_types(d->dtype, d->param_dtype, [&](auto t, auto p) {
     typedef decltype(t) T;
     typedef decltype(p) P;
-    if (dev_dx && d->rows)
-      hipLaunchKernelGGL((fira_layer_norm_dx_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(256), 0, (hipStream_t)hip_stream, n,
-                         (const typename T::raw*)dev_dy, (const typename T::raw*)dev_x, (const typename P::raw*)dev_weight, dev_mean, dev_rstd, (typename T::raw*)dev_dx);
-    if ((dev_dweight || dev_dbias) && (d->rows || !accumulate))
-      hipLaunchKernelGGL((fira_layer_norm_dw_kernel<T, P>), dim3((d->dim + 63) / 64), dim3(256), 0, (hipStream_t)hip_stream, n,
-                         (const typename T::raw*)dev_dy, (const typename T::raw*)dev_x, dev_mean, dev_rstd, (typename P::raw*)dev_dweight, (typename P::raw*)dev_dbias);
+    const typename T::raw *const dy = (const typename T::raw*)dev_dy, *const x = (const typename T::raw*)dev_x;
+    const typename P::raw* const w = (const typename P::raw*)dev_weight;
+    typename T::raw* const dx = (typename T::raw*)dev_dx;
+    const hipStream_t q = (hipStream_t)hip_stream;
+    const int parts = (int)norm_parts(d);
+    float* const pw = dev_dweight ? (float*)dev_workspace : nullptr;
+    float* const pb = dev_dbias ? (float*)dev_workspace + (int64_t)parts * d->dim : nullptr;
+    if (d->rows && d->dim > kNormWidest) {
+      if (dx) hipLaunchKernelGGL((fira_layer_norm_wide_dx_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx);
+      if (pw || pb) hipLaunchKernelGGL(fira_layer_norm_wide_dw_kernel<T>, dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dy, x, dev_mean, dev_rstd, pw, pb);
+    } else if (d->rows && (dx || pw || pb)) {
+      with_row_shape(d->dim, [&](auto width, auto threads, auto nv) {
+        constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+        hipLaunchKernelGGL((fira_layer_norm_gradient_kernel<T, P, W, THREADS, NV>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx,
+                           pw, pb);
+      });
+    }
+    if ((pw || pb) && (d->rows || !accumulate))
+      hipLaunchKernelGGL(fira_layer_norm_join_kernel<P>, dim3((d->dim + 31) / 32, 2), dim3(256), 0, q, pw, pb, parts, d->dim, (typename P::raw*)dev_dweight,
+                         (typename P::raw*)dev_dbias, accumulate);
   });
   return launched("layer norm gradient");
 }
