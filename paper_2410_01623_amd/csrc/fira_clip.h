@@ -1,4 +1,6 @@
 // The norm of a list of gradients taken together, and their scaling where it passes a limit.  gfx950 only.
+//
+// Two passes: the factor is known when all has been read, and what has to be cut is read again.  Both are bound by memory.
 #pragma once
 #include "fira_rows.h"
 
@@ -8,43 +10,85 @@ struct FiraSpan {
   void* out;
   int rows, cols;
   int ld, ld_out;
-  int vecs;          // vectors of eight values per row, the last one of a row maybe shorter
+  int vecs;          // vectors of a row: of as many values as the kernel takes, the last one of a row maybe shorter, or of one where a row has fewer
   int tile0;         // first tile of this piece
 };
 constexpr int kSpans = 96;            // a launch's pieces travel as kernel arguments, of which there are 4 KB
-constexpr int kClipTile = 2048;       // vectors of a tile
-constexpr int kClipWorkgroups = 2048;
+constexpr int kClipUnroll = 4;        // vectors of a thread that are on their way together
+constexpr int kClipTile = 256 * kClipUnroll;
+constexpr int kClipWorkgroups = 1024;
 struct FiraSpans {
   FiraSpan s[kSpans];
   int count, tiles;
+  int each;          // tiles of a workgroup
 };
+static_assert(sizeof(FiraSpans) + 64 <= 4096, "kernel arguments");
 
-// Calls f(piece, row, column, values there) for this workgroup's vectors: tiles blockIdx.x, blockIdx.x + gridDim.x, ...
+// Calls f(piece, first vector) for this workgroup's tiles, which adjoin.
 template <typename F>
-__device__ __forceinline__ void for_each_vector(const FiraSpans& l, F f) {
-  for (int tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
-    int k = 0;
+__device__ __forceinline__ void for_each_tile(const FiraSpans& l, F f) {
+  const int from = blockIdx.x * l.each, until = min(from + l.each, l.tiles);
+  int k = 0;                                             // the last piece that does not begin after the first tile
+#pragma unroll 1
+  for (int step = 64; step; step >>= 1)
+    if (k + step < l.count && l.s[k + step].tile0 <= from) k += step;
+#pragma unroll 1
+  for (int tile = from; tile < until; ++tile) {
     while (k + 1 < l.count && l.s[k + 1].tile0 <= tile) ++k;
-    const FiraSpan& s = l.s[k];
-    const unsigned total = (unsigned)s.rows * (unsigned)s.vecs;
-    const unsigned first = (unsigned)(tile - s.tile0) * kClipTile;
-    for (unsigned i = first + threadIdx.x; i < first + kClipTile && i < total; i += blockDim.x) {
-      const unsigned row = i / (unsigned)s.vecs, c = (i - row * (unsigned)s.vecs) * kVec;
-      f(s, row, c, s.cols - (int)c);
-    }
+    k = __builtin_amdgcn_readfirstlane(k);
+    f(l.s[k], (unsigned)(tile - l.s[k].tile0) * kClipTile);
   }
 }
 
-// Sum of squares in fp64: neither a square nor a sum of them leaves its range, whatever the gradients are.
+// Calls f(row, place of the vector, values in front that are another vector's, whether there is such a vector) for this thread's vectors of a tile
+// one after the other, so that f can put loads on their way; the last vector of a row starts earlier, so that it is whole.
+template <int W, bool STRIDED, typename F>
+__device__ __forceinline__ void for_each_vector(const FiraSpan& s, unsigned first, F f) {
+  const unsigned total = (unsigned)s.rows * (unsigned)s.vecs;
+#pragma unroll
+  for (int u = 0; u < kClipUnroll; ++u) {
+    const unsigned i = first + u * 256 + threadIdx.x, at = min(i, total - 1);
+    const unsigned row = STRIDED ? at / (unsigned)s.vecs : 0u;
+    const int c = (int)(at - row * (unsigned)s.vecs) * W, begin = min(c, s.cols - W);
+    f(u, row, begin, c - begin, i < total);
+  }
+}
+// Calls f with the constants for a piece: values of a vector, whether it has more than one row.
+template <int W, typename F>
+__device__ __forceinline__ void with_piece_shape(const FiraSpan& s, F f) {
+  if (s.cols < W) f(std::integral_constant<int, 1>{}, std::true_type{});
+  else if (s.rows > 1) f(std::integral_constant<int, W>{}, std::true_type{});
+  else f(std::integral_constant<int, W>{}, std::false_type{});
+}
+
+// Sum of squares in fp64: neither a square nor a sum of them leaves its range, whatever the gradients are, and the vector unit has room for it
+// beside the loads.
 template <typename T>
 __global__ __launch_bounds__(256) void fira_gradient_squares_kernel(FiraSpans l, double* partial) {
   __shared__ double part[4];
   double sum = 0.0;
-  for_each_vector(l, [&](const FiraSpan& s, unsigned row, unsigned c, int left) {
-    float v[kVec];
-    load_some<T>((const typename T::raw*)s.g + (long long)row * s.ld + c, left, v);
+  for_each_tile(l, [&](const FiraSpan& s, unsigned first) {
+    with_piece_shape<kWidth<T>>(s, [&](auto w, auto strided) {
+      constexpr int W = decltype(w)::value;
+      Raw<T, W> x[kClipUnroll];
+      const typename T::raw* p[kClipUnroll];
+      int skip[kClipUnroll];
+      for_each_vector<W, decltype(strided)::value>(s, first, [&](int u, unsigned row, int c, int before, bool here) {
+        p[u] = (const typename T::raw*)s.g + (long long)row * s.ld + c;
+        x[u].stream(p[u]);
+        skip[u] = here ? before : -1;
+      });
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) sum += (double)v[i] * (double)v[i];
+      for (int u = 0; u < kClipUnroll; ++u) {
+        double q = 0.0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) q += (double)x[u].get(j) * (double)x[u].get(j);
+        sum += skip[u] == 0 ? q : 0.0;
+        if (skip[u] > 0)
+#pragma unroll 1
+          for (int j = skip[u]; j < W; ++j) { const double v = load1<T>(p[u] + j); sum += v * v; }
+      }
+    });
   });
   sum = block_sum(sum, part);
   if (threadIdx.x == 0) *as_global(partial + blockIdx.x) = sum;
@@ -53,28 +97,51 @@ __global__ __launch_bounds__(256) void fira_gradient_squares_kernel(FiraSpans l,
 // The norm from all launches' sums, in an order that every workgroup keeps.
 __device__ __forceinline__ double norm_of(const double* partial, int n, double* part) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) s += *as_global(partial + i);
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n; i += 256) s += *as_global(partial + i);
   return sqrt(block_sum(s, part));
 }
+template <typename = void>
 __global__ __launch_bounds__(256) void fira_gradient_norm_kernel(const double* partial, int n, float* norm) {
   __shared__ double part[4];
   const double x = norm_of(partial, n, part);
   if (threadIdx.x == 0) *as_global(norm) = (float)x;
 }
 
-// out = min(1, max_norm / norm) g.  A norm that is not finite leaves the gradients as they are.
+// out = min(1, max_norm / norm) g.  A norm that is not finite leaves the gradients as they are.  Every workgroup works the norm out for itself, and
+// one of them leaves it in *norm: no launch in between.
 template <typename T, typename R>
-__global__ __launch_bounds__(256) void fira_clip_kernel(FiraSpans l, const double* partial, int n, double max_norm) {
+__global__ __launch_bounds__(256) void fira_clip_kernel(FiraSpans l, const double* partial, int n, double max_norm, float* norm) {
   __shared__ double part[4];
-  const double norm = norm_of(partial, n, part);
-  const bool cut = norm > max_norm && norm < INFINITY;
-  const float factor = cut ? (float)(max_norm / norm) : 1.0f;
-  for_each_vector(l, [&](const FiraSpan& s, unsigned row, unsigned c, int left) {
-    if (!cut && s.g == s.out) return;     // in place: they are what they have to be
-    float v[kVec];
-    load_some<T>((const typename T::raw*)s.g + (long long)row * s.ld + c, left, v);
+  const double x = norm_of(partial, n, part);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *as_global(norm) = (float)x;
+  const bool cut = x > max_norm && x < INFINITY;
+  const float factor = cut ? (float)(max_norm / x) : 1.0f;
+  for_each_tile(l, [&](const FiraSpan& s, unsigned first) {
+    if (!cut && s.g == s.out) return;                    // in place: they are what they have to be
+    with_piece_shape<kWidth<T, R>>(s, [&](auto w, auto strided) {
+      constexpr int W = decltype(w)::value;
+      Raw<T, W> x[kClipUnroll];
+      const typename T::raw* p[kClipUnroll];
+      typename R::raw* to[kClipUnroll];
+      int skip[kClipUnroll];
+      for_each_vector<W, decltype(strided)::value>(s, first, [&](int u, unsigned row, int c, int before, bool here) {
+        p[u] = (const typename T::raw*)s.g + (long long)row * s.ld + c;
+        to[u] = (typename R::raw*)s.out + (long long)row * s.ld_out + c;
+        x[u].stream(p[u]);
+        skip[u] = here ? before : -1;
+      });
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] *= factor;
-    store_some<R>((typename R::raw*)s.out + (long long)row * s.ld_out + c, left, v);
+      for (int u = 0; u < kClipUnroll; ++u) {
+        float y[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) y[j] = factor * x[u].get(j);
+        if (skip[u] == 0) store_w<R, W, true>(to[u], y);
+        // (what another vector has as well may have been scaled by now, and is left to it)
+        if (skip[u] > 0)
+#pragma unroll 1
+          for (int j = skip[u]; j < W; ++j) store1<R>(to[u] + j, factor * load1<T>(p[u] + j));
+      }
+    });
   });
 }

@@ -21,7 +21,9 @@ __device__ __forceinline__ int token_row(const FiraEmbed& e, const void* ids, lo
 }
 
 // out[t] = scale * table[id_t], zeros for an id outside the table.  A wavefront takes TOKENS tokens at a time, 64 / LANES of them side by side, and
-// NV vectors of each per lane.
+// NV vectors of each per lane.  131072 tokens x 2048, a table of 32000 rows in fp32, bf16 out: 168 us with two tokens and 2048 columns a wavefront, 172 with
+// one, 175 and 182 with 512 columns and two or four tokens; 179 to 198 where every XCD goes through columns of its own, so that more of the rows
+// that a text uses all the time are in its L2.
 template <typename T, typename R, int W, int LANES, int NV, int TOKENS>
 __global__ __launch_bounds__(256) void fira_embed_lookup_kernel(FiraEmbed e, const typename T::raw* table, const void* ids, typename R::raw* out) {
   constexpr int SIDE = 64 / LANES, EACH = TOKENS / SIDE;
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(256) void fira_embed_lookup_kernel(FiraEmbed e, con
         float y[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) y[j] = row[k] >= 0 ? e.scale * x[k][v].get(j) : 0.0f;
-        if (c.any && t < e.count) store_w<R, W>(out + t * e.ld_rows + c.at, y);
+        if (c.any && t < e.count) store_w<R, W, true>(out + t * e.ld_rows + c.at, y);
       }
   }
 }
@@ -64,7 +66,7 @@ __global__ __launch_bounds__(256) void fira_embed_lookup_kernel(FiraEmbed e, con
 // A row is cut by its own tokens alone, so that its bits depend on nothing else.
 constexpr int kBuckets = 256, kMostChunks = 256;
 constexpr int kPieceTokens = 32;
-constexpr int kCounters = 15360;                        // LDS of a bucket's workgroup: a counter for each of its rows and wavefronts
+constexpr int kCounters = 15360;                        // LDS of a bucket's workgroup, in words: a counter for each of its rows and wavefronts, then entries
 constexpr int64_t kMostEmbedRows = 1 << 21;             // ... of which there are kBuckets times fewer than rows of the table
 
 struct FiraEmbedSort {       // the sort's part of the workspace
@@ -72,6 +74,7 @@ struct FiraEmbedSort {       // the sort's part of the workspace
   int bins;                  // rows of a bucket
   int bits;                  // ... and bits that number them
   u32x2* sorted;             // [chunks][chunk]       (id >> 8, token), by bucket
+  u32x2* gathered;           // [count]               the same, a bucket's side by side, where they do not fit LDS
   u32x2* part;               // [kBuckets][chunks]    first entry and number of entries of a bucket in a chunk
   unsigned* order;           // [count]               tokens by row
   u32x2* rows;               // [kBuckets][bins]      first entry in `order` and number of entries of a row
@@ -81,14 +84,26 @@ struct FiraEmbedSort {       // the sort's part of the workspace
   float* partial;            // [pieces][dim]
 };
 
-// Lanes that are `in` and have this lane's key of `bits` bits.
+// Lanes that are `in` and have this lane's key of `bits` bits.  Up to four keys are taken out one after the other, since where there are many lanes to
+// be done most of them have the same one (the bucket of a text's most frequent token); the rest is compared bit by bit.
 __device__ __forceinline__ unsigned long long lanes_alike(unsigned key, int bits, bool in) {
-  unsigned long long m = __ballot(in);
-  for (int b = 0; b < bits; ++b) {
-    const int mine = (int)(key << (31 - b)) >> 31;      // all ones where the bit is set
-    m &= ~(__ballot(mine) ^ (unsigned long long)(long long)mine);
+  unsigned long long rest = __ballot(in), mine = 0;
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    if (!rest) return mine;
+    const bool same = in && key == (unsigned)__builtin_amdgcn_readlane((int)key, __builtin_ctzll(rest));
+    const unsigned long long m = __ballot(same);
+    mine = same ? m : mine;
+    rest &= ~m;
   }
-  return m;
+  if (!rest) return mine;
+  unsigned long long m = rest;
+#pragma unroll 1
+  for (int b = 0; b < bits; ++b) {
+    const int bit = (int)(key << (31 - b)) >> 31;       // all ones where it is set
+    m &= ~(__ballot(bit) ^ (unsigned long long)(long long)bit);
+  }
+  return mine ? mine : m;
 }
 // Sum of x over the threads before this one; *total: over all.  part: LDS, 17 values.
 __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
@@ -158,75 +173,85 @@ __device__ __forceinline__ int piece_tokens(int n) {
   return len;
 }
 
-// A wavefront takes the bucket's entries of neighbouring chunks, in groups of 64 lanes: as many chunks side by side as leave each the lanes for
-// its entries (an ordinary bucket has two or three in a chunk, the one with a text's most frequent token a tenth of the chunk).  One pass over
-// them finds each entry's place among the wavefront's own with the same row, which stays in registers until the rows' first places are known.
-// (dynamic LDS: a counter per wavefront and row of the bucket)
+// The bucket's entries come out of all chunks at once, a few threads to a chunk, side by side into LDS (those of the bucket of a text's most frequent
+// token may be too many: into the workspace then), and are counted on the way; a wavefront then places a part of them.  What has to wait for memory
+// waits once for all of it: with a group of 64 entries after the other, each fetched from another XCD's work, the largest of the 256 buckets of 131072
+// tokens took 21 us.
+// (dynamic LDS: a counter per wavefront and row of the bucket, then the entries)
 __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, FiraEmbedSort s) {
-  constexpr int KEPT = 16;                              // groups whose entries stay in registers; where there are more, they are read again
   extern __shared__ int count[];
-  __shared__ int at_of[kMostChunks], n_of[kMostChunks];
   __shared__ int part[17];
   __shared__ unsigned long long given;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, bucket = blockIdx.x;
-  int before = 0;                                       // entries of the buckets before this one
-  for (int c = threadIdx.x; c < s.chunks; c += blockDim.x) {
-    const u32x2 p = *as_global(s.part + (long long)bucket * s.chunks + c);
-    at_of[c] = (int)p[0];
-    n_of[c] = (int)p[1];
-    before += (int)p[0];
-  }
-  int base;
-  block_scan(before, part, &base);
+  u32x2* const staged = (u32x2*)(count + (waves * s.bins + 1) / 2 * 2);
+  const int room = (kCounters - (waves * s.bins + 1) / 2 * 2) / 2;
+  // `each` threads to a chunk, the chunks in their order
+  int each = 1;
+  while (2 * each * s.chunks <= (int)blockDim.x) each *= 2;
+  const int steps = (s.chunks * each + blockDim.x - 1) / blockDim.x;      // 1 but for few wavefronts
   for (int i = threadIdx.x; i < waves * s.bins; i += blockDim.x) count[i] = 0;
-  __syncthreads();
-  const int per = (s.chunks + waves - 1) / waves, c_mine = wave * per, c_until = min(c_mine + per, s.chunks);
-  int most = 0;                                         // entries of any of them
-  for (int c = c_mine + lane; c < c_until; c += 64) most = max(most, n_of[c]);
+  int before = 0, n = 0;                                // entries of the buckets before this one, and of this one
+  u32x2 mine{0, 0};
+  for (int k = 0; k < steps; ++k) {
+    const int c = (k * blockDim.x + threadIdx.x) / each;
+    mine = u32x2{0, 0};
+    if (c < s.chunks) mine = *as_global(s.part + (long long)bucket * s.chunks + c);
+    const bool first = threadIdx.x % each == 0;
+    before += first ? (int)mine[0] : 0;
+    n += first ? (int)mine[1] : 0;
+  }
+  int base, total;
+  block_scan(before, part, &base);
+  int at = block_scan(n, part, &total);                 // (where steps is 1: entries of the chunks before this thread's)
+  const int span = max(64, ((total + waves - 1) / waves + 63) / 64 * 64);   // entries of a wavefront
+  const bool in_lds = total <= room;
+  int done = 0;
+  for (int k = 0; k < steps; ++k) {
+    const int c = (k * blockDim.x + threadIdx.x) / each, j0 = threadIdx.x % each;
+    if (steps > 1) {
+      mine = u32x2{0, 0};
+      if (c < s.chunks) mine = *as_global(s.part + (long long)bucket * s.chunks + c);
+      int here;
+      at = done + block_scan(j0 == 0 ? (int)mine[1] : 0, part, &here);
+      done += here;
+    }
+    if (j0) at -= (int)mine[1];                         // (the scan has counted the chunk itself for all but its first thread)
+    const u32x2* const src = s.sorted + (long long)c * s.chunk + mine[0];
+    for (int j = j0; j < (int)mine[1]; j += 4 * each) {
+      u32x2 entry[4];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
-  int share = 4;                                        // lanes to a chunk
-  while (share < 64 && share < most) share *= 2;
-  const int side = 64 / share, rounds = max((most + 63) / 64, 1), groups = c_mine < c_until ? (per + side - 1) / side * rounds : 0;
-  volatile int* const own = count + wave * s.bins;
-  // group g: round g % rounds of the chunks from c_mine + g / rounds * side on
-  auto load = [&](int g, u32x2& entry) {
-    const int c = c_mine + g / rounds * side + lane / share, j = g % rounds * 64 + lane % share;
-    entry = u32x2{~0u, 0};
-    if (g < groups && c < c_until && j < n_of[c]) entry = *as_global(s.sorted + (long long)c * s.chunk + at_of[c] + j);
-  };
-  auto place = [&](u32x2 entry) {                       // (of the lanes with one row only the first one writes)
-    const bool in = entry[0] != ~0u;
-    const unsigned key = in ? entry[0] : 0;
-    const unsigned long long alike = lanes_alike(key, s.bits, in);
-    const unsigned long long below = alike & ((1ull << lane) - 1);
-    const int at = own[key] + __popcll(below);
-    __builtin_amdgcn_wave_barrier();
-    if (in && !below) own[key] = at + __popcll(alike);
-    __builtin_amdgcn_wave_barrier();
-    return at;
-  };
-  u32x2 entry[KEPT];
-  int at[KEPT];
-  for (int g0 = 0; g0 < groups; g0 += KEPT) {
+      for (int u = 0; u < 4; ++u)
+        if (j + u * each < (int)mine[1]) entry[u] = *as_global(src + j + u * each);
 #pragma unroll
-    for (int k = 0; k < KEPT; ++k) load(g0 + k, entry[k]);
-#pragma unroll
-    for (int k = 0; k < KEPT; ++k)
-      if (g0 + k < groups) at[k] = place(entry[k]);
+      for (int u = 0; u < 4; ++u)
+        if (j + u * each < (int)mine[1]) {
+          const int to = at + j + u * each;
+          if (in_lds) staged[to] = entry[u];
+          else *as_global(s.gathered + base + to) = entry[u];
+          atomicAdd(count + to / span * s.bins + entry[u][0], 1);
+        }
+    }
   }
   __syncthreads();
+  // the rows' first places, and each wavefront's among them
   int start = 0;
   for (int b0 = 0; b0 < s.bins; b0 += blockDim.x) {
     const int b = b0 + threadIdx.x;
     int sum = 0;
     if (b < s.bins)
+#pragma unroll 8
       for (int w = 0; w < waves; ++w) sum += count[w * s.bins + b];
     int here;
     int first = start + block_scan(sum, part, &here);
     start += here;
-    // rows in pieces: one addition per workgroup hands out the places for all of them, as those of all workgroups wait for one another
-    // (two for every such row took half of the kernel's time); which places does not matter to any result
+    if (b < s.bins) {
+      *as_global(s.rows + (long long)bucket * s.bins + b) = u32x2{(unsigned)(base + first), (unsigned)sum};
+      int next = first;
+#pragma unroll 8
+      for (int w = 0; w < waves; ++w) { const int c = count[w * s.bins + b]; count[w * s.bins + b] = next; next += c; }
+    }
+    // rows in pieces: one addition per workgroup hands out the places for all of them, as those of all workgroups wait for one another;
+    // which places does not matter to any result
     const int len = piece_tokens(sum), pieces = sum > kPieceTokens ? (sum + len - 1) / len : 0;
     if (__syncthreads_or(pieces)) {
       int all_pieces, all_rows;
@@ -243,26 +268,23 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
           *as_global(to + k) = u32x4{(unsigned)__builtin_amdgcn_readlane((int)row, l), (unsigned)(from + k * size), (unsigned)min(size, all - k * size), 0};
       }
     }
-    if (b >= s.bins) continue;                          // (no barrier before the next round's)
-    *as_global(s.rows + (long long)bucket * s.bins + b) = u32x2{(unsigned)(base + first), (unsigned)sum};
-    for (int w = 0; w < waves; ++w) { const int c = count[w * s.bins + b]; count[w * s.bins + b] = first; first += c; }
   }
   __syncthreads();
-  if (groups <= KEPT) {                                 // the first place of each row and wavefront, and the place among them
-#pragma unroll
-    for (int k = 0; k < KEPT; ++k)
-      if (k < groups && entry[k][0] != ~0u) *as_global(s.order + base + own[entry[k][0]] + at[k]) = entry[k][1];
-  } else {
-    for (int g0 = 0; g0 < groups; g0 += KEPT) {
-#pragma unroll
-      for (int k = 0; k < KEPT; ++k) load(g0 + k, entry[k]);
-#pragma unroll
-      for (int k = 0; k < KEPT; ++k)
-        if (g0 + k < groups) {
-          const int to = place(entry[k]);
-          if (entry[k][0] != ~0u) *as_global(s.order + base + to) = entry[k][1];
-        }
-    }
+  volatile int* const own = count + wave * s.bins;
+  const int until = min((wave + 1) * span, total);
+#pragma unroll 1
+  for (int i = wave * span + lane; i - lane < until; i += 64) {
+    const bool in = i < until;
+    u32x2 entry{0, 0};
+    if (in_lds) { if (in) entry = staged[i]; }
+    else if (in) entry = *as_global(s.gathered + base + i);
+    const unsigned long long alike = lanes_alike(entry[0], s.bits, in);
+    const unsigned long long below = alike & ((1ull << lane) - 1);
+    const int to = own[entry[0]] + __popcll(below);
+    __builtin_amdgcn_wave_barrier();
+    if (in && !below) own[entry[0]] = to + __popcll(alike);   // (of the lanes with one row only the first one writes)
+    __builtin_amdgcn_wave_barrier();
+    if (in) *as_global(s.order + base + to) = entry[1];
   }
 }
 
@@ -288,7 +310,7 @@ __device__ __forceinline__ void write_gradient(const FiraEmbed& e, typename T::r
       return;
     }
   }
-  store_w<T, W>(to, y);
+  store_w<T, W, !ADD>(to, y);
 }
 
 // Loads of N rows are put on their way together, without a branch between them; beyond the last row it is loaded again.  (One copy of the loop's
@@ -337,14 +359,15 @@ __global__ __launch_bounds__(256) void fira_embed_sum_narrow_kernel(FiraEmbed e,
 constexpr int kBatch = 8;
 template <typename T, typename R, bool ADD>
 __global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const typename R::raw* dout, typename T::raw* dtable, FiraEmbedSort s) {
-  constexpr int W = kVec, N = 8;
+  constexpr int W = kWidth<T, R>, NV = 8 / W, N = 8;
   const int lane = threadIdx.x & 63;
-  const unsigned tiles = (unsigned)((e.dim + 64 * W - 1) / (64 * W)), batches = (s.bins + kBatch - 1) / kBatch;
+  const unsigned tiles = (unsigned)((e.dim + 511) / 512), batches = (s.bins + kBatch - 1) / kBatch;
   const long long pieces = (long long)*as_global(s.counters) * tiles, all = pieces + (long long)batches * kBuckets * tiles;
   for (long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += gridDim.x * 4LL) {
     const bool piece = i < pieces;
     const long long unit = (piece ? i : i - pieces) / tiles;
-    const Columns<W> c(((piece ? i : i - pieces) - unit * tiles) * (64 * W) + lane * W, e.dim);
+    const long long c0 = ((piece ? i : i - pieces) - unit * tiles) * 512 + lane * W;
+    auto columns = [&](int v) { return Columns<W>(c0 + v * (64 * W), e.dim); };
     // lane k < kBatch: first token and number of tokens of row k
     unsigned row0 = 0;
     u32x2 r{0, 0};
@@ -361,11 +384,17 @@ __global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const 
 #pragma unroll
     for (int d = 1; d < kBatch; d <<= 1) { const int y = __shfl_up(upto, d, 64); upto += lane >= d ? y : 0; }
     const int total = __builtin_amdgcn_readlane(upto, kBatch - 1);
-    float sum[W] = {};
+    float sum[NV][W] = {};
+    auto finish = [&](unsigned to) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const Columns<W> c = columns(v);
+        if (c.any) write_gradient<T, W, ADD>(e, dtable, to, c, sum[v]);
+      }
+    };
     if (!ADD && !piece) {
       const bool none = r[1] == 0 && lane < kBatch && row0 + lane * kBuckets < (unsigned)e.vocab;
-      for (unsigned long long m = __ballot(none); m; m &= m - 1)
-        if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + __builtin_ctzll(m) * kBuckets, c, sum);
+      for (unsigned long long m = __ballot(none); m; m &= m - 1) finish(row0 + __builtin_ctzll(m) * kBuckets);
     }
     int row = -1;                                        // the one that is being summed
     for (int j0 = 0; j0 < total; j0 += 64) {
@@ -377,29 +406,38 @@ __global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const 
       const int before = __shfl(upto, of, 64) - __shfl(n, of, 64);
       const unsigned token = *as_global(s.order + (__shfl(r[0], of, 64) + at - before));
       for (int first = 0; first < 64 && j0 + first < total; first += N) {
-        Raw<R, W> x[N];
+        Raw<R, W> x[N][NV];
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k].load(dout + (unsigned)__builtin_amdgcn_readlane(token, first + k) * e.ld_rows + c.at);
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+          for (int v = 0; v < NV; ++v) x[k][v].load(dout + (unsigned)__builtin_amdgcn_readlane(token, first + k) * e.ld_rows + columns(v).at);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
           if (j0 + first + k >= total) break;
           const int next = __builtin_amdgcn_readlane(of, first + k);
           if (next != row) {
             if (row >= 0) {
-              if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + row * kBuckets, c, sum);
+              finish(row0 + row * kBuckets);
 #pragma unroll
-              for (int j = 0; j < W; ++j) sum[j] = 0.0f;
+              for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[v][j] = 0.0f;
             }
             row = next;
           }
 #pragma unroll
-          for (int j = 0; j < W; ++j) sum[j] += x[k].get(j);
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < W; ++j) sum[v][j] += x[k][v].get(j);
         }
       }
     }
-    if (row >= 0 && c.any) {
-      if (piece) store_w<FiraStoredF32, W>(s.partial + unit * e.dim + c.at, sum);
-      else write_gradient<T, W, ADD>(e, dtable, row0 + row * kBuckets, c, sum);
+    if (piece) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (columns(v).any) store_w<FiraStoredF32, W>(s.partial + unit * e.dim + columns(v).at, sum[v]);
+    } else if (row >= 0) {
+      finish(row0 + row * kBuckets);
     }
   }
 }

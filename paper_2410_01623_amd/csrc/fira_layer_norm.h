@@ -10,10 +10,10 @@ struct FiraNorm {
   int rms;                   // 1: no mean
 };
 
-// A row is held in registers by THREADS threads, NV vectors of W values to a thread (all but the last one of them inside the row), a part of a
-// wavefront, a wavefront or a workgroup as its width asks for, so that it is read once and its sums are taken of what is there.
+// A row is held in registers by THREADS threads, NV vectors of W values to a thread (the first half of them, rounded down, inside the row), a part of
+// a wavefront, a wavefront or a workgroup as its width asks for, so that it is read once and its sums are taken of what is there.
 // kNormWidest: widest row that is held; wider ones are read again for every sum.
-constexpr int kNormWidest = 1024 * 2 * kVec;
+constexpr int kNormWidest = 16384;
 
 // Sums of two values over a row's threads, in all of them.  part: LDS, two sets in turn, so that one barrier a row is enough.
 template <int THREADS>
@@ -48,21 +48,22 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
     Raw<T, W> xs[NV];
     Raw<P, W> ws[NV], bs[NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) xs[v].load(xr + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+    for (int v = 0; v < NV; ++v) xs[v].stream(xr + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
     if (w)
 #pragma unroll
       for (int v = 0; v < NV; ++v) ws[v].load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
     if (b)
 #pragma unroll
       for (int v = 0; v < NV; ++v) bs[v].load(b + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
-    const Columns<W> last((long long)((NV - 1) * THREADS + me) * W, n.dim);
-    const int skip = last.any ? last.skip : W;           // values of the last vector that are not this thread's
+    int skip[NV];                                        // values of a vector that are not this thread's
+#pragma unroll
+    for (int v = NV / 2; v < NV; ++v) { const Columns<W> c((long long)(v * THREADS + me) * W, n.dim); skip[v] = c.any ? c.skip : W; }
     float mu = 0.0f, none = 0.0f;
     if (!n.rms) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int j = 0; j < W; ++j) mu += v < NV - 1 || j >= skip ? xs[v].get(j) : 0.0f;
+        for (int j = 0; j < W; ++j) mu += v < NV / 2 || j >= skip[v] ? xs[v].get(j) : 0.0f;
       row_sums<THREADS>(mu, none, part, turn++);
       mu /= (float)n.dim;
     }
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         const float d = xs[v].get(j) - mu;
-        s += v < NV - 1 || j >= skip ? d * d : 0.0f;
+        s += v < NV / 2 || j >= skip[v] ? d * d : 0.0f;
       }
     row_sums<THREADS>(s, none, part, turn++);
     const float r = 1.0f / sqrtf(s / (float)n.dim + n.eps);
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
         if (w) o[j] *= ws[v].get(j);
         if (b) o[j] += bs[v].get(j);
       }
-      if (here && c.any) store_w<T, W>(y + row * n.ld_y + c.at, o);
+      if (here && c.any) store_w<T, W, true>(y + row * n.ld_y + c.at, o);
     }
     if (here && me == 0) {
       if (mean) *as_global(mean + row) = mu;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
                                                                                                  const typename P::raw* w, const float* mean, const float* rstd,
                                                                                                  typename T::raw* dx, float* partial_w, float* partial_b) {
   constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
-  constexpr int BUFS = THREADS * NV > 1024 ? 1 : 2;      // (there are no registers for two rows then)
+  constexpr int BUFS = THREADS * NV * W > 8192 ? 1 : 2;      // (there are no registers for two rows then)
   __shared__ float part[2][16][2];
   __shared__ float joined[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? THREADS * W : 1];
   const int me = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
@@ -112,8 +113,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
   if (w)
 #pragma unroll
     for (int v = 0; v < NV; ++v) ws[v].load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
-  const Columns<W> last((long long)((NV - 1) * THREADS + me) * W, n.dim);
-  const int skip = last.any ? last.skip : W;
+  int skip[NV];                                          // values of a vector that are not this thread's
+#pragma unroll
+  for (int v = NV / 2; v < NV; ++v) { const Columns<W> c((long long)(v * THREADS + me) * W, n.dim); skip[v] = c.any ? c.skip : W; }
   float sw[NV][W] = {}, sb[NV][W] = {};
   Raw<T, W> xs[BUFS][NV], gs[BUFS][NV];
   float mus[BUFS], rs[BUFS];
@@ -125,8 +127,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const long long c = Columns<W>((long long)(v * THREADS + me) * W, n.dim).at;
-      xs[to][v].load(x + row * n.ld_x + c);
-      gs[to][v].load(dy + row * n.ld_y + c);
+      xs[to][v].stream(x + row * n.ld_x + c);
+      gs[to][v].stream(dy + row * n.ld_y + c);
     }
   };
   int turn = 0;
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         const float d = here ? gs[of][v].get(j) : 0.0f, h = (xs[of][v].get(j) - mu) * r, g = w ? d * ws[v].get(j) : d;
-        const bool mine = v < NV - 1 || j >= skip;
+        const bool mine = v < NV / 2 || j >= skip[v];
         s1 += mine ? g : 0.0f;
         s2 += mine ? g * h : 0.0f;
         sw[v][j] += here ? d * h : 0.0f;
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
           const float h = (xs[of][v].get(j) - mu) * r, g = w ? gs[of][v].get(j) * ws[v].get(j) : gs[of][v].get(j);
           o[j] = r * (g - s1 - h * s2);
         }
-        if (c.any) store_w<T, W>(dx + row * n.ld_dx + c.at, o);
+        if (c.any) store_w<T, W, true>(dx + row * n.ld_dx + c.at, o);
       }
   };
   // (two rows a turn, so that which registers hold which is known to the compiler)

@@ -7,10 +7,17 @@
 struct FiraStoredF32 { typedef float raw; };
 struct FiraStoredBf16 { typedef bf16_raw raw; };
 
-constexpr int kVec = 8;   // values a lane takes at a time: 16 bytes of bf16, 32 of fp32
+// W neighbouring values of a row, as many as make 16 bytes of the wider type that a kernel streams (8 where all is bf16, 4 with fp32; 1 for rows
+// that are shorter): every load and store of a wavefront then covers whole lines, which fp32 in pieces of 32 bytes a lane does not (with those,
+// streaming stores cost the embedding gradient of 131072 x 1024 in fp32 167 us instead of 144, and streaming loads the norm's gradient 94 instead of 80).
+template <typename T, typename R = T>
+constexpr int kWidth = sizeof(typename T::raw) == 4 || sizeof(typename R::raw) == 4 ? 4 : 8;
+constexpr int kMostWidth = 8;
 
 // Rows start at any element (odd widths, any leading dimension), so these are vectors with element alignment; the hardware
 // takes such addresses.
+typedef u32x2 __attribute__((aligned(2))) u32x2_a2;
+
 template <typename T>
 __device__ __forceinline__ float load1(const typename T::raw* p) {
   if constexpr (sizeof(typename T::raw) == 4) return *as_global(p);
@@ -21,68 +28,67 @@ __device__ __forceinline__ void store1(typename T::raw* p, float x) {
   if constexpr (sizeof(typename T::raw) == 4) *as_global(p) = x;
   else *as_global(p) = f32_to_bf16(x);
 }
-template <typename T>
-__device__ __forceinline__ void load8(const typename T::raw* p, float (&v)[kVec]) {
-  if constexpr (sizeof(typename T::raw) == 4) {
-    const f32x4 a = *(gptr<const f32x4_a4>)as_global(p), b = *(gptr<const f32x4_a4>)as_global(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-  } else {
-    const u32x4 a = *(gptr<const u32x4_a2>)as_global(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(a[i] << 16); v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store8(typename T::raw* p, const float (&v)[kVec]) {
-  if constexpr (sizeof(typename T::raw) == 4) {
-    *(gptr<f32x4_a4>)as_global(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *(gptr<f32x4_a4>)as_global(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-  } else {
-    *(gptr<u32x4_a2>)as_global(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-  }
-}
-// The same for the n values of a row that are left, 0 <= n; what lies beyond is neither read nor written and counts as zero.
-template <typename T>
-__device__ __forceinline__ void load_some(const typename T::raw* p, long long n, float (&v)[kVec]) {
-  if (n >= kVec) return load8<T>(p, v);
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) v[i] = i < n ? load1<T>(p + i) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store_some(typename T::raw* p, long long n, const float (&v)[kVec]) {
-  if (n >= kVec) return store8<T>(p, v);
-#pragma unroll
-  for (int i = 0; i < kVec; ++i)
-    if (i < n) store1<T>(p + i, v[i]);
-}
 
-// W neighbouring values (8, or 1 for rows shorter than 8) as they are stored: what is on its way is held like this, in half the
-// registers where it is bf16.  One load each, without a branch, so that many stay on their way.
+// How W values of type T move: as one vector, or as two of fp32 where W is 8.
 template <typename T, int W>
-struct Raw;
-template <>
-struct Raw<FiraStoredF32, 8> {
-  f32x4 a, b;
-  __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
-  __device__ __forceinline__ void load(const float* p) { a = *(gptr<const f32x4_a4>)as_global(p); b = *(gptr<const f32x4_a4>)as_global(p + 4); }
-};
-template <>
-struct Raw<FiraStoredBf16, 8> {
-  u32x4 a;
-  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? a[i / 2] & 0xffff0000u : a[i / 2] << 16); }
-  __device__ __forceinline__ void load(const bf16_raw* p) { a = *(gptr<const u32x4_a2>)as_global(p); }
+struct Moved;
+template <> struct Moved<FiraStoredBf16, 8> { typedef u32x4 reg; typedef u32x4_a2 mem; };
+template <> struct Moved<FiraStoredBf16, 4> { typedef u32x2 reg; typedef u32x2_a2 mem; };
+template <> struct Moved<FiraStoredF32, 8> { typedef f32x4 reg; typedef f32x4_a4 mem; };
+template <> struct Moved<FiraStoredF32, 4> { typedef f32x4 reg; typedef f32x4_a4 mem; };
+
+// Values as they are stored: what is on its way is held like this, in half the registers where it is bf16.  load: one load (two for eight of fp32)
+// without a branch, so that many stay on their way.  stream: the same for what is not needed again.
+template <typename T, int W>
+struct Raw {
+  typedef typename Moved<T, W>::reg reg;
+  typedef typename Moved<T, W>::mem mem;
+  static constexpr bool F32 = sizeof(typename T::raw) == 4;
+  static constexpr int N = F32 ? W / 4 : 1;
+  reg a[N];
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (F32) return a[i / 4][i % 4];
+    else return __uint_as_float(i & 1 ? a[0][i / 2] & 0xffff0000u : a[0][i / 2] << 16);
+  }
+  __device__ __forceinline__ void load(const typename T::raw* p) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) a[k] = *(gptr<const mem>)as_global(p + 4 * k);
+  }
+  __device__ __forceinline__ void stream(const typename T::raw* p) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) a[k] = __builtin_nontemporal_load((gptr<const mem>)as_global(p + 4 * k));
+  }
 };
 template <typename T>
 struct Raw<T, 1> {
   float a;
   __device__ __forceinline__ float get(int) const { return a; }
   __device__ __forceinline__ void load(const typename T::raw* p) { a = load1<T>(p); }
+  __device__ __forceinline__ void stream(const typename T::raw* p) { load(p); }
 };
-template <typename T, int W>
+// STREAM: the result does not have to stay in the caches.
+template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ void store_w(typename T::raw* p, const float (&v)[W]) {
-  if constexpr (W == 8) store8<T>(p, v);
-  else store1<T>(p, v[0]);
+  if constexpr (W == 1) {
+    store1<T>(p, v[0]);
+  } else {
+    typedef typename Moved<T, W>::reg reg;
+    typedef typename Moved<T, W>::mem mem;
+    constexpr bool F32 = sizeof(typename T::raw) == 4;
+    constexpr int N = F32 ? W / 4 : 1;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      reg a;
+      if constexpr (F32) {
+        a = reg{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) a[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+      }
+      if constexpr (STREAM) __builtin_nontemporal_store((mem)a, (gptr<mem>)as_global(p + 4 * k));
+      else *(gptr<mem>)as_global(p + 4 * k) = a;
+    }
+  }
 }
 
 // A lane's W columns of rows that are `dim` >= W wide, by rights those from `c` on.  At the end of a row they start earlier, so that they are

@@ -108,6 +108,7 @@ EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
   while (1 << s.bits < s.bins) ++s.bits;
   r.pieces = 2 * (count / kPieceTokens);
   take(s.sorted, (int64_t)s.chunks * s.chunk);
+  take(s.gathered, count);
   take(s.part, (int64_t)kBuckets * s.chunks);
   take(s.order, count);
   take(s.rows, (int64_t)kBuckets * s.bins);
@@ -128,29 +129,33 @@ fira_status check_norm(const fira_layer_norm_desc* d) {
   return FIRA_OK;
 }
 
-// Calls f with the constants that a row of `dim` <= kNormWidest values is held by: values of a vector, threads, vectors of a thread.
-template <typename F>
+// Calls f with the constants that a row of `dim` <= kNormWidest values of type T is held by: values of a vector, threads, vectors of a thread.
+// EACH: values of a thread where a row takes more than a wavefront, 8 or 16.
+template <typename T, int EACH, typename F>
 void with_row_shape(int64_t dim, F f) {
-  const Int<kVec> w{};
-  if (dim < kVec) f(Int<1>{}, Int<8>{}, Int<1>{});
-  else if (dim <= 64) f(w, Int<8>{}, Int<1>{});
-  else if (dim <= 128) f(w, Int<16>{}, Int<1>{});
-  else if (dim <= 256) f(w, Int<32>{}, Int<1>{});
-  else if (dim <= 512) f(w, Int<64>{}, Int<1>{});
-  else if (dim <= 1024) f(w, Int<128>{}, Int<1>{});
-  else if (dim <= 2048) f(w, Int<256>{}, Int<1>{});
-  else if (dim <= 4096) f(w, Int<512>{}, Int<1>{});
-  else if (dim <= 8192) f(w, Int<1024>{}, Int<1>{});
-  else f(w, Int<1024>{}, Int<2>{});
+  constexpr int W = kWidth<T>, N = 8 / W, D = EACH / 8;
+  if (dim < kMostWidth) f(Int<1>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 8 * W) f(Int<W>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 16 * W) f(Int<W>{}, Int<16>{}, Int<1>{});
+  else if (dim <= 32 * W) f(Int<W>{}, Int<32>{}, Int<1>{});
+  else if (dim <= 64 * W) f(Int<W>{}, Int<64>{}, Int<1>{});
+  else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
+  else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
+  else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
+  else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
+  else if (dim <= 8192) f(Int<W>{}, Int<1024 / D>{}, Int<D * N>{});
+  else f(Int<W>{}, Int<1024>{}, Int<2 * N>{});
 }
 // Workgroups of the norm's gradient, each of which leaves its sums over rows: at most as many as the chip holds, and rows for all.
 int64_t norm_parts(const fira_layer_norm_desc* d) {
   if (d->dim > kNormWidest) return std::min<int64_t>(d->rows, 64);
   int64_t parts = 1;
-  with_row_shape(d->dim, [&](auto, auto threads, auto) {
+  auto shape = [&](auto, auto threads, auto) {
     constexpr int THREADS = decltype(threads)::value, GROUPS = std::max(1, 256 / THREADS);
     parts = std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 256 * 1024 / std::max(256, THREADS));
-  });
+  };
+  if (d->dtype == FIRA_F32) with_row_shape<FiraStoredF32, 8>(d->dim, shape);
+  else with_row_shape<FiraStoredBf16, 8>(d->dim, shape);
   return parts;
 }
 
@@ -166,21 +171,21 @@ fira_status check_gradients(const fira_gradient_desc* d, int count, bool outs) {
   return FIRA_OK;
 }
 
-// Cuts gradient i into pieces that the kernels take: at most kPiece values a row and kPiece vectors in all.
+// Cuts a gradient into pieces that the kernels take, in vectors of `width` values: at most kPiece values a row and kPiece vectors in all.
 constexpr int64_t kPiece = 1 << 30;
 template <typename F>
-void cut_up(const fira_gradient_desc& d, const void* g, void* out, bool outs, F piece) {
+void cut_up(const fira_gradient_desc& d, const void* g, void* out, bool outs, int width, F piece) {
   int64_t rows = d.rows, cols = d.cols, ld = d.ld, ld_out = outs ? d.ld_out : d.ld;
   if (!rows || !cols) return;
   const size_t size = size_of(d.dtype), size_out = size_of(outs ? d.out_dtype : d.dtype);
   if (ld == cols && ld_out == cols) { cols *= rows; rows = 1; }                       // dense: one long row
   const bool by_row = ld > kPiece || ld_out > kPiece || cols > kPiece;
-  const int64_t vecs = (cols + kVec - 1) / kVec, some = by_row ? 1 : std::min(rows, kPiece / std::min(vecs, kPiece));
+  const int64_t vecs = cols < width ? cols : (cols + width - 1) / width, some = by_row ? 1 : std::min(rows, kPiece / std::min(vecs, kPiece));
   for (int64_t r = 0; r < rows; r += some)
     for (int64_t c = 0; c < cols; c += kPiece) {
       const int64_t n = std::min(kPiece, cols - c);
       piece(FiraSpan{(const char*)g + (r * ld + c) * size, (char*)out + (r * ld_out + c) * size_out, (int)std::min(some, rows - r), (int)n,
-                     by_row ? 0 : (int)ld, by_row ? 0 : (int)ld_out, (int)((n + kVec - 1) / kVec), 0});
+                     by_row ? 0 : (int)ld, by_row ? 0 : (int)ld_out, (int)(n < width ? n : (n + width - 1) / width), 0});
     }
 }
 
@@ -192,21 +197,26 @@ struct Batch {
     l.s[l.count++] = s;
     l.tiles += (int)(((int64_t)s.rows * s.vecs + kClipTile - 1) / kClipTile);
   }
-  // (2^30 vectors are 2^19 tiles a piece, so a launch's tiles fit 32 bits)
+  // (2^30 vectors are 2^20 tiles a piece, so a launch's tiles fit 32 bits)
   bool full() const { return l.count == kSpans; }
 };
-int workgroups(const FiraSpans& l) { return std::min(l.tiles, kClipWorkgroups); }
+int workgroups(const FiraSpans& l) { return (l.tiles + l.each - 1) / l.each; }
 
-// Calls f(types, pieces, in place) for every launch that the list takes, types by types.
+// Calls f(types, pieces) for every launch that the list takes, types by types; by_out: the results' types as well.
 template <typename F>
 void for_each_launch(const fira_gradient_desc* d, int count, const void* const* G, void* const* out, bool by_out, F f) {
   for (int in = 0; in < 2; ++in)
     for (int to = 0; to < (by_out ? 2 : 1); ++to) {
       Batch b;
-      auto flush = [&] { if (b.l.count) f(in, to, b.l); b.l.count = b.l.tiles = 0; };
+      const int width = in == FIRA_F32 || (by_out && to == FIRA_F32) ? kWidth<FiraStoredF32> : kWidth<FiraStoredBf16>;
+      auto flush = [&] {
+        b.l.each = (b.l.tiles + kClipWorkgroups - 1) / kClipWorkgroups;
+        if (b.l.count) f(in, to, b.l);
+        b.l.count = b.l.tiles = 0;
+      };
       for (int i = 0; i < count; ++i) {
         if (d[i].dtype != in || (by_out && (out ? d[i].out_dtype : d[i].dtype) != to)) continue;
-        cut_up(d[i], G ? G[i] : nullptr, out ? out[i] : G ? const_cast<void*>(G[i]) : nullptr, by_out && out, [&](const FiraSpan& s) { b.add(s); if (b.full()) flush(); });
+        cut_up(d[i], G ? G[i] : nullptr, out ? out[i] : G ? const_cast<void*>(G[i]) : nullptr, by_out && out, width, [&](const FiraSpan& s) { b.add(s); if (b.full()) flush(); });
       }
       flush();
     }
@@ -263,11 +273,14 @@ fira_status fira_embed_lookup(const fira_embed_desc* d, const void* dev_table, c
       hipLaunchKernelGGL((fira_embed_lookup_kernel<T, R, W, LANES, NV, TOKENS>), dim3(std::min<int64_t>((units + 3) / 4, 1 << 20)), dim3(256), 0,
                          (hipStream_t)hip_stream, e, (const typename T::raw*)dev_table, dev_ids, (typename R::raw*)dev_out);
     };
-    if (d->dim < kVec) launch(Int<1>{}, Int<8>{}, Int<1>{}, Int<8>{});
-    else if (d->dim <= 64) launch(Int<kVec>{}, Int<8>{}, Int<1>{}, Int<16>{});
-    else if (d->dim <= 128) launch(Int<kVec>{}, Int<16>{}, Int<1>{}, Int<8>{});
-    else if (d->dim <= 256) launch(Int<kVec>{}, Int<32>{}, Int<1>{}, Int<4>{});
-    else launch(Int<kVec>{}, Int<64>{}, Int<1>{}, Int<4>{});
+    constexpr int W = kWidth<T, R>;
+    if (d->dim < kMostWidth) launch(Int<1>{}, Int<8>{}, Int<1>{}, Int<8>{});
+    else if (d->dim <= 8 * W) launch(Int<W>{}, Int<8>{}, Int<1>{}, Int<16>{});
+    else if (d->dim <= 16 * W) launch(Int<W>{}, Int<16>{}, Int<1>{}, Int<8>{});
+    else if (d->dim <= 32 * W) launch(Int<W>{}, Int<32>{}, Int<1>{}, Int<4>{});
+    else if ((d->dim + 511) / 512 % 4 == 0) launch(Int<W>{}, Int<64>{}, Int<32 / W>{}, Int<2>{});
+    else if ((d->dim + 511) / 512 % 2 == 0) launch(Int<W>{}, Int<64>{}, Int<16 / W>{}, Int<2>{});
+    else launch(Int<W>{}, Int<64>{}, Int<8 / W>{}, Int<2>{});
   });
   return launched("embedding lookup");
 }
@@ -306,27 +319,32 @@ fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, 
           hipLaunchKernelGGL((fira_embed_few_kernel<T, R, W, ADD>), grid((d->rows + kBatch - 1) / kBatch * ((dim + 64 * W - 1) / (64 * W)), 4), dim3(256), 0, q, e,
                              dout, dev_ids, dtable);
         };
-        if (dim < kVec) few(Int<1>{});
-        else few(Int<kVec>{});
+        if (dim < kMostWidth) few(Int<1>{});
+        else few(Int<kWidth<T, R>>{});
         return;
       }
       hipLaunchKernelGGL(fira_embed_chunk_kernel, dim3(s.chunks), dim3(256), 0, q, e, dev_ids, s);
       const int waves = std::min(16, kCounters / s.bins);
-      hipLaunchKernelGGL(fira_embed_bucket_kernel, dim3(kBuckets), dim3(64 * waves), 4 * waves * s.bins, q, e, s);
+      hipLaunchKernelGGL(fira_embed_bucket_kernel, dim3(kBuckets), dim3(64 * waves), 4 * kCounters, q, e, s);
       auto narrow = [&](auto w, auto lanes) {
         constexpr int W = decltype(w)::value, LANES = decltype(lanes)::value;
         hipLaunchKernelGGL((fira_embed_sum_narrow_kernel<T, R, W, LANES, ADD>), grid(sort.pieces + d->rows, 256 / LANES), dim3(256), 0, q, e, dout, dtable, s);
       };
       const int64_t batches = (int64_t)((s.bins + kBatch - 1) / kBatch) * kBuckets;
-      if (dim < kVec) narrow(Int<1>{}, Int<8>{});
-      else if (dim <= 64) narrow(Int<kVec>{}, Int<8>{});
-      else if (dim <= 128) narrow(Int<kVec>{}, Int<16>{});
-      else if (dim <= 256) narrow(Int<kVec>{}, Int<32>{});
-      else hipLaunchKernelGGL((fira_embed_sum_kernel<T, R, ADD>), grid((sort.pieces + batches) * ((dim + 64 * kVec - 1) / (64 * kVec)), 4), dim3(256), 0, q, e, dout, dtable, s);
+      constexpr int W = kWidth<T, R>;
+      if (dim < kMostWidth) narrow(Int<1>{}, Int<8>{});
+      else if (dim <= 8 * W) narrow(Int<W>{}, Int<8>{});
+      else if (dim <= 16 * W) narrow(Int<W>{}, Int<16>{});
+      else if (dim <= 32 * W) narrow(Int<W>{}, Int<32>{});
+      else hipLaunchKernelGGL((fira_embed_sum_kernel<T, R, ADD>), grid((sort.pieces + batches) * ((dim + 511) / 512), 4), dim3(256), 0, q, e, dout, dtable, s);
       // (a row in pieces has kPieceTokens + 1 tokens at least)
-      const dim3 joins(std::min<int64_t>(count / (kPieceTokens + 1) * ((dim + 32 * kVec - 1) / (32 * kVec)), 4096));
-      if (dim < kVec) hipLaunchKernelGGL((fira_embed_join_kernel<T, 1, ADD>), joins, dim3(256), 0, q, e, dtable, s);
-      else hipLaunchKernelGGL((fira_embed_join_kernel<T, kVec, ADD>), joins, dim3(256), 0, q, e, dtable, s);
+      auto join = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        hipLaunchKernelGGL((fira_embed_join_kernel<T, W, ADD>), dim3(std::min<int64_t>(count / (kPieceTokens + 1) * ((dim + 32 * W - 1) / (32 * W)), 4096)), dim3(256),
+                           0, q, e, dtable, s);
+      };
+      if (dim < kMostWidth) join(Int<1>{});
+      else join(Int<kWidth<FiraStoredF32>>{});
     });
   });
   return launched("embedding gradient");
@@ -355,7 +373,7 @@ fira_status fira_layer_norm(const fira_layer_norm_desc* d, const void* dev_x, in
       hipLaunchKernelGGL((fira_layer_norm_wide_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, x, w, b, y, mean, dev_rstd);
       return;
     }
-    with_row_shape(d->dim, [&](auto width, auto threads, auto nv) {
+    with_row_shape<T, 16>(d->dim, [&](auto width, auto threads, auto nv) {
       constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
       hipLaunchKernelGGL((fira_layer_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)),
                          dim3(std::max(256, THREADS)), 0, q, n, x, w, b, y, mean, dev_rstd);
@@ -401,7 +419,7 @@ fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* 
       if (dx) hipLaunchKernelGGL((fira_layer_norm_wide_dx_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx);
       if (pw || pb) hipLaunchKernelGGL(fira_layer_norm_wide_dw_kernel<T>, dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dy, x, dev_mean, dev_rstd, pw, pb);
     } else if (d->rows && (dx || pw || pb)) {
-      with_row_shape(d->dim, [&](auto width, auto threads, auto nv) {
+      with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
         constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
         hipLaunchKernelGGL((fira_layer_norm_gradient_kernel<T, P, W, THREADS, NV>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx,
                            pw, pb);
@@ -426,7 +444,7 @@ fira_status fira_gradient_norm(const fira_gradient_desc* d, int count, const voi
   const int64_t n = partials(d, count);
   if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, up256(8 * (n + 1)))) return st;
   launch_squares(d, count, dev_G, (double*)dev_workspace, (hipStream_t)hip_stream);
-  hipLaunchKernelGGL(fira_gradient_norm_kernel, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, (const double*)dev_workspace, (int)n, dev_norm);
+  hipLaunchKernelGGL(fira_gradient_norm_kernel<>, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, (const double*)dev_workspace, (int)n, dev_norm);
   return launched("gradient norm");
 }
 
@@ -440,10 +458,12 @@ fira_status fira_clip_gradients(const fira_gradient_desc* d, int count, void* co
   if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, up256(8 * (n + 1)))) return st;
   const hipStream_t q = (hipStream_t)hip_stream;
   launch_squares(d, count, dev_G, (double*)dev_workspace, q);
-  hipLaunchKernelGGL(fira_gradient_norm_kernel, dim3(1), dim3(256), 0, q, (const double*)dev_workspace, (int)n, dev_norm);
+  if (!n) hipLaunchKernelGGL(fira_gradient_norm_kernel<>, dim3(1), dim3(256), 0, q, (const double*)dev_workspace, 0, dev_norm);   // nothing in the list
+  float* norm = dev_norm;                                // the first launch writes it
   for_each_launch(d, count, dev_G, dev_out, true, [&](int in, int to, const FiraSpans& l) {
     with_types(in, to, [&](auto t, auto r) {
-      hipLaunchKernelGGL((fira_clip_kernel<decltype(t), decltype(r)>), dim3(workgroups(l)), dim3(256), 0, q, l, (const double*)dev_workspace, (int)n, max_norm);
+      hipLaunchKernelGGL((fira_clip_kernel<decltype(t), decltype(r)>), dim3(workgroups(l)), dim3(256), 0, q, l, (const double*)dev_workspace, (int)n, max_norm, norm);
+      norm = nullptr;
     });
   });
   return launched("gradient clipping");

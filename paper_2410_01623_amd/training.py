@@ -44,33 +44,26 @@ def _device(*tensors) -> torch.device:
 
 
 @contextlib.contextmanager
-def _on_device_and_stream(dev, stream):
+def _device_and_stream(dev, stream):
     with torch.cuda.device(dev), (torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()):
         yield
 
 
-class _Call:
-    """The device and the stream of one call: entered only where they are not the current ones, for they cost as much as a launch."""
+def _elsewhere(dev: torch.device, stream: Optional[torch.cuda.Stream]):
+    """None if the call belongs on the current device and its current stream (entering them costs as much as a launch), else what to call again in."""
+    if stream is None and dev.index == torch.cuda.current_device():
+        return None
+    if stream is not None and stream.device != dev:
+        _refuse(FIRA_ERR_INVALID_ARG, f"tensors on {dev}, stream on {stream.device}")
+    return _device_and_stream(dev, stream)
 
-    __slots__ = ("handle", "guard")
 
-    def __init__(self, dev: torch.device, stream: Optional[torch.cuda.Stream]):
-        if stream is not None and stream.device != dev:
-            _refuse(FIRA_ERR_INVALID_ARG, f"tensors on {dev}, stream on {stream.device}")
-        current = torch.cuda.current_stream(dev)
-        self.guard = None
-        if dev.index != torch.cuda.current_device() or (stream is not None and stream != current):
-            self.guard = _on_device_and_stream(dev, stream)
-        self.handle = (stream or current).cuda_stream
+def _stream(dev: torch.device) -> int:
+    """Handle of the current stream, without a torch.cuda.Stream made for it where torch can do so."""
+    return _raw_stream(dev.index)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _ld(t: torch.Tensor) -> Optional[int]:
@@ -104,8 +97,11 @@ def _input(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     return t, ld
 
 
-def _result(given: Optional[torch.Tensor], shape, dtype, dev, name: str) -> Tuple[torch.Tensor, int]:
+def _result(given: Optional[torch.Tensor], shape, dtype, dev, name: str, like: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, int]:
+    """A result and its leading dimension; like: a tensor of its shape, type and device, if there is one."""
     if given is None:
+        if like is not None and like.is_contiguous():
+            return torch.empty_like(like), shape[-1]
         return torch.empty(shape, dtype=dtype, device=dev), shape[-1]
     if tuple(given.shape) != tuple(shape):
         _refuse(FIRA_ERR_SHAPE, f"{name} is {tuple(given.shape)}, not {tuple(shape)}")
@@ -154,12 +150,16 @@ def fira_embed_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 
     dev = _device(table, ids, out)
     dtype = dtype or (out.dtype if out is not None else table.dtype)
     dt, rdt = _dtype(table, "table"), _dtype(dtype, "result")
-    with _Call(dev, stream) as call:
-        ids = _ids(ids)
-        table, ld = _input(table)
-        out, ld_out = _result(out, (*ids.shape, table.shape[1]), dtype, dev, "out")
-        d = fira.fira_embed_desc(table.shape[0], table.shape[1], ld, dt, rdt, _IDS[ids.dtype], scale)
-        _check(lib.fira_embed_lookup(d, table.data_ptr(), ids.data_ptr(), ids.numel(), out.data_ptr(), ld_out, call.handle))
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_embed_lookup(table, ids, scale=scale, dtype=dtype, out=out)
+    ids = _ids(ids)
+    table, ld = _input(table)
+    rows, dim = table.shape
+    out, ld_out = _result(out, (*ids.shape, dim), dtype, dev, "out")
+    d = fira.fira_embed_desc(rows, dim, ld, dt, rdt, _IDS[ids.dtype], scale)
+    _check(lib.fira_embed_lookup(d, table.data_ptr(), ids.data_ptr(), ids.numel(), out.data_ptr(), ld_out, _stream(dev)))
     return out
 
 
@@ -176,15 +176,18 @@ def fira_embed_gradient(dout: torch.Tensor, ids: torch.Tensor, rows: int, *, sca
         _refuse(FIRA_ERR_SHAPE, f"dout is {tuple(dout.shape)} for ids of {tuple(ids.shape)}")
     if accumulate and out is None:
         _refuse(FIRA_ERR_INVALID_ARG, "accumulate without out")
-    with _Call(dev, stream) as call:
-        ids = _ids(ids)
-        dout, ld_dout = _input(dout)
-        out, ld = _result(out, (rows, dout.shape[-1]), dtype, dev, "out")
-        d = fira.fira_embed_desc(rows, dout.shape[-1], ld, dt, rdt, _IDS[ids.dtype], scale)
-        count = ids.numel()
-        workspace = _workspace(workspace, lib.fira_embed_gradient_workspace_bytes(d, count), dev)
-        _check(lib.fira_embed_gradient(d, dout.data_ptr(), ld_dout, ids.data_ptr(), count, out.data_ptr(), bool(accumulate),
-                                       workspace.data_ptr(), workspace.numel(), call.handle))
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_embed_gradient(dout, ids, rows, scale=scale, dtype=dtype, out=out, accumulate=accumulate, workspace=workspace)
+    ids = _ids(ids)
+    dout, ld_dout = _input(dout)
+    dim, count = dout.shape[-1], ids.numel()
+    out, ld = _result(out, (rows, dim), dtype, dev, "out")
+    d = fira.fira_embed_desc(rows, dim, ld, dt, rdt, _IDS[ids.dtype], scale)
+    workspace = _workspace(workspace, lib.fira_embed_gradient_workspace_bytes(d, count), dev)
+    _check(lib.fira_embed_gradient(d, dout.data_ptr(), ld_dout, ids.data_ptr(), count, out.data_ptr(), bool(accumulate),
+                                   workspace.data_ptr(), workspace.numel(), _stream(dev)))
     return out
 
 
@@ -199,23 +202,30 @@ def fira_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     dev = _device(x, weight, bias, out)
     dt = _dtype(x, "x")
     pdt = _param_dtype(dt, weight, bias)
-    with _Call(dev, stream) as call:
-        x, ld_x = _input(x)
-        dim, shape = x.shape[-1], x.shape[:-1]
-        out, ld_y = _result(out, x.shape, x.dtype, dev, "out")
-        mean = None if rms else torch.empty(shape, dtype=torch.float32, device=dev)
-        rstd = torch.empty(shape, dtype=torch.float32, device=dev)
-        d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, eps)
-        _check(lib.fira_layer_norm(d, x.data_ptr(), ld_x, _vector(weight, dim, "weight"), _vector(bias, dim, "bias"), out.data_ptr(), ld_y,
-                                   None if rms else mean.data_ptr(), rstd.data_ptr(), call.handle))
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_layer_norm(x, weight, bias, eps=eps, rms=rms, out=out)
+    x, ld_x = _input(x)
+    dim = x.shape[-1]
+    out, ld_y = _result(out, x.shape, x.dtype, dev, "out", like=x)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    mean = None if rms else torch.empty_like(rstd)
+    d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, eps)
+    _check(lib.fira_layer_norm(d, x.data_ptr(), ld_x, _vector(weight, dim, "weight"), _vector(bias, dim, "bias"), out.data_ptr(), ld_y,
+                               None if rms else mean.data_ptr(), rstd.data_ptr(), _stream(dev)))
     return out, mean, rstd
 
 
 def _param_dtype(default: int, *params) -> int:
-    dts = {_dtype(p, "parameter") for p in params if p is not None}
-    if len(dts) > 1:
-        _refuse(FIRA_ERR_DTYPE, "parameters of two types")
-    return dts.pop() if dts else default
+    given = None
+    for p in params:
+        if p is not None:
+            dt = _dtype(p, "parameter")
+            if given is not None and dt != given:
+                _refuse(FIRA_ERR_DTYPE, "parameters of two types")
+            given = dt
+    return default if given is None else given
 
 
 def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: Optional[torch.Tensor], rstd: torch.Tensor, *,
@@ -235,26 +245,30 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
     pdt = _dtype(ptype, "parameter")
     if not rms and mean is None:
         _refuse(FIRA_ERR_INVALID_ARG, "a layer norm's gradient needs its mean")
-    for t, name in ((rstd, "rstd"),) if rms else ((mean, "mean"), (rstd, "rstd")):
-        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+    for t, name in ((rstd, "rstd"), (None if rms else mean, "mean")):
+        if t is not None and (t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous()):
             _refuse(FIRA_ERR_SHAPE, f"{name} is not a dense fp32 tensor of {tuple(x.shape[:-1])}")
     if accumulate and (dweight is None or (bias and dbias is None)):
         _refuse(FIRA_ERR_INVALID_ARG, "accumulate without dweight and dbias")
-    with _Call(dev, stream) as call:
-        x, ld_x = _input(x)
-        dy, ld_dy = _input(dy)
-        dim = x.shape[-1]
-        dx, ld_dx = _result(dx, x.shape, x.dtype, dev, "dx")
-        dweight, _ = _result(dweight, (dim,), ptype, dev, "dweight")
-        if bias:
-            dbias, _ = _result(dbias, (dim,), ptype, dev, "dbias")
-        else:
-            dbias = None
-        d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, 0.0)
-        workspace = _workspace(workspace, lib.fira_layer_norm_gradient_workspace_bytes(d), dev)
-        _check(lib.fira_layer_norm_gradient(d, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, _vector(weight, dim, "weight"),
-                                            None if rms else mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), ld_dx, _vector(dweight, dim, "dweight"),
-                                            _vector(dbias, dim, "dbias"), bool(accumulate), workspace.data_ptr(), workspace.numel(), call.handle))
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_layer_norm_gradient(dy, x, weight, mean, rstd, rms=rms, bias=bias, param_dtype=ptype, dx=dx, dweight=dweight, dbias=dbias,
+                                            accumulate=accumulate, workspace=workspace)
+    x, ld_x = _input(x)
+    dy, ld_dy = _input(dy)
+    dim = x.shape[-1]
+    dx, ld_dx = _result(dx, x.shape, x.dtype, dev, "dx", like=x)
+    dweight, _ = _result(dweight, (dim,), ptype, dev, "dweight", like=weight)
+    if bias:
+        dbias, _ = _result(dbias, (dim,), ptype, dev, "dbias", like=dweight)
+    else:
+        dbias = None
+    d = fira.fira_layer_norm_desc(rstd.numel(), dim, dt, pdt, fira.FIRA_RMS_NORM if rms else fira.FIRA_LAYER_NORM, 0.0)
+    workspace = _workspace(workspace, lib.fira_layer_norm_gradient_workspace_bytes(d), dev)
+    _check(lib.fira_layer_norm_gradient(d, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, _vector(weight, dim, "weight"),
+                                        None if rms else mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), ld_dx, _vector(dweight, dim, "dweight"),
+                                        _vector(dbias, dim, "dbias"), bool(accumulate), workspace.data_ptr(), workspace.numel(), _stream(dev)))
     return dx, dweight, dbias
 
 
@@ -268,7 +282,7 @@ class GradientList:
         grads = list(grads)
         if not grads and device is None:
             _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
-        self.device = _device(*grads, *(outs or ())) if grads else torch.device(device)
+        self.device = _device(*grads, *(outs or ())) if grads else torch.empty(0, device=device).device
         if outs is not None and len(outs) != len(grads):
             _refuse(FIRA_ERR_INVALID_ARG, f"{len(outs)} results for {len(grads)} gradients")
         n = self.count = len(grads)
@@ -298,16 +312,22 @@ class GradientList:
 
     def fira_gradient_norm(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The norm of all gradients together, an fp32 scalar on the GPU."""
-        with _Call(self.device, stream) as call:
-            norm = torch.empty((), dtype=torch.float32, device=self.device)
-            _check(self.lib.fira_gradient_norm(self.descs, self.count, self.G, norm.data_ptr(), self.workspace.data_ptr(), self.bytes, call.handle))
+        elsewhere = _elsewhere(self.device, stream)
+        if elsewhere is not None:
+            with elsewhere:
+                return self.fira_gradient_norm()
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        _check(self.lib.fira_gradient_norm(self.descs, self.count, self.G, norm.data_ptr(), self.workspace.data_ptr(), self.bytes, _stream(self.device)))
         return norm
 
     def fira_clip_gradients(self, max_norm: float, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Scales all gradients by min(1, max_norm / norm) -> the norm before, an fp32 scalar on the GPU.  A norm that is not finite leaves
         them as they are."""
-        with _Call(self.device, stream) as call:
-            norm = torch.empty((), dtype=torch.float32, device=self.device)
-            _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), self.workspace.data_ptr(),
-                                                self.bytes, call.handle))
+        elsewhere = _elsewhere(self.device, stream)
+        if elsewhere is not None:
+            with elsewhere:
+                return self.fira_clip_gradients(max_norm)
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), self.workspace.data_ptr(),
+                                            self.bytes, _stream(self.device)))
         return norm
