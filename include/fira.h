@@ -316,7 +316,7 @@ FIRA_API const char* fira_kernel_name(int k);
  *   - fira_last_error(NULL) has the message of the last failure on this thread.  A call refused for its arguments enqueues nothing.
  *   - dev_workspace: device scratch of at least what the matching *_workspace_bytes call says (0 for invalid arguments), 256-byte
  *     aligned, its contents arbitrary, owned by the caller and free to reuse once the stream has passed the call.
- * Limits: tokens, rows and widths below 2^31, embedding tables of up to 2^21 rows. */
+ * Limits: tokens and rows below 2^31, embedding tables of up to 2^21 rows, embeddings and norms up to 2^24 wide; gradients of any size. */
 
 typedef enum { FIRA_I32 = 0, FIRA_I64 = 1 } fira_index_type;
 

@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr int64_t kMost = 0x7fffffff;
+constexpr int64_t kMost = 0x7fffffff, kMostDim = 1 << 24;
 
 __attribute__((format(printf, 2, 3))) fira_status refuse(fira_status st, const char* format, ...) {
   char msg[256];
@@ -77,7 +77,7 @@ void with_flag(bool flag, F f) {
 
 fira_status check_embed(const fira_embed_desc* d, int64_t count) {
   if (!d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
-  if (d->rows < 1 || d->rows > kMostEmbedRows || d->dim < 1 || d->dim > kMost) return refuse(FIRA_ERR_SHAPE, "embedding table of %lld x %lld", (long long)d->rows, (long long)d->dim);
+  if (d->rows < 1 || d->rows > kMostEmbedRows || d->dim < 1 || d->dim > kMostDim) return refuse(FIRA_ERR_SHAPE, "embedding table of %lld x %lld", (long long)d->rows, (long long)d->dim);
   FIRA_LEADING(d->ld, d->dim, d->rows);
   if (count < 0 || count > kMost) return refuse(FIRA_ERR_SHAPE, "%lld tokens", (long long)count);
   if (!known(d->dtype) || !known(d->row_dtype)) return refuse(FIRA_ERR_DTYPE, "embedding types %d and %d", d->dtype, d->row_dtype);
@@ -122,7 +122,7 @@ EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
 
 fira_status check_norm(const fira_layer_norm_desc* d) {
   if (!d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
-  if (d->rows < 0 || d->rows > kMost || d->dim < 1 || d->dim > kMost) return refuse(FIRA_ERR_SHAPE, "norm of %lld rows of %lld", (long long)d->rows, (long long)d->dim);
+  if (d->rows < 0 || d->rows > kMost || d->dim < 1 || d->dim > kMostDim) return refuse(FIRA_ERR_SHAPE, "norm of %lld rows of %lld", (long long)d->rows, (long long)d->dim);
   if (!known(d->dtype) || !known(d->param_dtype)) return refuse(FIRA_ERR_DTYPE, "norm types %d and %d", d->dtype, d->param_dtype);
   if (d->kind != FIRA_LAYER_NORM && d->kind != FIRA_RMS_NORM) return refuse(FIRA_ERR_INVALID_ARG, "norm kind %d", d->kind);
   if (!(d->eps >= 0.0) || !std::isfinite((float)d->eps)) return refuse(FIRA_ERR_INVALID_ARG, "eps is negative or not finite");
