@@ -315,8 +315,11 @@ FIRA_API const char* fira_kernel_name(int k);
  *   - Results must not overlap inputs unless a call says so.
  *   - fira_last_error(NULL) has the message of the last failure on this thread.  A call refused for its arguments enqueues nothing.
  *   - dev_workspace: device scratch of at least what the matching *_workspace_bytes call says (0 for invalid arguments), 256-byte
- *     aligned, its contents arbitrary, owned by the caller and free to reuse once the stream has passed the call.
+ *     aligned, its contents arbitrary, owned by the caller and free to reuse once the stream has passed the call.  Where
+ *     FIRA_UNUSED_WORKSPACE_BYTES are asked for, as for few rows or tokens, the call does not touch them.
  * Limits: tokens and rows below 2^31, embedding tables of up to 2^21 rows, embeddings and norms up to 2^24 wide; gradients of any size. */
+
+#define FIRA_UNUSED_WORKSPACE_BYTES 256u
 
 typedef enum { FIRA_I32 = 0, FIRA_I64 = 1 } fira_index_type;
 

@@ -96,6 +96,55 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
   }
 }
 
+// What the gradient's kernels do with a row, in the same roundings wherever it is done: this thread's part of the sums of g and g h, and of dw and db.
+template <typename T, typename P, int W, int NV>
+struct NormRow {
+  Raw<T, W> x[NV], dy[NV];
+  float mu, r;
+  __device__ __forceinline__ void load(const FiraNorm& n, const typename T::raw* xs, const typename T::raw* dys, const float* mean, const float* rstd, long long row,
+                                       int me, int threads) {
+    mu = n.rms ? 0.0f : *as_global(mean + row);
+    r = *as_global(rstd + row);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const long long c = Columns<W>((long long)(v * threads + me) * W, n.dim).at;
+      x[v].stream(xs + row * n.ld_x + c);
+      dy[v].stream(dys + row * n.ld_y + c);
+    }
+  }
+  __device__ __forceinline__ void sums(const Raw<P, W> (&w)[NV], bool weighted, const int (&skip)[NV], bool here, float& s1, float& s2, float (&sw)[NV][W],
+                                       float (&sb)[NV][W]) const {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float d = here ? dy[v].get(j) : 0.0f, h = (x[v].get(j) - mu) * r, g = weighted ? d * w[v].get(j) : d;
+        const bool mine = v < NV / 2 || j >= skip[v];
+        s1 += mine ? g : 0.0f;
+        s2 = mine ? __builtin_fmaf(g, h, s2) : s2;
+        sw[v][j] = here ? __builtin_fmaf(d, h, sw[v][j]) : sw[v][j];
+        sb[v][j] += d;
+      }
+  }
+  // s1, s2: the means of g and g h
+  __device__ __forceinline__ void write(const FiraNorm& n, const Raw<P, W> (&w)[NV], bool weighted, float s1, float s2, typename T::raw* dx, long long row, int me,
+                                        int threads) const {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const Columns<W> c((long long)(v * threads + me) * W, n.dim);
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float h = (x[v].get(j) - mu) * r, g = weighted ? dy[v].get(j) * w[v].get(j) : dy[v].get(j);
+        o[j] = r * (g - __builtin_fmaf(h, s2, s1));
+      }
+      if (c.any) store_w<T, W, true>(dx + row * n.ld_dx + c.at, o);
+    }
+  }
+};
+
 // g = w dy, h = (x - mu) rstd:  dx = rstd (g - mean g - h mean(g h)), without mean g where there is no mean;  dw = sum over rows of dy h,
 // db = sum over rows of dy.  One pass: a workgroup takes every gridDim.x-th row (or set of rows side by side), the next one's values on their way
 // while it works on one, and adds up dy h and dy of its columns in registers; fira_layer_norm_join_kernel adds up the workgroups' sums.
@@ -117,52 +166,17 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
 #pragma unroll
   for (int v = NV / 2; v < NV; ++v) { const Columns<W> c((long long)(v * THREADS + me) * W, n.dim); skip[v] = c.any ? c.skip : W; }
   float sw[NV][W] = {}, sb[NV][W] = {};
-  Raw<T, W> xs[BUFS][NV], gs[BUFS][NV];
-  float mus[BUFS], rs[BUFS];
+  NormRow<T, P, W, NV> rows[BUFS];
   const long long step = (long long)gridDim.x * GROUPS;
-  auto load = [&](int to, long long row) {
-    row = min(row, n.rows - 1);
-    mus[to] = n.rms ? 0.0f : *as_global(mean + row);
-    rs[to] = *as_global(rstd + row);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const long long c = Columns<W>((long long)(v * THREADS + me) * W, n.dim).at;
-      xs[to][v].stream(x + row * n.ld_x + c);
-      gs[to][v].stream(dy + row * n.ld_y + c);
-    }
-  };
+  auto load = [&](int to, long long row) { rows[to].load(n, x, dy, mean, rstd, min(row, n.rows - 1), me, THREADS); };
   int turn = 0;
   auto work = [&](int of, long long row0) {
     const long long row = row0 + group;
     const bool here = row < n.rows;
-    const float mu = mus[of], r = here ? rs[of] : 0.0f;
     float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const float d = here ? gs[of][v].get(j) : 0.0f, h = (xs[of][v].get(j) - mu) * r, g = w ? d * ws[v].get(j) : d;
-        const bool mine = v < NV / 2 || j >= skip[v];
-        s1 += mine ? g : 0.0f;
-        s2 += mine ? g * h : 0.0f;
-        sw[v][j] += here ? d * h : 0.0f;
-        sb[v][j] += d;
-      }
+    rows[of].sums(ws, w != nullptr, skip, here, s1, s2, sw, sb);
     row_sums<THREADS>(s1, s2, part, turn++);
-    s1 = n.rms ? 0.0f : s1 / (float)n.dim;
-    s2 = s2 / (float)n.dim;
-    if (dx && here)
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
-        float o[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const float h = (xs[of][v].get(j) - mu) * r, g = w ? gs[of][v].get(j) * ws[v].get(j) : gs[of][v].get(j);
-          o[j] = r * (g - s1 - h * s2);
-        }
-        if (c.any) store_w<T, W, true>(dx + row * n.ld_dx + c.at, o);
-      }
+    if (dx && here) rows[of].write(n, ws, w != nullptr, n.rms ? 0.0f : s1 / (float)n.dim, s2 / (float)n.dim, dx, row, me, THREADS);
   };
   // (two rows a turn, so that which registers hold which is known to the compiler)
   long long row0 = (long long)blockIdx.x * GROUPS;
@@ -238,6 +252,81 @@ __global__ __launch_bounds__(256) void fira_layer_norm_join_kernel(const float* 
 #pragma unroll
   for (int k = 0; k < SETS; ++k) all += sums[k][threadIdx.x];
   store1<P>(to + c0 + threadIdx.x, accumulate ? load1<P>(to + c0 + threadIdx.x) + all : all);
+}
+
+// Few rows: all in one launch and without a workspace.  The first workgroups take the rows, the others 8 W columns each, for which they read all
+// rows again: eight lanes to a row's columns, as many rows side by side as there are sets of eight lanes.
+constexpr int kFewRows = 512;
+template <typename T, typename P, int W, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm_gradient_few_kernel(FiraNorm n, const typename T::raw* dy, const typename T::raw* x,
+                                                                                                     const typename P::raw* w, const float* mean, const float* rstd,
+                                                                                                     typename T::raw* dx, typename P::raw* dw, typename P::raw* db,
+                                                                                                     int accumulate, int row_groups) {
+  constexpr int ALL = THREADS < 256 ? 256 : THREADS, GROUPS = ALL / THREADS;
+  __shared__ float part[2][16][2];
+  __shared__ float sums[ALL / 64][2][8 * W];
+  if ((int)blockIdx.x < row_groups) {
+    const int me = threadIdx.x % THREADS;
+    const long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / THREADS;
+    const bool here = row < n.rows;
+    Raw<P, W> ws[NV];
+    if (w)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) ws[v].load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+    int skip[NV];
+#pragma unroll
+    for (int v = NV / 2; v < NV; ++v) { const Columns<W> c((long long)(v * THREADS + me) * W, n.dim); skip[v] = c.any ? c.skip : W; }
+    NormRow<T, P, W, NV> r;
+    r.load(n, x, dy, mean, rstd, min(row, n.rows - 1), me, THREADS);
+    float s1 = 0.0f, s2 = 0.0f, sw[NV][W], sb[NV][W];    // (the sums over rows are not wanted here)
+    r.sums(ws, w != nullptr, skip, here, s1, s2, sw, sb);
+    row_sums<THREADS>(s1, s2, part, 0);
+    if (here) r.write(n, ws, w != nullptr, n.rms ? 0.0f : s1 / (float)n.dim, s2 / (float)n.dim, dx, row, me, THREADS);
+    return;
+  }
+  constexpr int SETS = ALL / 8, N = 4;
+  const int lane = threadIdx.x % 8, set = threadIdx.x / 8;
+  const Columns<W> c((long long)(blockIdx.x - row_groups) * (8 * W) + lane * W, n.dim);
+  float sw[W] = {}, sb[W] = {};
+  for (int row0 = set; row0 < (int)n.rows; row0 += N * SETS) {
+    Raw<T, W> xs[N], gs[N];
+    float mu[N], r[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const long long row = min((long long)row0 + k * SETS, n.rows - 1);
+      xs[k].load(x + row * n.ld_x + c.at);
+      gs[k].load(dy + row * n.ld_y + c.at);
+      mu[k] = n.rms ? 0.0f : *as_global(mean + row);
+      r[k] = *as_global(rstd + row);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (row0 + k * SETS < (int)n.rows)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          sw[j] += gs[k].get(j) * ((xs[k].get(j) - mu[k]) * r[k]);
+          sb[j] += gs[k].get(j);
+        }
+  }
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    sw[j] = add_xor<8>(add_xor<16>(add_xor<32>(sw[j])));
+    sb[j] = add_xor<8>(add_xor<16>(add_xor<32>(sb[j])));
+  }
+  if ((threadIdx.x & 63) < 8)
+#pragma unroll
+    for (int j = 0; j < W; ++j) { sums[threadIdx.x >> 6][0][j * 8 + lane] = sw[j]; sums[threadIdx.x >> 6][1][j * 8 + lane] = sb[j]; }
+  __syncthreads();
+  if (threadIdx.x >= 16) return;                         // eight lanes for dw, eight for db
+  typename P::raw* const to = threadIdx.x < 8 ? dw : db;
+  if (!to || !c.any) return;
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    float all = 0.0f;
+#pragma unroll
+    for (int k = 0; k < ALL / 64; ++k) all += sums[k][threadIdx.x >> 3][j * 8 + lane];
+    if (j >= c.skip) store1<P>(to + c.at + j, accumulate ? load1<P>(to + c.at + j) + all : all);
+  }
 }
 
 // Rows wider than kNormWidest: one workgroup per row, which reads it for each sum and for the result.

@@ -99,7 +99,7 @@ struct EmbedSort {
 EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
   EmbedSort r{};
   FiraEmbedSort& s = r.s;
-  if (count <= kFewTokens) { r.bytes = 256; return r; }      // no sort
+  if (count <= kFewTokens) { r.bytes = FIRA_UNUSED_WORKSPACE_BYTES; return r; }      // no sort
   char* const begin = at;
   auto take = [&](auto*& p, int64_t n) { p = (std::remove_reference_t<decltype(p)>)at; at += up256(n * sizeof *p); };
   s.chunk = (int)std::max<int64_t>(512, up256((count + kMostChunks - 1) / kMostChunks));
@@ -116,7 +116,7 @@ EmbedSort embed_sort(const fira_embed_desc* d, int64_t count, char* at) {
   take(s.pieces, r.pieces);
   take(s.cut, r.pieces);
   take(s.partial, r.pieces * d->dim);
-  r.bytes = at - begin;
+  r.bytes = at - begin;                                 // (more than that, of the lists' parts alone)
   return r;
 }
 
@@ -146,13 +146,18 @@ void with_row_shape(int64_t dim, F f) {
   else if (dim <= 8192) f(Int<W>{}, Int<1024 / D>{}, Int<D * N>{});
   else f(Int<W>{}, Int<1024>{}, Int<2 * N>{});
 }
-// Workgroups of the norm's gradient, each of which leaves its sums over rows: at most as many as the chip holds, and rows for all.
+// Workgroups of the norm's gradient, each of which leaves its sums over rows: as many as the chip holds, but fewer where that leaves each less than ten
+// turns (of a row, or of the rows that it has side by side), and a quarter of that at least.  2048 rows x 2048 f32: 16.5 us with 256 workgroups, 17.6
+// with 512, 24.7 with 1024; 5840 x 1680 f32: 34, 29.6 and 33.7; 16384 x 2048 bf16: 57, 49.7 and 49.3.
 int64_t norm_parts(const fira_layer_norm_desc* d) {
   if (d->dim > kNormWidest) return std::min<int64_t>(d->rows, 64);
   int64_t parts = 1;
   auto shape = [&](auto, auto threads, auto) {
     constexpr int THREADS = decltype(threads)::value, GROUPS = std::max(1, 256 / THREADS);
-    parts = std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 256 * 1024 / std::max(256, THREADS));
+    constexpr int64_t full = 256 * 1024 / std::max(256, THREADS);
+    const int64_t turns = std::max<int64_t>(1, (d->rows + GROUPS - 1) / GROUPS);
+    const int64_t each = std::min(std::max<int64_t>(10, (turns + full - 1) / full), (4 * turns + full - 1) / full);
+    parts = (turns + each - 1) / each;
   };
   if (d->dtype == FIRA_F32) with_row_shape<FiraStoredF32, 8>(d->dim, shape);
   else with_row_shape<FiraStoredBf16, 8>(d->dim, shape);
@@ -383,7 +388,8 @@ fira_status fira_layer_norm(const fira_layer_norm_desc* d, const void* dev_x, in
 }
 
 size_t fira_layer_norm_gradient_workspace_bytes(const fira_layer_norm_desc* d) {
-  return check_norm(d) ? 0 : up256(std::max<int64_t>(1, 2 * norm_parts(d) * d->dim * 4));
+  if (check_norm(d)) return 0;
+  return d->rows <= kFewRows && d->dim <= kNormWidest ? FIRA_UNUSED_WORKSPACE_BYTES : std::max<size_t>(2 * FIRA_UNUSED_WORKSPACE_BYTES, up256(2 * norm_parts(d) * d->dim * 4));
 }
 
 fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* dev_dy, int64_t ld_dy, const void* dev_x, int64_t ld_x,
@@ -412,13 +418,24 @@ fira_status fira_layer_norm_gradient(const fira_layer_norm_desc* d, const void* 
     const typename P::raw* const w = (const typename P::raw*)dev_weight;
     typename T::raw* const dx = (typename T::raw*)dev_dx;
     const hipStream_t q = (hipStream_t)hip_stream;
+    if (d->rows <= kFewRows && d->dim <= kNormWidest) {
+      with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
+        constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
+        const int rows = dx ? (int)((d->rows + GROUPS - 1) / GROUPS) : 0;
+        const int columns = (dev_dweight || dev_dbias) && (d->rows || !accumulate) ? (int)((d->dim + 8 * W - 1) / (8 * W)) : 0;
+        if (rows + columns)
+          hipLaunchKernelGGL((fira_layer_norm_gradient_few_kernel<T, P, W, THREADS, NV>), dim3(rows + columns), dim3(std::max(256, THREADS)), 0, q, n, dy, x, w, dev_mean,
+                             dev_rstd, dx, (typename P::raw*)dev_dweight, (typename P::raw*)dev_dbias, accumulate, rows);
+      });
+      return;
+    }
     const int parts = (int)norm_parts(d);
     float* const pw = dev_dweight ? (float*)dev_workspace : nullptr;
     float* const pb = dev_dbias ? (float*)dev_workspace + (int64_t)parts * d->dim : nullptr;
-    if (d->rows && d->dim > kNormWidest) {
-      if (dx) hipLaunchKernelGGL((fira_layer_norm_wide_dx_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx);
-      if (pw || pb) hipLaunchKernelGGL(fira_layer_norm_wide_dw_kernel<T>, dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dy, x, dev_mean, dev_rstd, pw, pb);
-    } else if (d->rows && (dx || pw || pb)) {
+    if (d->dim > kNormWidest) {
+      if (dx && d->rows) hipLaunchKernelGGL((fira_layer_norm_wide_dx_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx);
+      if ((pw || pb) && d->rows) hipLaunchKernelGGL(fira_layer_norm_wide_dw_kernel<T>, dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dy, x, dev_mean, dev_rstd, pw, pb);
+    } else if (dx || pw || pb) {
       with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
         constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
         hipLaunchKernelGGL((fira_layer_norm_gradient_kernel<T, P, W, THREADS, NV>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dy, x, w, dev_mean, dev_rstd, dx,

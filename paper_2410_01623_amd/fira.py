@@ -28,6 +28,7 @@ FIRA_SCALE_COLUMN, FIRA_SCALE_MATRIX, FIRA_SCALE_NONE = 0, 1, 2
 FIRA_VARIANT_FULL, FIRA_VARIANT_ONLY_SCALING = 0, 1
 FIRA_NORM_RESIDUAL, FIRA_NORM_GRAM = 0, 1
 FIRA_I32, FIRA_I64 = 0, 1
+FIRA_UNUSED_WORKSPACE_BYTES = 256
 FIRA_LAYER_NORM, FIRA_RMS_NORM = 0, 1
 FIRA_NUM_KERNELS = 6
 FIRA_STATIC_SCRATCH_BYTES = 64 << 20

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -26,8 +27,8 @@ def _refuse(status: int, message: str):
     raise FiraError(status, message)
 
 
-def _dtype(t, name: str) -> int:
-    dt = _DTYPE.get(t.dtype if isinstance(t, torch.Tensor) else t)
+def _dtype(dtype: torch.dtype, name: str) -> int:
+    dt = _DTYPE.get(dtype)
     if dt is None:
         _refuse(FIRA_ERR_DTYPE, f"{name} is neither bf16 nor fp32")
     return dt
@@ -126,7 +127,15 @@ def _workspace(given: Optional[torch.Tensor], need: int, dev) -> torch.Tensor:
         if given.device != dev or given.dtype != torch.uint8 or not given.is_contiguous():
             _refuse(FIRA_ERR_INVALID_ARG, f"workspace is not a dense byte tensor on {dev}")
         return given
+    if need == fira.FIRA_UNUSED_WORKSPACE_BYTES:
+        return _unused_workspace(dev)
     return torch.empty(need, dtype=torch.uint8, device=dev)
+
+
+@functools.lru_cache(maxsize=None)
+def _unused_workspace(dev) -> torch.Tensor:
+    """What calls are given that want a workspace but do not touch it."""
+    return torch.empty(fira.FIRA_UNUSED_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
 
 
 def _ids(ids: torch.Tensor) -> torch.Tensor:
@@ -149,7 +158,7 @@ def fira_embed_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 
         _refuse(FIRA_ERR_SHAPE, "the table is no matrix")
     dev = _device(table, ids, out)
     dtype = dtype or (out.dtype if out is not None else table.dtype)
-    dt, rdt = _dtype(table, "table"), _dtype(dtype, "result")
+    dt, rdt = _dtype(table.dtype, "table"), _dtype(dtype, "result")
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
         with elsewhere:
@@ -171,7 +180,7 @@ def fira_embed_gradient(dout: torch.Tensor, ids: torch.Tensor, rows: int, *, sca
     lib = fira.load_library()
     dev = _device(dout, ids, out)
     dtype = dtype or (out.dtype if out is not None else dout.dtype)
-    dt, rdt = _dtype(dtype, "result"), _dtype(dout, "dout")
+    dt, rdt = _dtype(dtype, "result"), _dtype(dout.dtype, "dout")
     if dout.dim() < 1 or dout.shape[:-1] != ids.shape:
         _refuse(FIRA_ERR_SHAPE, f"dout is {tuple(dout.shape)} for ids of {tuple(ids.shape)}")
     if accumulate and out is None:
@@ -200,7 +209,7 @@ def fira_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     if x.dim() < 1:
         _refuse(FIRA_ERR_SHAPE, "x has no dimension")
     dev = _device(x, weight, bias, out)
-    dt = _dtype(x, "x")
+    dt = _dtype(x.dtype, "x")
     pdt = _param_dtype(dt, weight, bias)
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
@@ -221,7 +230,7 @@ def _param_dtype(default: int, *params) -> int:
     given = None
     for p in params:
         if p is not None:
-            dt = _dtype(p, "parameter")
+            dt = _dtype(p.dtype, "parameter")
             if given is not None and dt != given:
                 _refuse(FIRA_ERR_DTYPE, "parameters of two types")
             given = dt
@@ -238,7 +247,7 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
     if x.dim() < 1 or dy.shape != x.shape:
         _refuse(FIRA_ERR_SHAPE, f"dy is {tuple(dy.shape)} for x of {tuple(x.shape)}")
     dev = _device(x, dy, weight, mean, rstd, dx, dweight, dbias)
-    dt = _dtype(x, "x")
+    dt = _dtype(x.dtype, "x")
     if dy.dtype != x.dtype:
         _refuse(FIRA_ERR_DTYPE, "dy is not of x's type")
     ptype = weight.dtype if weight is not None else param_dtype or (dweight.dtype if dweight is not None else x.dtype)
@@ -292,7 +301,7 @@ class GradientList:
             if o.shape != g.shape:
                 _refuse(FIRA_ERR_SHAPE, f"result {i} is {tuple(o.shape)}, not {tuple(g.shape)}")
             (rows, cols, ld), (_, _, ld_out) = self._matrix(g, f"gradient {i}"), self._matrix(o, f"result {i}")
-            self.descs[i] = fira.fira_gradient_desc(rows, cols, ld, _dtype(g, f"gradient {i}"), _dtype(o, f"result {i}"), ld_out)
+            self.descs[i] = fira.fira_gradient_desc(rows, cols, ld, _dtype(g.dtype, f"gradient {i}"), _dtype(o.dtype, f"result {i}"), ld_out)
         pointers = ctypes.c_void_p * n
         self.G = pointers(*[g.data_ptr() for g in grads])
         self.outs = pointers(*[o.data_ptr() for o in outs]) if outs is not None else None
