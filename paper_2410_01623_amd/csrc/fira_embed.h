@@ -480,62 +480,99 @@ __global__ __launch_bounds__(256) void fira_embed_join_kernel(FiraEmbed e, typen
   }
 }
 
-// Few tokens: no sort, every wavefront looks through all ids for kBatch neighbouring rows of the table and 64 W columns.
-constexpr int kFewTokens = 512;
+// Few tokens: no sort, every workgroup looks through all ids for kFewBatch neighbouring rows of the table and 64 W columns.  A row's tokens are summed in
+// the pieces and parts of the kernels above, so that it gets the same bits whatever the number of other tokens; of a row with more than one piece each
+// wavefront takes two of the eight parts (one token for all of 256: 34 us with one wavefront for it, 13 with four).
+constexpr int kFewTokens = 512, kFewBatch = 32;
 template <typename T, typename R, int W, bool ADD>
 __global__ __launch_bounds__(256) void fira_embed_few_kernel(FiraEmbed e, const typename R::raw* dout, const void* ids, typename T::raw* dtable) {
-  constexpr int N = 8;
+  constexpr int N = 8, PARTS = 8, GROUPS = kFewTokens / 64;
+  static_assert(kFewTokens <= 2 * PARTS * kPieceTokens, "a part is of two pieces at most");
   __shared__ short found[4][kFewTokens];
+  __shared__ float parts[PARTS][64 * W];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned tiles = (unsigned)((e.dim + 64 * W - 1) / (64 * W));
-  const long long all = (e.vocab + kBatch - 1LL) / kBatch * tiles;
-  int id[kFewTokens / 64];
+  const long long all = (e.vocab + kFewBatch - 1LL) / kFewBatch * tiles;
+  int id[GROUPS];
 #pragma unroll
-  for (int g = 0; g < kFewTokens / 64; ++g) id[g] = g * 64 + lane < e.count ? token_row(e, ids, g * 64 + lane) : -1;
+  for (int g = 0; g < GROUPS; ++g) id[g] = g * 64 + lane < e.count ? token_row(e, ids, g * 64 + lane) : -1;
   volatile short* const mine = found[wave];
-  for (long long i = (long long)blockIdx.x * 4 + wave; i < all; i += gridDim.x * 4LL) {
+  for (long long i = blockIdx.x; i < all; i += gridDim.x) {
     const long long unit = i / tiles;
     const Columns<W> c((i - unit * tiles) * (64 * W) + lane * W, e.dim);
-    const int row0 = (int)unit * kBatch, rows = min(kBatch, e.vocab - row0);
-    unsigned named = 0;                                  // rows of these with a token
+    const int row0 = (int)unit * kFewBatch, rows = min(kFewBatch, e.vocab - row0);
+    unsigned named = 0, several = 0;                     // rows of these with a token, with more than one piece
 #pragma unroll
-    for (int g = 0; g < kFewTokens / 64; ++g) {
+    for (int g = 0; g < GROUPS; ++g) {
       unsigned long long m = __ballot((unsigned)(id[g] - row0) < (unsigned)rows && id[g] >= 0);
       for (; m; m &= m - 1) named |= 1u << (__builtin_amdgcn_readlane(id[g], __builtin_ctzll(m)) - row0);
     }
-    for (int k = 0; k < rows; ++k) {
-      float sum[W] = {};
-      if (named >> k & 1) {
-        int total = 0;                                   // its tokens, in order
+    // the row's tokens in order, in this wavefront's list; their number
+    auto find = [&](int k) {
+      int total = 0;
 #pragma unroll
-        for (int g = 0; g < kFewTokens / 64; ++g) {
-          const bool is = id[g] == row0 + k;
-          const unsigned long long m = __ballot(is);
-          if (is) mine[total + __popcll(m & ((1ull << lane) - 1))] = (short)(g * 64 + lane);
-          total += __popcll(m);
-        }
-        __builtin_amdgcn_wave_barrier();
-        for (int p0 = 0; p0 < total; p0 += kPieceTokens) {     // in pieces as by the other kernels
-          float piece[W] = {};
-          const int until = min(p0 + kPieceTokens, total);
-          const int token = mine[min(p0 + (lane & (kPieceTokens - 1)), until - 1)];
-          for (int first = 0; p0 + first < until; first += N) {
-            Raw<R, W> x[N];
-#pragma unroll
-            for (int u = 0; u < N; ++u) x[u].load(dout + (long long)__builtin_amdgcn_readlane(token, first + u) * e.ld_rows + c.at);
-#pragma unroll
-            for (int u = 0; u < N; ++u)
-              if (p0 + first + u < until)
-#pragma unroll
-                for (int j = 0; j < W; ++j) piece[j] += x[u].get(j);
-          }
-#pragma unroll
-          for (int j = 0; j < W; ++j) sum[j] += piece[j];
-        }
-      } else if (ADD) {
-        continue;
+      for (int g = 0; g < GROUPS; ++g) {
+        const bool is = id[g] == row0 + k;
+        const unsigned long long m = __ballot(is);
+        if (is) mine[total + __popcll(m & ((1ull << lane) - 1))] = (short)(g * 64 + lane);
+        total += __popcll(m);
       }
+      __builtin_amdgcn_wave_barrier();
+      return total;
+    };
+    auto add_piece = [&](int p0, int total, float (&sum)[W]) {
+      float piece[W] = {};
+      const int until = min(p0 + kPieceTokens, total);
+      const int token = mine[min(p0 + (lane & (kPieceTokens - 1)), until - 1)];
+#pragma unroll 1
+      for (int first = 0; p0 + first < until; first += N) {
+        Raw<R, W> x[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) x[u].load(dout + (long long)__builtin_amdgcn_readlane(token, first + u) * e.ld_rows + c.at);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+          if (p0 + first + u < until)
+#pragma unroll
+            for (int j = 0; j < W; ++j) piece[j] += x[u].get(j);
+      }
+#pragma unroll
+      for (int j = 0; j < W; ++j) sum[j] += piece[j];
+    };
+    float zeros[W] = {};
+    if (!ADD)                                            // rows without a token, a quarter for each wavefront
+      for (unsigned m = ~named & (rows == 32 ? ~0u : (1u << rows) - 1) & (0xffu << 8 * wave); m; m &= m - 1)
+        if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + __builtin_ctz(m), c, zeros);
+#pragma unroll 1
+    for (unsigned m = named; m; m &= m - 1) {            // rows of one piece: a wavefront each
+      const int k = __builtin_ctz(m), total = find(k);
+      if (total > kPieceTokens) { several |= 1u << k; continue; }
+      if (k / 8 != wave) continue;
+      float sum[W] = {};
+      add_piece(0, total, sum);
       if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + k, c, sum);
+    }
+    for (; several; several &= several - 1) {            // (the same rows for all wavefronts)
+      const int k = __builtin_ctz(several), total = find(k);
+#pragma unroll 1
+      for (int part = wave; part < PARTS; part += 4) {
+        float sum[W] = {};
+#pragma unroll 1
+        for (int p0 = part * kPieceTokens; p0 < total; p0 += PARTS * kPieceTokens) add_piece(p0, total, sum);
+#pragma unroll
+        for (int j = 0; j < W; ++j) parts[part][j * 64 + lane] = sum[j];
+      }
+      __syncthreads();
+      if (wave == 0) {
+        float sum[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] = parts[0][j * 64 + lane];
+#pragma unroll
+        for (int part = 1; part < PARTS; ++part)
+#pragma unroll
+          for (int j = 0; j < W; ++j) sum[j] += parts[part][j * 64 + lane];
+        if (c.any) write_gradient<T, W, ADD>(e, dtable, row0 + k, c, sum);
+      }
+      __syncthreads();
     }
   }
 }

@@ -321,7 +321,7 @@ fira_status fira_embed_gradient(const fira_embed_desc* d, const void* dev_dout, 
       if (count <= kFewTokens) {
         auto few = [&](auto w) {
           constexpr int W = decltype(w)::value;
-          hipLaunchKernelGGL((fira_embed_few_kernel<T, R, W, ADD>), grid((d->rows + kBatch - 1) / kBatch * ((dim + 64 * W - 1) / (64 * W)), 4), dim3(256), 0, q, e,
+          hipLaunchKernelGGL((fira_embed_few_kernel<T, R, W, ADD>), grid((d->rows + kFewBatch - 1) / kFewBatch * ((dim + 64 * W - 1) / (64 * W)), 1), dim3(256), 0, q, e,
                              dout, dev_ids, dtable);
         };
         if (dim < kMostWidth) few(Int<1>{});

@@ -120,6 +120,25 @@ def test_embed_gradient_of_a_row_depends_on_its_own_tokens_only():
     assert same(a[450], training.fira_embed_gradient(dout[keep].contiguous(), ids[keep], 900, dtype=F32)[450])
 
 
+@pytest.mark.parametrize("dim", [5, 64, 520])
+@pytest.mark.parametrize("own", [1, 32, 33, 100, 257, 480, 512])
+def test_embed_gradient_of_a_row_does_not_depend_on_the_number_of_tokens(own, dim):
+    """The row of `own` tokens among no others, among a few, and among so many that the tokens are sorted; in fp32 and added to."""
+    gen = generator(own)
+    _, dout = matrix(3000, dim, 0, F32, gen)
+    got = []
+    for others in (0, 5, 513 - own if own < 512 else 1, 3000 - own):
+        at = torch.randperm(own + others, device=DEV, generator=gen)[:own].sort().values
+        ids = torch.randint(8, 50, (own + others,), device=DEV, generator=gen)
+        ids[at] = 7
+        rows = torch.randn(own + others, dim, device=DEV, generator=gen)
+        rows[at] = dout[:own]
+        out = torch.ones(50, dim, device=DEV)
+        got.append(training.fira_embed_gradient(rows, ids, 50, scale=0.7, out=out, accumulate=True)[7].clone())
+        got.append(training.fira_embed_gradient(rows, ids, 50, scale=0.7)[7])
+    assert all(same(a, got[0]) for a in got[2::2]) and all(same(a, got[1]) for a in got[3::2])
+
+
 def test_no_tokens():
     table = torch.randn(20, 24, device=DEV)
     none = torch.empty(0, dtype=torch.int64, device=DEV)
