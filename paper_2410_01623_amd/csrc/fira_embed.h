@@ -84,26 +84,15 @@ struct FiraEmbedSort {       // the sort's part of the workspace
   float* partial;            // [pieces][dim]
 };
 
-// Lanes that are `in` and have this lane's key of `bits` bits.  Up to four keys are taken out one after the other, since where there are many lanes to
-// be done most of them have the same one (the bucket of a text's most frequent token); the rest is compared bit by bit.
+// Lanes that are `in` and have this lane's key of `bits` bits.  (Taking keys out one after the other instead, or four of them before this, as the bucket of a
+// text's most frequent token has mostly one: 131072 tokens 130.9 and 129.8 us for 127.4.)
 __device__ __forceinline__ unsigned long long lanes_alike(unsigned key, int bits, bool in) {
-  unsigned long long rest = __ballot(in), mine = 0;
-#pragma unroll 1
-  for (int k = 0; k < 4; ++k) {
-    if (!rest) return mine;
-    const bool same = in && key == (unsigned)__builtin_amdgcn_readlane((int)key, __builtin_ctzll(rest));
-    const unsigned long long m = __ballot(same);
-    mine = same ? m : mine;
-    rest &= ~m;
-  }
-  if (!rest) return mine;
-  unsigned long long m = rest;
-#pragma unroll 1
+  unsigned long long m = __ballot(in);
   for (int b = 0; b < bits; ++b) {
-    const int bit = (int)(key << (31 - b)) >> 31;       // all ones where it is set
-    m &= ~(__ballot(bit) ^ (unsigned long long)(long long)bit);
+    const int mine = (int)(key << (31 - b)) >> 31;      // all ones where the bit is set
+    m &= ~(__ballot(mine) ^ (unsigned long long)(long long)mine);
   }
-  return mine ? mine : m;
+  return m;
 }
 // Sum of x over the threads before this one; *total: over all.  part: LDS, 17 values.
 __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
@@ -482,7 +471,7 @@ __global__ __launch_bounds__(256) void fira_embed_join_kernel(FiraEmbed e, typen
 
 // Few tokens: no sort, every workgroup looks through all ids for kFewBatch neighbouring rows of the table and 64 W columns.  A row's tokens are summed in
 // the pieces and parts of the kernels above, so that it gets the same bits whatever the number of other tokens; of a row with more than one piece each
-// wavefront takes two of the eight parts (one token for all of 256: 34 us with one wavefront for it, 13 with four).
+// wavefront takes two of the eight parts (one token for all of 256: 34 us with one wavefront for it, 19 with four).
 constexpr int kFewTokens = 512, kFewBatch = 32;
 template <typename T, typename R, int W, bool ADD>
 __global__ __launch_bounds__(256) void fira_embed_few_kernel(FiraEmbed e, const typename R::raw* dout, const void* ids, typename T::raw* dtable) {
