@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256) void fira_embed_sum_kernel(FiraEmbed e, const 
       row0 = key0 * kBuckets + bucket;                   // row k is row0 + k * kBuckets
       if (lane < kBatch && key0 + lane < (unsigned)s.bins) r = *as_global(s.rows + (long long)bucket * s.bins + key0 + lane);
     }
-    const int n = r[1] > kPieceTokens ? 0 : (int)r[1];
+    const int n = !piece && r[1] > kPieceTokens ? 0 : (int)r[1];      // (such rows are in pieces, which may be longer than that)
     int upto = n;                                        // tokens of the rows up to this lane's
 #pragma unroll
     for (int d = 1; d < kBatch; d <<= 1) { const int y = __shfl_up(upto, d, 64); upto += lane >= d ? y : 0; }
