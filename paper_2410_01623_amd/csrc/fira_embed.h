@@ -155,11 +155,18 @@ __global__ __launch_bounds__(256) void fira_embed_chunk_kernel(FiraEmbed e, cons
   }
 }
 
-// Tokens of a piece of a row with n tokens: at most 256 pieces, which the join has to read one after the other.
-__device__ __forceinline__ int piece_tokens(int n) {
+// How a row of n < 2^31 tokens is cut: at most 256 pieces, which the join has to read one after the other.  (256 pieces of the next length may be 2^31
+// tokens, and so may whole spans of all wavefronts: nothing here goes past 32 bits for it.)
+__host__ __device__ __forceinline__ int piece_tokens(int n) {
   int len = kPieceTokens;
-  while (n > 256 * len) len *= 2;
+  while ((n - 1) / 256 >= len) len *= 2;
   return len;
+}
+__host__ __device__ __forceinline__ int row_pieces(int n) { return n > kPieceTokens ? (n - 1) / piece_tokens(n) + 1 : 0; }
+// Entries of a bucket with `total` that each of its wavefronts places: whole groups of 64.
+__host__ __device__ __forceinline__ unsigned wave_span(unsigned total, unsigned waves) {
+  const unsigned each = total / waves + (total % waves != 0);
+  return each ? (each + 63) / 64 * 64 : 64;
 }
 
 // The bucket's entries come out of all chunks at once, a few threads to a chunk, side by side into LDS (those of the bucket of a text's most frequent
@@ -192,7 +199,7 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
   int base, total;
   block_scan(before, part, &base);
   int at = block_scan(n, part, &total);                 // (where steps is 1: entries of the chunks before this thread's)
-  const int span = max(64, ((total + waves - 1) / waves + 63) / 64 * 64);   // entries of a wavefront
+  const unsigned span = wave_span(total, waves);
   const bool in_lds = total <= room;
   int done = 0;
   for (int k = 0; k < steps; ++k) {
@@ -214,7 +221,7 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (j + u * each < (int)mine[1]) {
-          const int to = at + j + u * each;
+          const unsigned to = at + j + u * each;
           if (in_lds) staged[to] = entry[u];
           else *as_global(s.gathered + base + to) = entry[u];
           atomicAdd(count + to / span * s.bins + entry[u][0], 1);
@@ -241,7 +248,7 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
     }
     // rows in pieces: one addition per workgroup hands out the places for all of them, as those of all workgroups wait for one another;
     // which places does not matter to any result
-    const int len = piece_tokens(sum), pieces = sum > kPieceTokens ? (sum + len - 1) / len : 0;
+    const int len = piece_tokens(sum), pieces = row_pieces(sum);
     if (__syncthreads_or(pieces)) {
       int all_pieces, all_rows;
       const int my_pieces = block_scan(pieces, part, &all_pieces), my_row = block_scan(pieces > 0, part, &all_rows);
@@ -260,9 +267,9 @@ __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, Fi
   }
   __syncthreads();
   volatile int* const own = count + wave * s.bins;
-  const int until = min((wave + 1) * span, total);
+  const unsigned until = min((wave + 1) * span, (unsigned)total);
 #pragma unroll 1
-  for (int i = wave * span + lane; i - lane < until; i += 64) {
+  for (unsigned i = wave * span + lane; i - lane < until; i += 64) {
     const bool in = i < until;
     u32x2 entry{0, 0};
     if (in_lds) { if (in) entry = staged[i]; }
