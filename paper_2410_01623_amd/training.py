@@ -3,10 +3,11 @@ and root-mean-square norm, each with its gradient, and the norm and clipping of 
 
 As in `fira`, this is argument marshalling: tensors become pointers, sizes and leading dimensions, everything is computed by
 libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.  `stream` is the torch stream to enqueue on (default: the
-current one of that GPU); the caller orders it after whatever made the inputs.  Results and workspaces that are not given
-are allocated on that stream.  Of a tensor with more than two dimensions all but the last are its rows.  An input whose rows cannot
-be told from one leading dimension (an expanded or permuted view) is copied first; a result given by the caller has
-to be such a matrix.  What the library refuses raises fira.FiraError with its status, and so does a tensor that does not fit the others."""
+current one of that GPU); the caller orders it after whatever made the inputs, and keeps tensors of another stream until it has passed
+the call.  Results and workspaces that are not given are allocated on that stream.  Of a tensor with more than two dimensions all but
+the last are its rows.  An input whose rows cannot be told from one leading dimension (an expanded or permuted view) is copied first; a
+result given by the caller has to be such a matrix.  What the library refuses raises fira.FiraError with its status, and so does a
+tensor that does not fit the others."""
 from __future__ import annotations
 
 import contextlib
@@ -283,8 +284,9 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
 
 class GradientList:
     """Gradients that are measured and clipped together, marshalled once: any tensors of bf16 and fp32 on one GPU that can be seen as
-    matrices.  outs, one per gradient and of its shape, take the clipped gradients in their own type; without them clipping is in place.  The
-    workspace is the list's own, so that its calls belong on one stream at a time."""
+    matrices.  outs, one per gradient and of its shape, take the clipped gradients in their own type; without them clipping is in place.  A list
+    holds no device memory but the tensors it was given: the workspace is allocated on the stream of each call, so that a list may be used on any
+    stream, and dropped while its calls are still at work if the tensors are kept."""
 
     def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, device: Optional[torch.device] = None):
         self.lib = fira.load_library()
@@ -306,7 +308,6 @@ class GradientList:
         self.G = pointers(*[g.data_ptr() for g in grads])
         self.outs = pointers(*[o.data_ptr() for o in outs]) if outs is not None else None
         self.bytes = self.lib.fira_gradient_workspace_bytes(self.descs, n)
-        self.workspace = torch.empty(max(self.bytes, 256), dtype=torch.uint8, device=self.device)
         self._keep = (grads, list(outs) if outs is not None else None)
 
     @staticmethod
@@ -319,14 +320,17 @@ class GradientList:
         cols = t.shape[-1]
         return (t.numel() // cols if cols else 0), cols, ld
 
+    def _result_and_workspace(self) -> Tuple[torch.Tensor, torch.Tensor]:
+        return torch.empty((), dtype=torch.float32, device=self.device), torch.empty(self.bytes, dtype=torch.uint8, device=self.device)
+
     def fira_gradient_norm(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The norm of all gradients together, an fp32 scalar on the GPU."""
         elsewhere = _elsewhere(self.device, stream)
         if elsewhere is not None:
             with elsewhere:
                 return self.fira_gradient_norm()
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
-        _check(self.lib.fira_gradient_norm(self.descs, self.count, self.G, norm.data_ptr(), self.workspace.data_ptr(), self.bytes, _stream(self.device)))
+        norm, workspace = self._result_and_workspace()
+        _check(self.lib.fira_gradient_norm(self.descs, self.count, self.G, norm.data_ptr(), workspace.data_ptr(), self.bytes, _stream(self.device)))
         return norm
 
     def fira_clip_gradients(self, max_norm: float, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
@@ -336,7 +340,7 @@ class GradientList:
         if elsewhere is not None:
             with elsewhere:
                 return self.fira_clip_gradients(max_norm)
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
-        _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), self.workspace.data_ptr(),
+        norm, workspace = self._result_and_workspace()
+        _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), workspace.data_ptr(),
                                             self.bytes, _stream(self.device)))
         return norm
