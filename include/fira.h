@@ -377,16 +377,16 @@ typedef struct {
 } fira_gradient_desc;
 
 /* *dev_norm (fp32) = sqrt of the sum of the squares of all values of all `count` gradients; the squares are summed in fp64, so that no
- * finite gradient overflows on the way.  d and dev_G are host arrays of length count. */
+ * finite gradient overflows on the way (a norm that fp32 does not hold is inf).  d and dev_G are host arrays of length count. */
 FIRA_API size_t fira_gradient_workspace_bytes(const fira_gradient_desc* d, int count);
 FIRA_API fira_status fira_gradient_norm(const fira_gradient_desc* d, int count, const void* const* dev_G, float* dev_norm,
                                         void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradient clipping by that norm n: every gradient times min(1, max_norm / n), *dev_norm = n, the norm before.  dev_out[i] (host array) is where
  * gradient i goes, converted to out_dtype; it may be dev_G[i] itself with the same type and leading dimension.  dev_out NULL: all in place, and
- * then gradients that need no cut are read once and not written.  A norm that is not finite leaves the values as they are (the caller sees
- * it in *dev_norm), as the norm-growth limiter of fira_step leaves such a step.  max_norm >= 0, +inf for no limit.  The tensors must
- * not overlap one another. */
+ * then gradients that need no cut are read once and not written.  A norm that is not finite, as it stands in *dev_norm (one beyond the
+ * range of fp32 is inf there), leaves the values as they are, as the norm-growth limiter of fira_step leaves such a step.  max_norm >= 0,
+ * +inf for no limit.  The tensors must not overlap one another. */
 FIRA_API fira_status fira_clip_gradients(const fira_gradient_desc* d, int count, void* const* dev_G, void* const* dev_out, double max_norm,
                                          float* dev_norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -108,14 +108,14 @@ __global__ __launch_bounds__(256) void fira_gradient_norm_kernel(const double* p
   if (threadIdx.x == 0) *as_global(norm) = (float)x;
 }
 
-// out = min(1, max_norm / norm) g.  A norm that is not finite leaves the gradients as they are.  Every workgroup works the norm out for itself, and
-// one of them leaves it in *norm: no launch in between.
+// out = min(1, max_norm / norm) g.  A norm that is not finite, as the fp32 value that the caller reads, leaves the gradients as they are.  Every
+// workgroup works the norm out for itself, and one of them leaves it in *norm: no launch in between.
 template <typename T, typename R>
 __global__ __launch_bounds__(256) void fira_clip_kernel(FiraSpans l, const double* partial, int n, double max_norm, float* norm) {
   __shared__ double part[4];
   const double x = norm_of(partial, n, part);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *as_global(norm) = (float)x;
-  const bool cut = x > max_norm && x < INFINITY;
+  const bool cut = x > max_norm && (float)x < INFINITY;
   const float factor = cut ? (float)(max_norm / x) : 1.0f;
   for_each_tile(l, [&](const FiraSpan& s, unsigned first) {
     if (!cut && s.g == s.out) return;                    // in place: they are what they have to be
