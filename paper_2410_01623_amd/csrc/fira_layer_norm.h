@@ -278,7 +278,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_layer_norm
     for (int v = NV / 2; v < NV; ++v) { const Columns<W> c((long long)(v * THREADS + me) * W, n.dim); skip[v] = c.any ? c.skip : W; }
     NormRow<T, P, W, NV> r;
     r.load(n, x, dy, mean, rstd, min(row, n.rows - 1), me, THREADS);
-    float s1 = 0.0f, s2 = 0.0f, sw[NV][W], sb[NV][W];    // (the sums over rows are not wanted here)
+    float s1 = 0.0f, s2 = 0.0f, sw[NV][W] = {}, sb[NV][W] = {};      // (the sums over rows are not wanted here)
     r.sums(ws, w != nullptr, skip, here, s1, s2, sw, sb);
     row_sums<THREADS>(s1, s2, part, 0);
     if (here) r.write(n, ws, w != nullptr, n.rms ? 0.0f : s1 / (float)n.dim, s2 / (float)n.dim, dx, row, me, THREADS);
