@@ -193,9 +193,12 @@ def fira_embed_gradient(dout: torch.Tensor, ids: torch.Tensor, rows: int, *, sca
     ids = _ids(ids)
     dout, ld_dout = _input(dout)
     dim, count = dout.shape[-1], ids.numel()
-    out, ld = _result(out, (rows, dim), dtype, dev, "out")
-    d = fira.fira_embed_desc(rows, dim, ld, dt, rdt, _IDS[ids.dtype], scale)
-    workspace = _workspace(workspace, lib.fira_embed_gradient_workspace_bytes(d, count), dev)
+    d = fira.fira_embed_desc(rows, dim, dim, dt, rdt, _IDS[ids.dtype], scale)
+    need = lib.fira_embed_gradient_workspace_bytes(d, count)
+    if not need:                                         # refused: before anything of such a size is allocated
+        _check(lib.fira_embed_gradient(d, None, ld_dout, None, count, None, 0, None, 0, None))
+    out, d.ld = _result(out, (rows, dim), dtype, dev, "out")
+    workspace = _workspace(workspace, need, dev)
     _check(lib.fira_embed_gradient(d, dout.data_ptr(), ld_dout, ids.data_ptr(), count, out.data_ptr(), bool(accumulate),
                                    workspace.data_ptr(), workspace.numel(), _stream(dev)))
     return out
