@@ -296,7 +296,7 @@ class GradientList:
         grads = list(grads)
         if not grads and device is None:
             _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
-        self.device = _device(*grads, *(outs or ())) if grads else torch.empty(0, device=device).device
+        self.device = _device(*(grads or [torch.empty(0, device=device)]), *(outs or ()))
         if outs is not None and len(outs) != len(grads):
             _refuse(FIRA_ERR_INVALID_ARG, f"{len(outs)} results for {len(grads)} gradients")
         n = self.count = len(grads)
