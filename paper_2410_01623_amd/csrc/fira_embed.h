@@ -172,7 +172,8 @@ __host__ __device__ __forceinline__ unsigned wave_span(unsigned total, unsigned 
 // The bucket's entries come out of all chunks at once, a few threads to a chunk, side by side into LDS (those of the bucket of a text's most frequent
 // token may be too many: into the workspace then), and are counted on the way; a wavefront then places a part of them.  What has to wait for memory
 // waits once for all of it: with a group of 64 entries after the other, each fetched from another XCD's work, the largest of the 256 buckets of 131072
-// tokens took 21 us.
+// tokens took 21 us.  The workgroup is alone with its bucket: with a fifth of those tokens one id it takes 54 us, with all of them 218 (the whole gradient,
+// x 1024 in fp32, 127, 163 and 345 us).
 // (dynamic LDS: a counter per wavefront and row of the bucket, then the entries)
 __global__ __launch_bounds__(1024) void fira_embed_bucket_kernel(FiraEmbed e, FiraEmbedSort s) {
   extern __shared__ int count[];
@@ -312,7 +313,8 @@ __device__ __forceinline__ void write_gradient(const FiraEmbed& e, typename T::r
 // Loads of N rows are put on their way together, without a branch between them; beyond the last row it is loaded again.  (One copy of the loop's
 // body: with blocks of 8, 4, 2 and 1 for the remainder the wavefronts of fira_embed_sum_kernel waited for instructions half of their time.)
 
-// Widths up to 256: LANES lanes to a row; four tokens' rows are on their way at a time.  The pieces come first, as they take longest.
+// Widths up to 32 W: LANES lanes to a row; four tokens' rows are on their way at a time.  The pieces come first, as they take longest.  Bound by memory and
+// by what has to be waited for one after the other: 131072 tokens x 128 bf16, 50257 rows, 16.5 us (2.8 TB/s) of the gradient's 43, the sort being 22.
 template <typename T, typename R, int W, int LANES, bool ADD>
 __global__ __launch_bounds__(256) void fira_embed_sum_narrow_kernel(FiraEmbed e, const typename R::raw* dout, typename T::raw* dtable, FiraEmbedSort s) {
   constexpr int N = 4;
@@ -479,6 +481,8 @@ __global__ __launch_bounds__(256) void fira_embed_join_kernel(FiraEmbed e, typen
 // Few tokens: no sort, every workgroup looks through all ids for kFewBatch neighbouring rows of the table and 64 W columns.  A row's tokens are summed in
 // the pieces and parts of the kernels above, so that it gets the same bits whatever the number of other tokens; of a row with more than one piece each
 // wavefront takes two of the eight parts (one token for all of 256: 34 us with one wavefront for it, 19 with four).
+// Up to kFewTokens, the most that two pieces a part hold; us here and with the sort, bf16: 512 tokens x 512 of 32000 rows 9.6 and 20.4, x 2048 24.7 and 36.5, x 512
+// of 131072 rows 25 and 38, x 192 of 768 rows 15.0 and 15.9; the sort is ahead where most tokens are one id of a small table (512 x 512, all of them 36 and 24).
 constexpr int kFewTokens = 512, kFewBatch = 32;
 template <typename T, typename R, int W, bool ADD>
 __global__ __launch_bounds__(256) void fira_embed_few_kernel(FiraEmbed e, const typename R::raw* dout, const void* ids, typename T::raw* dtable) {

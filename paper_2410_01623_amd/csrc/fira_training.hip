@@ -283,6 +283,10 @@ fira_status fira_embed_lookup(const fira_embed_desc* d, const void* dev_table, c
     else if (d->dim <= 8 * W) launch(Int<W>{}, Int<8>{}, Int<1>{}, Int<16>{});
     else if (d->dim <= 16 * W) launch(Int<W>{}, Int<16>{}, Int<1>{}, Int<8>{});
     else if (d->dim <= 32 * W) launch(Int<W>{}, Int<32>{}, Int<1>{}, Int<4>{});
+    // (2048 or 1024 columns where a row is made of such, else 512.  Wide ones pay where tables and results leave the caches, and cost where few wavefronts are
+    // left to wait.  us with 512, 1024 and 2048 columns, 32000 rows: 131072 tokens x 2048, f32 to bf16 176, 175, 169, bf16 120, 115, 117, bf16 to f32 190, 209, 203;
+    // 65536 x 4096 bf16 153, 132, 143; 131072 x 1024 bf16 55, 57, 57, of 131072 rows 70, 60, 61; 4096 x 2048 bf16 6.4, 6.0, 5.9; 16384 x 4096 bf16 31, 34, 34;
+    // 256 x 2048 bf16 3.0, 3.2, 3.7, which is less than the call takes to reach the GPU)
     else if ((d->dim + 511) / 512 % 4 == 0) launch(Int<W>{}, Int<64>{}, Int<32 / W>{}, Int<2>{});
     else if ((d->dim + 511) / 512 % 2 == 0) launch(Int<W>{}, Int<64>{}, Int<16 / W>{}, Int<2>{});
     else launch(Int<W>{}, Int<64>{}, Int<8 / W>{}, Int<2>{});

@@ -6,8 +6,11 @@ libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.
 current one of that GPU); the caller orders it after whatever made the inputs, and keeps tensors of another stream until it has passed
 the call.  Results and workspaces that are not given are allocated on that stream.  Of a tensor with more than two dimensions all but
 the last are its rows.  An input whose rows cannot be told from one leading dimension (an expanded or permuted view) is copied first; a
-result given by the caller has to be such a matrix.  What the library refuses raises fira.FiraError with its status, and so does a
-tensor that does not fit the others."""
+result given by the caller has to be such a matrix, and must not overlap an input.  What the library refuses raises fira.FiraError with its status, and so does a
+tensor that does not fit the others.
+
+Autograd does not see these calls: their results carry no graph, whether or not an input requires a gradient, and gradients are what
+the *_gradient calls return (examples/train_small_lm.py has them as torch.autograd.Function)."""
 from __future__ import annotations
 
 import contextlib
@@ -246,7 +249,8 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
                              dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
                              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Gradients of fira_layer_norm -> (dx, dweight, dbias); dbias is None without `bias`.  mean and rstd are the forward pass's.  dweight and dbias
-    are of weight's type (without weight: param_dtype, default x's).  accumulate adds them to what the given dweight and dbias hold."""
+    are of weight's type (without weight: param_dtype, default x's).  accumulate adds them to what the given dweight and dbias hold, rounding to
+    their type each time: to add up a bf16 weight's gradients in fp32, give weight.float(), whose values are the same."""
     lib = fira.load_library()
     if x.dim() < 1 or dy.shape != x.shape:
         _refuse(FIRA_ERR_SHAPE, f"dy is {tuple(dy.shape)} for x of {tuple(x.shape)}")
