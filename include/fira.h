@@ -390,6 +390,59 @@ FIRA_API fira_status fira_gradient_norm(const fira_gradient_desc* d, int count, 
 FIRA_API fira_status fira_clip_gradients(const fira_gradient_desc* d, int count, void* const* dev_G, void* const* dev_out, double max_norm,
                                          float* dev_norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- AdamW over a list of tensors ----
+ * For what fira_step is not for: embeddings, heads, norms, or all tensors of a model.  One step, with c = 1, or max_norm / norm where the
+ * norm passes max_norm and is finite (as in fira_clip_gradients, whose second pass this saves; G is not written):
+ *     t = t + 1,  g = c G
+ *     m = b1 m + (1-b1) g,  v = b2 v + (1-b2) g^2
+ *     W = (1 - lr weight_decay) W - lr (m / (1-b1^t)) / (sqrt(v / (1-b2^t)) + eps)
+ * (eps stands beside the corrected root; fira_step's Adam has it beside the root alone, as Eq. 4 does.)  W is rounded once, to nearest even.
+ *
+ * States of FIRA_STATE_F32 are m and v, in fp32.  Those of FIRA_STATE_E4M3 are m and sqrt(v), of which the step works with the new values before
+ * they are rounded: 256 neighbouring values (of the tensor's rows one after the other; the last such block may be shorter) share an fp32 scale, their
+ * largest size / 448, and each value is held as the OCP e4m3 code (1 sign, 4 exponent, 3 mantissa bits) of value / scale.  It is rounded up
+ * or down at random, with the chances that keep its mean: to nearest, changes below a sixteenth would be lost, and an average over a
+ * thousand steps changes by a thousandth in each.  With u = (r + 1/2) / 2^16 the code is the one at or below |value| / scale + u steps (a step: the distance of codes
+ * there).  r is 16 bits, the low ones for m and the high ones for sqrt(v), of
+ *     hash(i, seed, t) = mix(i + mix(mix(seed) + t)),   mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16     (modulo 2^32)
+ * with i the value's place in the tensor and t the number of the step: the same call gives the same bits.  A sqrt(v) above zero is held as
+ * the smallest code at least, so that a step is never divided by eps alone.  A block whose largest size is below 2^-100 is held as zeros.  What is not finite is held as NaN and
+ * spoils nothing but its own value; in fp32 it stays what it is.
+ * A tensor's result does not depend on what else is listed. */
+typedef enum { FIRA_STATE_F32 = 0, FIRA_STATE_E4M3 = 1 } fira_state_type;
+typedef struct {
+  int64_t rows, cols;      /* any tensor as a matrix; cols < 2^31 where rows are apart */
+  int64_t ld_w, ld_g;
+  int32_t dtype;           /* fira_dtype of W */
+  int32_t grad_dtype;      /* fira_dtype of G */
+  int32_t state_type;      /* fira_state_type */
+  uint32_t seed;           /* of the rounding of FIRA_STATE_E4M3 */
+  double weight_decay;     /* >= 0 */
+} fira_adamw_desc;
+/* m, v: rows * cols values without gaps, zero at first: fp32, or a byte each.  m_scale, v_scale: fira_adamw_scales() fp32 values of a FIRA_STATE_E4M3 tensor,
+ * zero at first; not looked at with FIRA_STATE_F32. */
+typedef struct {
+  void *m, *v;
+  float *m_scale, *v_scale;
+} fira_adamw_state;
+typedef struct {
+  double lr, beta1, beta2, eps;    /* betas in [0, 1), eps > 0 as fp32 */
+  double max_norm;                 /* >= 0, +inf for no limit; looked at with dev_norm only */
+} fira_adamw_hparams;
+
+/* Scales of each of m and v: a value for every 256 of the tensor, or 0 for invalid arguments and for FIRA_STATE_F32. */
+FIRA_API int64_t fira_adamw_scales(const fira_adamw_desc* d);
+
+/* d, dev_W, dev_G and dev_state are host arrays of length count; W is updated in place.
+ *   dev_t      two int64 on the device, zero before the first step: the steps taken, which the call counts up, and a value that the call needs
+ *              and leaves at zero.  One for each list, not to be used by two calls at a time.
+ *   dev_lr     the learning rate as an fp32 scalar on the device, or NULL: hp->lr.  With it, a schedule reaches a step that replays from a HIP graph; all
+ *              else is as it was at capture.
+ *   dev_norm   the gradients' norm, as fira_gradient_norm leaves it, or NULL: they are not cut.
+ * The tensors must not overlap one another. */
+FIRA_API fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adamw_hparams* hp, void* const* dev_W, const void* const* dev_G,
+                                     const fira_adamw_state* dev_state, int64_t* dev_t, const float* dev_lr, const float* dev_norm, void* hip_stream);
+
 FIRA_API const char* fira_last_error(const fira_ctx* ctx);
 
 FIRA_API void fira_destroy(fira_ctx* ctx);

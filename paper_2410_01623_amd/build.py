@@ -17,7 +17,7 @@ HIPCC_FLAGS = [
 ]
 
 
-SOURCES = ("fira.hip", "fira_training.hip")   # the optimizer step; the operators around it
+SOURCES = ("fira.hip", "fira_training.hip", "fira_model.hip")   # the optimizer step; the operators around it, in two parts
 
 
 def build_library(verbose: bool = True, extra_flags=()) -> str:

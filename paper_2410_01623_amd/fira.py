@@ -29,7 +29,8 @@ FIRA_VARIANT_FULL, FIRA_VARIANT_ONLY_SCALING = 0, 1
 FIRA_NORM_RESIDUAL, FIRA_NORM_GRAM = 0, 1
 FIRA_I32, FIRA_I64 = 0, 1
 FIRA_UNUSED_WORKSPACE_BYTES = 256
-FIRA_LAYER_NORM, FIRA_RMS_NORM = 0, 1
+FIRA_LAYER_NORM, FIRA_RMS_NORM, FIRA_NO_NORM = 0, 1, 2
+FIRA_STATE_F32, FIRA_STATE_E4M3 = 0, 1
 FIRA_NUM_KERNELS = 6
 FIRA_STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -43,6 +44,7 @@ EXPORTS = (
     "fira_embed_lookup", "fira_embed_gradient_workspace_bytes", "fira_embed_gradient",
     "fira_layer_norm", "fira_layer_norm_gradient_workspace_bytes", "fira_layer_norm_gradient",
     "fira_gradient_workspace_bytes", "fira_gradient_norm", "fira_clip_gradients",
+    "fira_adamw_scales", "fira_adamw_step",
 )
 
 
@@ -69,6 +71,19 @@ class fira_layer_norm_desc(ctypes.Structure):
 class fira_gradient_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("out_dtype", ctypes.c_int32), ("ld_out", ctypes.c_int64)]
+
+
+class fira_adamw_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld_w", ctypes.c_int64), ("ld_g", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("state_type", ctypes.c_int32), ("seed", ctypes.c_uint32), ("weight_decay", ctypes.c_double)]
+
+
+class fira_adamw_state(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class fira_adamw_hparams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("max_norm", ctypes.c_double)]
 
 
 class FiraError(RuntimeError):
@@ -170,6 +185,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fira_gradient_norm.argtypes = [grad, ci, ctypes.POINTER(vp), vp, vp, cz, vp]
     lib.fira_clip_gradients.restype = ci
     lib.fira_clip_gradients.argtypes = [grad, ci, ctypes.POINTER(vp), ctypes.POINTER(vp), cd, vp, vp, cz, vp]
+    adamw, state, adamw_hp = (ctypes.POINTER(t) for t in (fira_adamw_desc, fira_adamw_state, fira_adamw_hparams))
+    lib.fira_adamw_scales.restype = c64
+    lib.fira_adamw_scales.argtypes = [adamw]
+    lib.fira_adamw_step.restype = ci
+    lib.fira_adamw_step.argtypes = [adamw, ci, adamw_hp, ctypes.POINTER(vp), ctypes.POINTER(vp), state, vp, vp, vp, vp]
     if path is None:
         _lib = lib
     return lib

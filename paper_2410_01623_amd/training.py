@@ -1,5 +1,5 @@
 """The operators around the optimizer step, by the names of their C entry points (include/fira.h): embedding lookup, layer norm
-and root-mean-square norm, each with its gradient, and the norm and clipping of a list of gradients.
+and root-mean-square norm, each with its gradient, the norm and clipping of a list of gradients, and AdamW over a list of tensors.
 
 As in `fira`, this is argument marshalling: tensors become pointers, sizes and leading dimensions, everything is computed by
 libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.  `stream` is the torch stream to enqueue on (default: the
@@ -351,3 +351,79 @@ class GradientList:
         _check(self.lib.fira_clip_gradients(self.descs, self.count, self.G, self.outs, max_norm, norm.data_ptr(), workspace.data_ptr(),
                                             self.bytes, _stream(self.device)))
         return norm
+
+
+_STATES = {torch.float32: fira.FIRA_STATE_F32, torch.float8_e4m3fn: fira.FIRA_STATE_E4M3}
+
+
+class AdamWList:
+    """Tensors that take AdamW steps together, marshalled once: parameters and gradients of bf16 and fp32 (a gradient's type need not be its
+    parameter's) on one GPU that can be seen as matrices, and their states.  weight_decay: of all, or one for each.  state: torch.float32 or
+    torch.float8_e4m3fn, of all or one for each; the latter's m and sqrt(v) are codes, to be multiplied with the scale of their 256 values, and
+    are rounded at random by seeds (default: the place in the list).
+
+    m, v, m_scale, v_scale (lists; the scales of a float32 state are None) and t (two int64: the steps taken, and a value of the call's) are a
+    checkpoint.  Those that are not given begin at zero, on the stream that is current then."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, weight_decay=0.0, state=torch.float32,
+                 m: Optional[Sequence[torch.Tensor]] = None, v: Optional[Sequence[torch.Tensor]] = None, m_scale: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 v_scale: Optional[Sequence[Optional[torch.Tensor]]] = None, t: Optional[torch.Tensor] = None, seeds: Optional[Sequence[int]] = None,
+                 device: Optional[torch.device] = None):
+        self.lib = fira.load_library()
+        params, grads = list(params), list(grads)
+        if not params and device is None:
+            _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
+        n = self.count = len(params)
+        each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
+        decays, states, seeds = each(weight_decay), each(state) if m is None else [x.dtype for x in m], list(range(n)) if seeds is None else list(seeds)
+        for given, name in ((grads, "gradients"), (decays, "weight decays"), (states, "states"), (seeds, "seeds"), (v if m is not None else states, "states v")):
+            if given is None or len(given) != n:
+                _refuse(FIRA_ERR_INVALID_ARG, f"{None if given is None else len(given)} {name} for {n} tensors")
+        for i, x in enumerate(states):
+            if x not in _STATES:
+                _refuse(FIRA_ERR_DTYPE, f"state {i} is neither float32 nor float8_e4m3fn")
+        self.device = dev = _device(*(params or [torch.empty(0, device=device)]), *grads)
+        self.descs = (fira.fira_adamw_desc * n)()
+        for i, (p, g) in enumerate(zip(params, grads)):
+            if p.shape != g.shape:
+                _refuse(FIRA_ERR_SHAPE, f"gradient {i} is {tuple(g.shape)}, not {tuple(p.shape)}")
+            (rows, cols, ld_w), (_, _, ld_g) = GradientList._matrix(p, f"tensor {i}"), GradientList._matrix(g, f"gradient {i}")
+            self.descs[i] = fira.fira_adamw_desc(rows, cols, ld_w, ld_g, _dtype(p.dtype, f"tensor {i}"), _dtype(g.dtype, f"gradient {i}"), _STATES[states[i]],
+                                                 seeds[i] & 0xffffffff, decays[i])
+        sizes, scales = [p.numel() for p in params], [self.lib.fira_adamw_scales(self.descs[i]) for i in range(n)]
+        self.m, self.v = ([self._state(x, i, sizes[i], states[i], name) for i, x in enumerate(given or [None] * n)] for given, name in ((m, "m"), (v, "v")))
+        if m is not None and any(s is torch.float8_e4m3fn for s in states) and (m_scale is None or v_scale is None):
+            _refuse(FIRA_ERR_INVALID_ARG, "8-bit states without their scales")
+        self.m_scale, self.v_scale = ([self._state(x, i, scales[i], torch.float32, name) if states[i] is not torch.float32 else None
+                                       for i, x in enumerate(given or [None] * n)] for given, name in ((m_scale, "m_scale"), (v_scale, "v_scale")))
+        self.t = self._state(t, 0, 2, torch.int64, "t")
+        pointers = ctypes.c_void_p * n
+        self.W, self.G = pointers(*[p.data_ptr() for p in params]), pointers(*[g.data_ptr() for g in grads])
+        at = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        self.states = (fira.fira_adamw_state * n)(*[fira.fira_adamw_state(*map(at, x)) for x in zip(self.m, self.v, self.m_scale, self.v_scale)])
+        self._keep = (params, grads)
+
+    def _state(self, given, i: int, size: int, dtype, name: str) -> torch.Tensor:
+        if given is None:
+            return torch.zeros(size, dtype=torch.uint8 if dtype is torch.float8_e4m3fn else dtype, device=self.device).view(dtype)
+        if given.dtype != dtype or given.numel() != size or not given.is_contiguous():
+            _refuse(FIRA_ERR_SHAPE, f"{name} of tensor {i} is not {size} dense values of {dtype}")
+        if given.device != self.device:
+            _refuse(FIRA_ERR_INVALID_ARG, f"tensors on {self.device} and {given.device}")
+        return given
+
+    def fira_adamw_step(self, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, *, norm: Optional[torch.Tensor] = None,
+                        max_norm: float = float("inf"), stream: Optional[torch.cuda.Stream] = None):
+        """One step of all tensors, in place.  lr: a number, or an fp32 scalar on the GPU, which a captured step reads again.  norm: the gradients' norm, an
+        fp32 scalar on the GPU (GradientList.fira_gradient_norm), by which they are cut to max_norm on their way in."""
+        given = lr if isinstance(lr, torch.Tensor) else None
+        for x, name in ((given, "lr"), (norm, "norm")):
+            if x is not None and (x.device != self.device or x.dtype != torch.float32 or x.numel() != 1):
+                _refuse(FIRA_ERR_INVALID_ARG, f"{name} is not an fp32 scalar on {self.device}")
+        elsewhere = _elsewhere(self.device, stream)
+        if elsewhere is not None:
+            with elsewhere:
+                return self.fira_adamw_step(lr, beta1, beta2, eps, norm=norm, max_norm=max_norm)
+        hp = fira.fira_adamw_hparams(0.0 if given is not None else lr, beta1, beta2, eps, max_norm)
+        _check(self.lib.fira_adamw_step(self.descs, self.count, hp, self.W, self.G, self.states, self.t.data_ptr(), None if given is None else given.data_ptr(),
+                                        None if norm is None else norm.data_ptr(), _stream(self.device)))

@@ -1,0 +1,55 @@
+"""What AdamW, rotary positions and the block norm refuse, and that they enqueue nothing then (no GPU)."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2410_01623_amd import fira, training
+
+P = ctypes.c_void_p(4096)          # never looked at: every call here is refused on the host, or has nothing to do
+ODD = ctypes.c_void_p(4097)
+N = None
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return fira.load_library()
+
+
+def adamw(rows=4, cols=8, ld_w=8, ld_g=8, dtype=0, grad_dtype=1, state_type=1, seed=0, weight_decay=0.0):
+    return fira.fira_adamw_desc(rows, cols, ld_w, ld_g, dtype, grad_dtype, state_type, seed, weight_decay)
+
+
+def test_adamw(lib):
+    P2, P3 = ctypes.c_void_p(8192), ctypes.c_void_p(16384)
+    one = lambda p: (ctypes.c_void_p * 1)(p)  # noqa: E731
+    state = lambda m=P, v=P2, ms=P, vs=P: (fira.fira_adamw_state * 1)(fira.fira_adamw_state(m, v, ms, vs))  # noqa: E731
+    hp = lambda lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, max_norm=1.0: fira.fira_adamw_hparams(lr, b1, b2, eps, max_norm)  # noqa: E731
+
+    def call(d=adamw(), count=1, h=hp(), W=one(P), G=one(P3), s=state(), t=P, lr=N, norm=N):
+        return lib.fira_adamw_step(d, count, h, W, G, s, t, lr, norm, N)
+
+    for d, want in ((adamw(rows=-1), -2), (adamw(cols=-1), -2), (adamw(rows=1 << 31), -2), (adamw(ld_w=7), -2), (adamw(ld_g=7), -2), (adamw(ld_w=1 << 62), -2), (adamw(dtype=2), -4),
+                    (adamw(grad_dtype=-1), -4), (adamw(state_type=2), -4), (adamw(weight_decay=-0.1), -1), (adamw(weight_decay=math.nan), -1), (adamw(weight_decay=math.inf), -1),
+                    (adamw(rows=2, cols=1 << 31, ld_w=1 << 31, ld_g=(1 << 31) + 1), -2)):
+        assert call(d) == want and lib.fira_adamw_scales(d) == 0
+        assert len(lib.fira_last_error(None)) > 0
+    for h in (None, hp(lr=math.nan), hp(lr=math.inf), hp(b1=-0.1), hp(b1=1.0), hp(b2=1.0), hp(b2=1.0 - 1e-12), hp(b2=math.nan), hp(eps=0.0), hp(eps=-1e-8), hp(eps=1e-60), hp(eps=math.inf)):
+        assert call(h=h) == -1
+    for bad in (-1.0, math.nan):
+        assert call(h=hp(max_norm=bad), norm=P) == -1
+    for args in (dict(count=-1), dict(d=None), dict(W=None), dict(G=None), dict(s=None), dict(t=N), dict(t=ctypes.c_void_p(4100)), dict(lr=ODD), dict(norm=ODD), dict(W=one(N)), dict(G=one(N)),
+                 dict(W=one(ODD)), dict(G=one(ODD)), dict(s=state(m=N)), dict(s=state(v=N)), dict(s=state(ms=N)), dict(s=state(vs=N)), dict(s=state(ms=ODD)), dict(W=one(P3)),
+                 dict(s=state(v=P)), dict(d=adamw(state_type=0), s=state(m=ODD))):
+        assert call(**args) == -1, args
+    assert lib.fira_adamw_scales(adamw()) == 1 and lib.fira_adamw_scales(adamw(rows=33)) == 2 and lib.fira_adamw_scales(adamw(rows=0)) == 0
+    assert lib.fira_adamw_scales(adamw(state_type=0)) == 0 and lib.fira_adamw_scales(None) == 0
+
+
+def test_adamw_lists_of_cpu_tensors():
+    w = torch.zeros(3)
+    for args, kwargs in ((([w], [w]), {}), (([], []), {}), (([], []), {"device": "cpu"}), (([w], []), {}), (([w], [w]), {"state": torch.float16}), (([w], [w]), {"m": [w]}),
+                         (([w], [w]), {"weight_decay": [0.0, 0.0]})):
+        with pytest.raises(fira.FiraError):
+            training.AdamWList(*args, **kwargs)
