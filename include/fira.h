@@ -443,6 +443,45 @@ FIRA_API int64_t fira_adamw_scales(const fira_adamw_desc* d);
 FIRA_API fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adamw_hparams* hp, void* const* dev_W, const void* const* dev_G,
                                      const fira_adamw_state* dev_state, int64_t* dev_t, const float* dev_lr, const float* dev_norm, void* hip_stream);
 
+/* ---- Rotary positions ----
+ * The first `rotated` values of every head of a token at position p are turned, pair by pair, by the angle p f_j, and multiplied by `scale`:
+ *     (a, b) -> scale (a cos - b sin, a sin + b cos)
+ * and the other dim - rotated values are copied.  Pair j is (x_j, x_(j + rotated/2)) with FIRA_ROTARY_HALVES and (x_2j, x_(2j+1)) with FIRA_ROTARY_INTERLEAVED.  Angles are
+ * taken in fp64 (in fp32 an angle of 10^6 is off by 0.06), sines and cosines to fp32's accuracy; results are rounded once. */
+typedef enum { FIRA_ROTARY_HALVES = 0, FIRA_ROTARY_INTERLEAVED = 1 } fira_rotary_layout;
+typedef struct {
+  int64_t batch, length;   /* sequences, and tokens of each */
+  int64_t dim, rotated;    /* values of a head, 1 to 2^16, and how many are turned: even, 2 to dim */
+  int32_t dtype;           /* fira_dtype */
+  int32_t layout;          /* fira_rotary_layout */
+  int32_t position_type;   /* fira_index_type of dev_positions */
+  int64_t position_stride; /* values between the positions of one sequence and the next, >= 0 (0: all have the same); those of a sequence are neighbours */
+  double scale;            /* finite, as fp32 */
+} fira_rotary_desc;
+/* The heads of one tensor (queries, or keys).  Strides in elements, of sequences, tokens and heads, >= 0; a head's values are neighbours.  Those of the
+ * result must keep its elements apart: in the order of their size, each at least the extent of what the one before spans.  dev_y may be dev_x with the same strides. */
+typedef struct {
+  const void* dev_x;
+  void* dev_y;
+  int64_t heads;
+  int64_t x_stride[3], y_stride[3];
+} fira_rotary_heads;
+
+/* `count` tensors (1 to 4) of one description.  dev_frequencies: rotated/2 fp64 angles of one position.  dev_positions: any integers, or NULL: 0 to length - 1 in every
+ * sequence.  Sequences times tokens, and the heads of a tensor, are below 2^31. */
+FIRA_API fira_status fira_rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* dev_frequencies, const void* dev_positions,
+                                 void* hip_stream);
+/* The gradient: dev_x are the gradients of the results, dev_y those of the inputs; the transpose, scale times the turn by -p f_j. */
+FIRA_API fira_status fira_rotary_gradient(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* dev_frequencies, const void* dev_positions,
+                                          void* hip_stream);
+
+/* Frequencies f_j = base^(-2j/rotated) in host memory, for contexts longer than the `trained` one.  FIRA_ROTARY_LINEAR: f_j / factor.  FIRA_ROTARY_BY_PARTS: what turns fewer
+ * than `low` times over the trained context is divided by factor, what turns more than `high` times is kept, in between it goes over linearly in the
+ * number of turns; *scale is then 0.1 ln(factor) + 1, else 1. */
+typedef enum { FIRA_ROTARY_PLAIN = 0, FIRA_ROTARY_LINEAR = 1, FIRA_ROTARY_BY_PARTS = 2 } fira_rotary_context;
+FIRA_API fira_status fira_rotary_frequencies(int64_t rotated, double base, int32_t context, double factor, double trained, double low, double high,
+                                             double* host_frequencies, double* scale);
+
 FIRA_API const char* fira_last_error(const fira_ctx* ctx);
 
 FIRA_API void fira_destroy(fira_ctx* ctx);

@@ -2,6 +2,7 @@
 // state, no allocation, nothing that throws.
 #include "fira_host.h"
 #include "fira_adamw.h"
+#include "fira_rotary.h"
 
 namespace {
 
@@ -24,6 +25,69 @@ fira_status check_adamw_hparams(const fira_adamw_hparams* hp, bool norm) {
   if (!((float)hp->eps > 0.0f) || !std::isfinite((float)hp->eps)) return refuse(FIRA_ERR_INVALID_ARG, "eps is not positive and finite");
   if (norm && !(hp->max_norm >= 0.0)) return refuse(FIRA_ERR_INVALID_ARG, "max_norm is negative or not a number");
   return FIRA_OK;
+}
+
+// Whether the elements of a result are apart: strides in the order of their size, each at least what those before it span.  span: of all.
+bool strides_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t dim, bool result, int64_t* span) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+  int64_t extent = dim, most = dim;
+  for (int k : order) {
+    int64_t far;
+    if (size[k] <= 1) continue;
+    if (result && stride[k] < extent) return false;
+    if (stride[k] < 0 || __builtin_mul_overflow(stride[k], size[k] - 1, &far) || far > INT64_MAX / 16) return false;
+    extent = far + extent;
+    most += far;
+  }
+  *span = most;
+  return true;
+}
+
+fira_status check_rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* frequencies, const void* positions) {
+  if (!d || !h) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
+  if (count < 1 || count > 4) return refuse(FIRA_ERR_INVALID_ARG, "%d tensors to turn", count);
+  if (d->batch < 0 || d->length < 0 || d->batch > kMost || d->length > kMost || d->batch * d->length > kMost)
+    return refuse(FIRA_ERR_SHAPE, "%lld sequences of %lld tokens", (long long)d->batch, (long long)d->length);
+  if (d->dim < 1 || d->dim > 1 << 16 || d->rotated < 2 || d->rotated > d->dim || d->rotated % 2) return refuse(FIRA_ERR_SHAPE, "heads of %lld, %lld turned", (long long)d->dim, (long long)d->rotated);
+  if (!known(d->dtype) || (d->position_type != FIRA_I32 && d->position_type != FIRA_I64)) return refuse(FIRA_ERR_DTYPE, "rotary types %d and %d", d->dtype, d->position_type);
+  if (d->layout != FIRA_ROTARY_HALVES && d->layout != FIRA_ROTARY_INTERLEAVED) return refuse(FIRA_ERR_INVALID_ARG, "rotary layout %d", d->layout);
+  if (!std::isfinite((float)d->scale)) return refuse(FIRA_ERR_INVALID_ARG, "scale is not finite");
+  if (d->position_stride < 0 || d->position_stride > kMost) return refuse(FIRA_ERR_SHAPE, "position stride %lld", (long long)d->position_stride);
+  if (!d->batch || !d->length) return FIRA_OK;
+  for (int i = 0; i < count; ++i) {
+    if (h[i].heads < 0 || h[i].heads > kMost) return refuse(FIRA_ERR_SHAPE, "%lld heads", (long long)h[i].heads);
+    if (!h[i].heads) continue;
+    const int64_t size[3] = {d->batch, d->length, h[i].heads};
+    int64_t span;
+    if (!strides_apart(size, h[i].x_stride, d->dim, false, &span)) return refuse(FIRA_ERR_SHAPE, "strides of tensor %d are negative or out of range", i);
+    if (!strides_apart(size, h[i].y_stride, d->dim, true, &span)) return refuse(FIRA_ERR_SHAPE, "strides of result %d let elements overlap, or are out of range", i);
+    if (!h[i].dev_x || !h[i].dev_y || !aligned(h[i].dev_x, size_of(d->dtype)) || !aligned(h[i].dev_y, size_of(d->dtype)))
+      return refuse(FIRA_ERR_INVALID_ARG, "tensor or result %d is null or not aligned to its elements", i);
+    if (h[i].dev_x == h[i].dev_y)
+      for (int k = 0; k < 3; ++k)
+        if (size[k] > 1 && h[i].x_stride[k] != h[i].y_stride[k]) return refuse(FIRA_ERR_INVALID_ARG, "tensor %d in place with other strides", i);
+  }
+  FIRA_POINTER(frequencies, 8);
+  if (!aligned(positions, d->position_type == FIRA_I64 ? 8 : 4)) return refuse(FIRA_ERR_INVALID_ARG, "positions are not aligned to their elements");
+  return FIRA_OK;
+}
+
+fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* frequencies, const void* positions, float sign, void* hip_stream) {
+  if (const fira_status st = check_rotary(d, h, count, frequencies, positions)) return st;
+  if (!d->batch || !d->length) return FIRA_OK;
+  for (int i = 0; i < count; ++i) {
+    const int64_t total = d->batch * d->length * h[i].heads * (d->dim - d->rotated / 2);
+    if (!total) continue;
+    FiraRotary r{d->batch, d->length, h[i].heads, d->dim, d->rotated, d->position_stride, {}, {}, (float)d->scale, sign, d->layout == FIRA_ROTARY_INTERLEAVED, d->position_type == FIRA_I64};
+    for (int k = 0; k < 3; ++k) { r.xs[k] = h[i].x_stride[k]; r.ys[k] = h[i].y_stride[k]; }
+    with_types(d->dtype, d->dtype, [&](auto t, auto) {
+      typedef typename decltype(t)::raw raw;
+      hipLaunchKernelGGL(fira_rotary_kernel<decltype(t)>, dim3(std::min<int64_t>((total + 255) / 256, 1 << 20)), dim3(256), 0, (hipStream_t)hip_stream, r, (const raw*)h[i].dev_x,
+                         (raw*)h[i].dev_y, frequencies, positions);
+    });
+  }
+  return launched("rotary positions");
 }
 
 }  // namespace
@@ -69,6 +133,33 @@ fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adam
   }
   hipLaunchKernelGGL(fira_adamw_count_kernel<>, dim3(1), dim3(1), 0, q, (long long*)dev_t);
   return launched("AdamW step");
+}
+
+fira_status fira_rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* dev_frequencies, const void* dev_positions, void* hip_stream) {
+  return rotary(d, h, count, dev_frequencies, dev_positions, 1.0f, hip_stream);
+}
+
+fira_status fira_rotary_gradient(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* dev_frequencies, const void* dev_positions, void* hip_stream) {
+  return rotary(d, h, count, dev_frequencies, dev_positions, -1.0f, hip_stream);
+}
+
+fira_status fira_rotary_frequencies(int64_t rotated, double base, int32_t context, double factor, double trained, double low, double high, double* host_frequencies,
+                                    double* scale) {
+  if (rotated < 2 || rotated > 1 << 16 || rotated % 2) return refuse(FIRA_ERR_SHAPE, "%lld values turned", (long long)rotated);
+  if (!host_frequencies) return refuse(FIRA_ERR_INVALID_ARG, "host_frequencies is null");
+  if (!(base > 0.0) || !std::isfinite(base)) return refuse(FIRA_ERR_INVALID_ARG, "base is not positive and finite");
+  if (context < FIRA_ROTARY_PLAIN || context > FIRA_ROTARY_BY_PARTS) return refuse(FIRA_ERR_INVALID_ARG, "context %d", context);
+  if (context != FIRA_ROTARY_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return refuse(FIRA_ERR_INVALID_ARG, "factor is below one or not finite");
+  if (context == FIRA_ROTARY_BY_PARTS && !(trained > 0.0 && std::isfinite(trained) && low >= 0.0 && high > low && std::isfinite(high)))
+    return refuse(FIRA_ERR_INVALID_ARG, "trained context, low or high out of range");
+  for (int64_t j = 0; j < rotated / 2; ++j) {
+    const double f = std::pow(base, -2.0 * (double)j / (double)rotated);
+    double keep = context == FIRA_ROTARY_PLAIN ? 1.0 : 0.0;
+    if (context == FIRA_ROTARY_BY_PARTS) keep = std::min(1.0, std::max(0.0, (trained * f / 6.283185307179586477 - low) / (high - low)));
+    host_frequencies[j] = keep == 1.0 ? f : f * keep + f / factor * (1.0 - keep);
+  }
+  if (scale) *scale = context == FIRA_ROTARY_BY_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return FIRA_OK;
 }
 
 }  // extern "C"

@@ -31,6 +31,8 @@ FIRA_I32, FIRA_I64 = 0, 1
 FIRA_UNUSED_WORKSPACE_BYTES = 256
 FIRA_LAYER_NORM, FIRA_RMS_NORM, FIRA_NO_NORM = 0, 1, 2
 FIRA_STATE_F32, FIRA_STATE_E4M3 = 0, 1
+FIRA_ROTARY_HALVES, FIRA_ROTARY_INTERLEAVED = 0, 1
+FIRA_ROTARY_PLAIN, FIRA_ROTARY_LINEAR, FIRA_ROTARY_BY_PARTS = 0, 1, 2
 FIRA_NUM_KERNELS = 6
 FIRA_STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -45,6 +47,7 @@ EXPORTS = (
     "fira_layer_norm", "fira_layer_norm_gradient_workspace_bytes", "fira_layer_norm_gradient",
     "fira_gradient_workspace_bytes", "fira_gradient_norm", "fira_clip_gradients",
     "fira_adamw_scales", "fira_adamw_step",
+    "fira_rotary", "fira_rotary_gradient", "fira_rotary_frequencies",
 )
 
 
@@ -84,6 +87,15 @@ class fira_adamw_state(ctypes.Structure):
 
 class fira_adamw_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("max_norm", ctypes.c_double)]
+
+
+class fira_rotary_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("length", ctypes.c_int64), ("dim", ctypes.c_int64), ("rotated", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("position_type", ctypes.c_int32), ("position_stride", ctypes.c_int64), ("scale", ctypes.c_double)]
+
+
+class fira_rotary_heads(ctypes.Structure):
+    _fields_ = [("dev_x", ctypes.c_void_p), ("dev_y", ctypes.c_void_p), ("heads", ctypes.c_int64), ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3)]
 
 
 class FiraError(RuntimeError):
@@ -190,6 +202,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fira_adamw_scales.argtypes = [adamw]
     lib.fira_adamw_step.restype = ci
     lib.fira_adamw_step.argtypes = [adamw, ci, adamw_hp, ctypes.POINTER(vp), ctypes.POINTER(vp), state, vp, vp, vp, vp]
+    rotary, heads = ctypes.POINTER(fira_rotary_desc), ctypes.POINTER(fira_rotary_heads)
+    for call in (lib.fira_rotary, lib.fira_rotary_gradient):
+        call.restype = ci
+        call.argtypes = [rotary, heads, ci, vp, vp, vp]
+    lib.fira_rotary_frequencies.restype = ci
+    lib.fira_rotary_frequencies.argtypes = [c64, cd, ctypes.c_int32, cd, cd, cd, cd, ctypes.POINTER(cd), ctypes.POINTER(cd)]
     if path is None:
         _lib = lib
     return lib

@@ -1,5 +1,6 @@
 """The operators around the optimizer step, by the names of their C entry points (include/fira.h): embedding lookup, layer norm
-and root-mean-square norm, each with its gradient, the norm and clipping of a list of gradients, and AdamW over a list of tensors.
+and root-mean-square norm, each with its gradient, the norm and clipping of a list of gradients, AdamW over a list
+of tensors, and rotary positions.
 
 As in `fira`, this is argument marshalling: tensors become pointers, sizes and leading dimensions, everything is computed by
 libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.  `stream` is the torch stream to enqueue on (default: the
@@ -287,6 +288,106 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
                                         None if rms else mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), ld_dx, _vector(dweight, dim, "dweight"),
                                         _vector(dbias, dim, "dbias"), bool(accumulate), workspace.data_ptr(), workspace.numel(), _stream(dev)))
     return dx, dweight, dbias
+
+
+def fira_rotary_frequencies(rotated: int, base: float = 10000.0, *, context: int = fira.FIRA_ROTARY_PLAIN, factor: float = 1.0, trained: float = 4096.0,
+                            low: float = 1.0, high: float = 32.0, device="cuda") -> Tuple[torch.Tensor, float]:
+    """-> (angles of one position, rotated / 2 fp64 values on `device`, and the scale that goes with them) for fira_rotary; context: FIRA_ROTARY_PLAIN, or
+    FIRA_ROTARY_LINEAR or FIRA_ROTARY_BY_PARTS for one `factor` times as long as the trained one."""
+    lib = fira.load_library()
+    f, scale = (ctypes.c_double * max(1, rotated // 2))(), ctypes.c_double()
+    _check(lib.fira_rotary_frequencies(rotated, base, context, factor, trained, low, high, f, scale))
+    return torch.tensor(list(f), dtype=torch.float64, device=device), scale.value
+
+
+def fira_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[torch.Tensor], frequencies: torch.Tensor, *, interleaved: bool = False,
+                scale: float = 1.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Turns queries and keys (k may be None) of shape (..., length, heads, dim), each with heads of its own, by their positions -> (q, k).  The first
+    2 * len(frequencies) values of a head are turned, the rest copied; frequencies: fp64, as fira_rotary_frequencies makes them.  positions: int32 or int64 of shape
+    (..., length) or (length,), or None: 0, 1, ... in every sequence.  q_out and k_out may be q and k themselves.  Any strides will do where a head's
+    values are neighbours and the leading dimensions can be seen as one, as in parts of one buffer of queries, keys and values; other inputs are copied first."""
+    return _rotary("fira_rotary", q, k, positions, frequencies, interleaved, scale, q_out, k_out, stream)
+
+
+def fira_rotary_gradient(dq: torch.Tensor, dk: Optional[torch.Tensor], positions: Optional[torch.Tensor], frequencies: torch.Tensor, *, interleaved: bool = False,
+                         scale: float = 1.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Gradients of fira_rotary's q and k from those of its results, with the arguments of that call."""
+    return _rotary("fira_rotary_gradient", dq, dk, positions, frequencies, interleaved, scale, q_out, k_out, stream)
+
+
+def _heads(t: torch.Tensor):
+    """Strides of sequences, tokens and heads of t, or None if it has no such."""
+    shape, strides = t.shape, t.stride()
+    if shape[-1] > 1 and strides[-1] != 1:
+        return None
+    batch = 0
+    need = None            # stride that the next dimension outwards has to have
+    for size, stride in zip(reversed(shape[:-3]), reversed(strides[:-3])):
+        if size == 1:
+            continue
+        if need is None:
+            batch = stride
+        elif stride != need:
+            return None
+        need = stride * size
+    return batch, strides[-3], strides[-2]
+
+
+def _rotary(name, q, k, positions, frequencies, interleaved, scale, q_out, k_out, stream):
+    lib = fira.load_library()
+    if k is None and k_out is not None:
+        _refuse(FIRA_ERR_INVALID_ARG, "k_out without k")
+    for t in (q, k):
+        if t is not None and (t.dim() < 3 or t.shape[:-2] != q.shape[:-2] or t.shape[-1] != q.shape[-1]):
+            _refuse(FIRA_ERR_SHAPE, f"queries are {tuple(q.shape)}, keys {None if k is None else tuple(k.shape)}")
+    dev = _device(q, k, positions, frequencies, q_out, k_out)
+    dt = _dtype(q.dtype, "q")
+    if k is not None and k.dtype != q.dtype:
+        _refuse(FIRA_ERR_DTYPE, "k is not of q's type")
+    if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
+        _refuse(FIRA_ERR_DTYPE, "frequencies are not a dense fp64 vector")
+    length, (heads, dim) = q.shape[-3], q.shape[-2:]
+    stride = 0
+    if positions is not None:
+        if positions.dtype not in _IDS:
+            _refuse(FIRA_ERR_DTYPE, "positions are neither int32 nor int64")
+        if positions.shape != q.shape[:-2] and positions.shape != (length,):
+            _refuse(FIRA_ERR_SHAPE, f"positions are {tuple(positions.shape)} for tokens of {tuple(q.shape[:-2])}")
+        stride = length if positions.dim() > 1 else 0
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return _rotary(name, q, k, positions, frequencies, interleaved, scale, q_out, k_out, None)
+    if positions is not None:
+        positions = positions.contiguous()
+    rows = fira.fira_rotary_heads * (1 if k is None else 2)
+    h, outs, keep = rows(), [], []
+    for i, (x, given) in enumerate(((q, q_out), (k, k_out))):
+        if x is None:
+            outs.append(None)
+            continue
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev) if given is None else given
+        if out.shape != x.shape or out.dtype != x.dtype:
+            _refuse(FIRA_ERR_SHAPE, f"result {i} is {tuple(out.shape)} of {out.dtype}, not {tuple(x.shape)} of {x.dtype}")
+        to = _heads(out)
+        if to is None:
+            _refuse(FIRA_ERR_SHAPE, f"result {i} has no strides of sequences, tokens and heads")
+        at = _heads(x)
+        if at is None:
+            x = x.contiguous()
+            at = _heads(x)
+        keep.append(x)
+        h[i] = fira.fira_rotary_heads(x.data_ptr(), out.data_ptr(), x.shape[-2], (ctypes.c_int64 * 3)(*at), (ctypes.c_int64 * 3)(*to))
+        outs.append(out)
+    batch = 1
+    for n in q.shape[:-3]:
+        batch *= n
+    d = fira.fira_rotary_desc(batch, length, dim, 2 * frequencies.shape[0], dt, fira.FIRA_ROTARY_INTERLEAVED if interleaved else fira.FIRA_ROTARY_HALVES,
+                              FIRA_I64 if positions is None else _IDS[positions.dtype], stride, scale)
+    _check(getattr(lib, name)(d, h, len(h), frequencies.data_ptr(), None if positions is None else positions.data_ptr(), _stream(dev)))
+    return outs[0], outs[1]
 
 
 class GradientList:

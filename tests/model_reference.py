@@ -71,3 +71,24 @@ def adamw(w, g, m, v, taken, decay, lr, b1, b2, eps, cut=1.0):
     w2 = w * (1.0 - lr * decay) - step
     # (the smallest results are fp32 subnormals: off by a step of those)
     return {"w": (w2, off + 3 * U * np.abs(w) + U * np.abs(step)), "m": (m2, off_m + 1e-44), "v": (v2, off_v + 1e-44), "root": (root, off_root + 1e-22)}
+
+
+# ---- rotary positions ----------------------------------------------------------------------------------------------
+
+
+def rotary(x, positions, frequencies, interleaved, scale, gradient):
+    """x: (batch, length, heads, dim), positions: (batch, length) whole numbers -> (y, bound).  Off may be: the angle by 4 roundings of fp64 and one of fp32 of half a turn, the sine by
+    4 u, its scale by 1, products and sum by 3."""
+    dtype = x.dtype
+    x, f = f64(x), f64(frequencies)
+    scale = float(np.float32(scale))
+    angle = np.asarray(positions, dtype=np.float64)[..., None] * f
+    off_angle = (np.abs(angle) * 4 * 2.0 ** -53 + math.pi * U + 5 * U)[..., None, :]
+    c, s = scale * np.cos(angle)[..., None, :], scale * (-np.sin(angle) if gradient else np.sin(angle))[..., None, :]
+    half, rotated = len(f), 2 * len(f)
+    a, b = (slice(0, rotated, 2), slice(1, rotated, 2)) if interleaved else (slice(0, half), slice(half, rotated))
+    y, off = x.copy(), np.zeros_like(x)
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+    size = abs(scale) * (np.abs(x[..., a]) + np.abs(x[..., b])) * (off_angle + 3 * U)
+    off[..., a] = off[..., b] = size
+    return y, off + np.where(off > 0, HALF_ULP[dtype] * (np.abs(y) + off) * (1 + 1e-3) + TINY, 0.0)

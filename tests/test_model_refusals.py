@@ -53,3 +53,33 @@ def test_adamw_lists_of_cpu_tensors():
                          (([w], [w]), {"weight_decay": [0.0, 0.0]})):
         with pytest.raises(fira.FiraError):
             training.AdamWList(*args, **kwargs)
+
+
+def test_rotary(lib):
+    desc = lambda batch=2, length=3, dim=16, rotated=8, dtype=0, layout=0, position_type=1, position_stride=3, scale=1.0: fira.fira_rotary_desc(  # noqa: E731
+        batch, length, dim, rotated, dtype, layout, position_type, position_stride, scale)
+    strides = ctypes.c_int64 * 3
+    heads = lambda x=P, y=ctypes.c_void_p(8192), n=4, xs=(192, 64, 16), ys=(192, 64, 16): (fira.fira_rotary_heads * 1)(fira.fira_rotary_heads(x, y, n, strides(*xs), strides(*ys)))  # noqa: E731
+    for call in (lib.fira_rotary, lib.fira_rotary_gradient):
+        for d, want in ((None, -1), (desc(batch=-1), -2), (desc(length=-1), -2), (desc(batch=1 << 20, length=1 << 20), -2), (desc(dim=0), -2), (desc(dim=(1 << 16) + 1), -2), (desc(rotated=0), -2),
+                        (desc(rotated=7), -2), (desc(rotated=18), -2), (desc(dtype=2), -4), (desc(position_type=2), -4), (desc(layout=2), -1), (desc(scale=math.nan), -1), (desc(scale=1e60), -1),
+                        (desc(position_stride=-1), -2), (desc(position_stride=1 << 40), -2)):
+            assert call(d, heads(), 1, P, P, N) == want
+        for h, want in ((None, -1), (heads(x=N), -1), (heads(y=N), -1), (heads(x=ODD), -1), (heads(y=ODD), -1), (heads(n=-1), -2), (heads(n=1 << 31), -2), (heads(ys=(192, 64, 15)), -2),
+                        (heads(ys=(192, 63, 16)), -2), (heads(ys=(191, 64, 16)), -2), (heads(ys=(0, 64, 16)), -2), (heads(xs=(-192, 64, 16)), -2), (heads(xs=(1 << 62, 64, 16)), -2),
+                        (heads(ys=(1 << 62, 64, 16)), -2), (heads(x=P, y=P, xs=(384, 64, 16)), -1)):
+            assert call(desc(), h, 1, P, P, N) == want, want
+            assert len(lib.fira_last_error(None)) > 0
+        for count, f, p in ((0, P, P), (5, P, P), (1, N, P), (1, ctypes.c_void_p(4100), P), (1, P, ctypes.c_void_p(4100))):
+            assert call(desc(), heads(), count, f, p, N) == -1
+        assert call(desc(batch=0), heads(), 1, N, N, N) == 0 and call(desc(length=0), heads(x=N, y=N), 1, N, N, N) == 0
+
+
+def test_rotary_frequencies(lib):
+    f, scale = (ctypes.c_double * 8)(), ctypes.c_double()
+    for args, want in (((0, 1e4, 0, 1, 1, 1, 2), -2), ((15, 1e4, 0, 1, 1, 1, 2), -2), (((1 << 16) + 2, 1e4, 0, 1, 1, 1, 2), -2), ((16, 0.0, 0, 1, 1, 1, 2), -1), ((16, math.inf, 0, 1, 1, 1, 2), -1),
+                       ((16, 1e4, 3, 1, 1, 1, 2), -1), ((16, 1e4, 1, 0.5, 1, 1, 2), -1), ((16, 1e4, 2, math.nan, 1, 1, 2), -1), ((16, 1e4, 2, 2.0, 0.0, 1, 2), -1), ((16, 1e4, 2, 2.0, 1, 2, 2), -1),
+                       ((16, 1e4, 2, 2.0, 1, -1, 2), -1)):
+        assert lib.fira_rotary_frequencies(*args, f, scale) == want
+    assert lib.fira_rotary_frequencies(16, 1e4, 0, 1, 1, 1, 2, None, scale) == -1
+    assert lib.fira_rotary_frequencies(16, 1e4, 1, 2.0, 0, 0, 0, f, None) == 0 and abs(f[0] - 0.5) < 1e-15
