@@ -345,7 +345,7 @@ FIRA_API fira_status fira_embed_gradient(const fira_embed_desc* d, const void* d
 
 /* FIRA_LAYER_NORM: mu = mean x, rstd = (mean (x - mu)^2 + eps)^(-1/2), y = weight (x - mu) rstd + bias, per row.
  * FIRA_RMS_NORM: the same with mu = 0. */
-typedef enum { FIRA_LAYER_NORM = 0, FIRA_RMS_NORM = 1 } fira_layer_norm_kind;
+typedef enum { FIRA_LAYER_NORM = 0, FIRA_RMS_NORM = 1, FIRA_NO_NORM = 2 /* fira_block_norm only */ } fira_layer_norm_kind;
 typedef struct {
   int64_t rows, dim;
   int32_t dtype;           /* fira_dtype of x, y and their gradients */
@@ -481,6 +481,45 @@ FIRA_API fira_status fira_rotary_gradient(const fira_rotary_desc* d, const fira_
 typedef enum { FIRA_ROTARY_PLAIN = 0, FIRA_ROTARY_LINEAR = 1, FIRA_ROTARY_BY_PARTS = 2 } fira_rotary_context;
 FIRA_API fira_status fira_rotary_frequencies(int64_t rotated, double base, int32_t context, double factor, double trained, double low, double high,
                                              double* host_frequencies, double* scale);
+
+/* ---- Between two blocks of a model ----
+ * The result b of a block goes through its own norm, its gate and its scale to the residual stream x, whose norm is the next block's input:
+ *     u = post norm of b (b itself with FIRA_NO_NORM),  r = residual_scale x + block_scale gate u,  y = norm of r (nothing with FIRA_NO_NORM)
+ * per row, norms as in fira_layer_norm.  y and its statistics are those of r before it is rounded; r and y are rounded once. */
+typedef struct {
+  int64_t rows, dim;
+  int32_t dtype;           /* fira_dtype of x, b, r, y and their gradients */
+  int32_t param_dtype;     /* fira_dtype of the vectors below and their gradients */
+  int32_t norm, post;      /* fira_layer_norm_kind */
+  double eps, post_eps;    /* >= 0 */
+  double residual_scale, block_scale;   /* finite, as fp32 */
+} fira_block_norm_desc;
+/* dim values each on the device, NULL for ones (gate, weights) and zeros (biases).  Those of a FIRA_NO_NORM are not looked at. */
+typedef struct {
+  const void *gate, *weight, *bias, *post_weight, *post_bias;
+} fira_block_norm_params;
+typedef struct {
+  void *gate, *weight, *bias, *post_weight, *post_bias;
+} fira_block_norm_gradients;
+
+/* dev_residual: r.  dev_mean, dev_rstd (of r) and dev_post_mean, dev_post_rstd (of b): fp32, `rows` values each, for the backward pass; any may be NULL, and
+ * what a kind does not have is not written.  dev_residual may be NULL as well, and dev_y has to be NULL with norm FIRA_NO_NORM. */
+FIRA_API fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, int64_t ld_x, const void* dev_block, int64_t ld_block,
+                                     const fira_block_norm_params* params, void* dev_residual, int64_t ld_residual, void* dev_y, int64_t ld_y, float* dev_mean,
+                                     float* dev_rstd, float* dev_post_mean, float* dev_post_rstd, void* hip_stream);
+
+/* dev_dresidual: gradient of r from what uses it besides the norm, NULL for none; dev_dy: gradient of y, NULL with norm FIRA_NO_NORM.  dev_residual (r as it was rounded; for a norm),
+ * dev_block and the statistics are the forward pass's.  With t the gradient of r from both, h = (r - mu) rstd, and h' = (b - mu') rstd' (b without a post norm):
+ *     dx = residual_scale t,  dblock = gradient of the post norm from block_scale gate t,  weight: sum over rows of dy h,  bias: of dy,
+ *     gate: of block_scale t u,  post_weight: of block_scale gate t h',  post_bias: of block_scale gate t
+ * dev_dx, dev_dblock and any of `gradients` (or all: NULL) may be NULL.  accumulate != 0 adds the vectors' gradients to what their buffers hold. */
+FIRA_API size_t fira_block_norm_gradient_workspace_bytes(const fira_block_norm_desc* d);
+FIRA_API fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* dev_dresidual, int64_t ld_dresidual, const void* dev_dy, int64_t ld_dy,
+                                              const void* dev_residual, int64_t ld_residual, const void* dev_block, int64_t ld_block,
+                                              const fira_block_norm_params* params, const float* dev_mean, const float* dev_rstd, const float* dev_post_mean,
+                                              const float* dev_post_rstd, void* dev_dx, int64_t ld_dx, void* dev_dblock, int64_t ld_dblock,
+                                              const fira_block_norm_gradients* gradients, int accumulate, void* dev_workspace, size_t workspace_bytes,
+                                              void* hip_stream);
 
 FIRA_API const char* fira_last_error(const fira_ctx* ctx);
 

@@ -1,0 +1,181 @@
+// What stands between two blocks on the residual stream: the block's norm, gate and scale, the sum, and the next block's norm; and the gradients.  gfx950 only.
+#pragma once
+#include "fira_layer_norm.h"
+
+enum { kLayer = 0, kRms = 1, kNone = 2 };
+
+struct FiraBlockNorm {
+  long long rows, dim;
+  long long ld_x, ld_b, ld_r, ld_y;       // x: in the gradient that of r from elsewhere; y: in the gradient that of y
+  long long ld_dx, ld_db;
+  float eps, post_eps, alpha, beta;       // alpha: of the block, beta: of the residual
+  int norm, post;
+};
+template <typename P>
+struct FiraBlockVectors {
+  const typename P::raw *gate, *w, *b, *pw, *pb;
+};
+struct FiraBlockStats {
+  float *mean, *rstd, *post_mean, *post_rstd;
+};
+
+// Sum over a workgroup of 1024.
+__device__ __forceinline__ float wide_sum(float x, float* part) { return block_sum(x, part); }
+
+// A workgroup for a row, which it reads again for every sum.
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void fira_block_norm_wide_kernel(FiraBlockNorm n, const typename T::raw* x, const typename T::raw* b, FiraBlockVectors<P> v, typename T::raw* r,
+                                                                    typename T::raw* y, FiraBlockStats to) {
+  __shared__ float part[16];
+  const float dim = (float)n.dim;
+  for (long long row = blockIdx.x; row < n.rows; row += gridDim.x) {
+    const typename T::raw *const xr = x + row * n.ld_x, *const br = b + row * n.ld_b;
+    auto total = [&](auto f) {
+      float s = 0.0f;
+      for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) s += f(c);
+      return wide_sum(s, part);
+    };
+    // mean and 1 / deviation of f
+    auto stats = [&](int kind, float eps, auto f, float& mu, float& rs) {
+      mu = kind == kLayer ? total(f) / dim : 0.0f;
+      rs = 1.0f / sqrtf(total([&](long long c) { const float d = f(c) - mu; return d * d; }) / dim + eps);
+    };
+    float pm = 0.0f, ps = 1.0f, mu = 0.0f, rs = 1.0f;
+    if (n.post != kNone) stats(n.post, n.post_eps, [&](long long c) { return load1<T>(br + c); }, pm, ps);
+    auto residual = [&](long long c) {
+      float u = load1<T>(br + c);
+      if (n.post != kNone) {
+        u = (u - pm) * ps;
+        if (v.pw) u *= load1<P>(v.pw + c);
+        if (v.pb) u += load1<P>(v.pb + c);
+      }
+      if (v.gate) u *= load1<P>(v.gate + c);
+      return n.beta * load1<T>(xr + c) + n.alpha * u;
+    };
+    if (n.norm != kNone) stats(n.norm, n.eps, residual, mu, rs);
+    for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) {
+      const float s = residual(c);
+      if (r) store1<T>(r + row * n.ld_r + c, s);
+      if (y) {
+        float o = (s - mu) * rs;
+        if (v.w) o *= load1<P>(v.w + c);
+        if (v.b) o += load1<P>(v.b + c);
+        store1<T>(y + row * n.ld_y + c, o);
+      }
+    }
+    if (threadIdx.x == 0) {
+      if (to.mean && n.norm == kLayer) *as_global(to.mean + row) = mu;
+      if (to.rstd && n.norm != kNone) *as_global(to.rstd + row) = rs;
+      if (to.post_mean && n.post == kLayer) *as_global(to.post_mean + row) = pm;
+      if (to.post_rstd && n.post != kNone) *as_global(to.post_rstd + row) = ps;
+    }
+  }
+}
+
+// What the gradient's kernels read of a row's values.
+template <typename T, typename P>
+struct BlockRow {
+  const typename T::raw *dr, *dy, *r, *b;
+  float mu, rs, pm, ps;
+  __device__ __forceinline__ BlockRow(const FiraBlockNorm& n, const typename T::raw* dr0, const typename T::raw* dy0, const typename T::raw* r0, const typename T::raw* b0,
+                                      const FiraBlockStats& s, long long row) {
+    dr = dr0 ? dr0 + row * n.ld_x : nullptr;
+    dy = n.norm != kNone ? dy0 + row * n.ld_y : nullptr;
+    r = n.norm != kNone ? r0 + row * n.ld_r : nullptr;
+    b = b0 ? b0 + row * n.ld_b : nullptr;
+    mu = n.norm == kLayer ? *as_global(s.mean + row) : 0.0f;
+    rs = n.norm != kNone ? *as_global(s.rstd + row) : 1.0f;
+    pm = n.post == kLayer ? *as_global(s.post_mean + row) : 0.0f;
+    ps = n.post != kNone ? *as_global(s.post_rstd + row) : 1.0f;
+  }
+  __device__ __forceinline__ float h(long long c) const { return (load1<T>(r + c) - mu) * rs; }
+  __device__ __forceinline__ float g(const FiraBlockVectors<P>& v, long long c) const { return load1<T>(dy + c) * (v.w ? load1<P>(v.w + c) : 1.0f); }
+  // the gradient of r; s1, s2: the means of g and g h
+  __device__ __forceinline__ float t(const FiraBlockVectors<P>& v, float s1, float s2, long long c) const {
+    const float from = dr ? load1<T>(dr + c) : 0.0f;
+    return dy ? from + rs * (g(v, c) - s1 - h(c) * s2) : from;
+  }
+  __device__ __forceinline__ float hb(long long c) const { return b ? (load1<T>(b + c) - pm) * ps : 0.0f; }
+};
+
+// t = dr + rstd (g - mean g - h mean(g h)), g = w dy;  dx = beta t;  q = alpha gate t pw,  db = rstd' (q - mean q - h' mean(q h')).  A workgroup for a row; means: of g and g h of every row,
+// for the sums over rows.
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void fira_block_norm_wide_rows_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
+                                                                         const typename T::raw* b, FiraBlockVectors<P> v, FiraBlockStats stats, typename T::raw* dx,
+                                                                         typename T::raw* db, float* means) {
+  __shared__ float part[16];
+  const float dim = (float)n.dim;
+  for (long long row = blockIdx.x; row < n.rows; row += gridDim.x) {
+    const BlockRow<T, P> at(n, dr, dy, r, b, stats, row);
+    auto total = [&](auto f) {
+      float s = 0.0f;
+      for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) s += f(c);
+      return wide_sum(s, part);
+    };
+    const float s1 = n.norm == kLayer ? total([&](long long c) { return at.g(v, c); }) / dim : 0.0f;
+    const float s2 = n.norm != kNone ? total([&](long long c) { return at.g(v, c) * at.h(c); }) / dim : 0.0f;
+    if (threadIdx.x == 0) { *as_global(means + 2 * row) = s1; *as_global(means + 2 * row + 1) = s2; }
+    auto q = [&](long long c) {
+      float x = n.alpha * at.t(v, s1, s2, c);
+      if (v.gate) x *= load1<P>(v.gate + c);
+      if (n.post != kNone && v.pw) x *= load1<P>(v.pw + c);
+      return x;
+    };
+    const float q1 = db && n.post == kLayer ? total(q) / dim : 0.0f;
+    const float q2 = db && n.post != kNone ? total([&](long long c) { return q(c) * at.hb(c); }) / dim : 0.0f;
+    for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) {
+      if (dx) store1<T>(dx + row * n.ld_dx + c, n.beta * at.t(v, s1, s2, c));
+      if (db) store1<T>(db + row * n.ld_db + c, n.post == kNone ? q(c) : at.ps * (q(c) - q1 - at.hb(c) * q2));
+    }
+  }
+}
+
+// Sums over rows, gridDim.y-th part of them: partial[k][blockIdx.y][dim] of dy h, dy, t h' and t.
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void fira_block_norm_wide_sums_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
+                                                                        const typename T::raw* b, FiraBlockVectors<P> v, FiraBlockStats stats, const float* means, float* partial) {
+  const long long c = blockIdx.x * 256LL + threadIdx.x;
+  if (c >= n.dim) return;
+  float s[4] = {};
+  for (long long row = blockIdx.y; row < n.rows; row += gridDim.y) {
+    const BlockRow<T, P> at(n, dr, dy, r, b, stats, row);
+    if (n.norm != kNone) {
+      const float d = load1<T>(at.dy + c);
+      s[0] += d * at.h(c);
+      s[1] += d;
+    }
+    const float t = at.t(v, *as_global(means + 2 * row), *as_global(means + 2 * row + 1), c);
+    s[2] += t * at.hb(c);
+    s[3] += t;
+  }
+  for (int k = 0; k < 4; ++k) *as_global(partial + ((long long)k * gridDim.y + blockIdx.y) * n.dim + c) = s[k];
+}
+
+// The vectors' gradients from the sums S0 .. S3 over all rows: weight S0, bias S1, gate alpha (pw S2 + pb S3), post weight alpha gate S2, post bias alpha gate S3.
+template <typename P>
+struct FiraBlockGradients {
+  typename P::raw *gate, *w, *b, *pw, *pb;
+};
+template <typename P>
+__device__ __forceinline__ void block_vector_gradients(const FiraBlockNorm& n, const FiraBlockVectors<P>& v, const FiraBlockGradients<P>& to, const float (&s)[4], long long c,
+                                                       int accumulate) {
+  const float gate = v.gate ? load1<P>(v.gate + c) : 1.0f, pw = n.post != kNone && v.pw ? load1<P>(v.pw + c) : 1.0f, pb = n.post != kNone && v.pb ? load1<P>(v.pb + c) : 0.0f;
+  auto put = [&](typename P::raw* p, float x) {
+    if (p) store1<P>(p + c, accumulate ? load1<P>(p + c) + x : x);
+  };
+  put(to.w, s[0]);
+  put(to.b, s[1]);
+  put(to.gate, n.alpha * (pw * s[2] + pb * s[3]));
+  put(to.pw, n.alpha * (gate * s[2]));
+  put(to.pb, n.alpha * (gate * s[3]));
+}
+template <typename P>
+__global__ __launch_bounds__(256) void fira_block_norm_join_kernel(FiraBlockNorm n, const float* partial, int parts, FiraBlockVectors<P> v, FiraBlockGradients<P> to, int accumulate) {
+  const long long c = blockIdx.x * 256LL + threadIdx.x;
+  if (c >= n.dim) return;
+  float s[4] = {};
+  for (int k = 0; k < 4; ++k)
+    for (int p = 0; p < parts; ++p) s[k] += *as_global(partial + ((long long)k * parts + p) * n.dim + c);
+  block_vector_gradients(n, v, to, s, c, accumulate);
+}

@@ -3,6 +3,7 @@
 #include "fira_host.h"
 #include "fira_adamw.h"
 #include "fira_rotary.h"
+#include "fira_block_norm.h"
 
 namespace {
 
@@ -90,6 +91,40 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
   return launched("rotary positions");
 }
 
+bool kind_known(int32_t k) { return k == FIRA_LAYER_NORM || k == FIRA_RMS_NORM || k == FIRA_NO_NORM; }
+static_assert(FIRA_LAYER_NORM == (int)kLayer && FIRA_RMS_NORM == (int)kRms && FIRA_NO_NORM == (int)kNone, "kinds");
+
+fira_status check_block(const fira_block_norm_desc* d, const fira_block_norm_params* p) {
+  if (!d) return refuse(FIRA_ERR_INVALID_ARG, "null descriptor");
+  if (d->rows < 0 || d->rows > kMost || d->dim < 1 || d->dim > kMostDim) return refuse(FIRA_ERR_SHAPE, "block norm of %lld rows of %lld", (long long)d->rows, (long long)d->dim);
+  if (!known(d->dtype) || !known(d->param_dtype)) return refuse(FIRA_ERR_DTYPE, "block norm types %d and %d", d->dtype, d->param_dtype);
+  if (!kind_known(d->norm) || !kind_known(d->post)) return refuse(FIRA_ERR_INVALID_ARG, "norm kinds %d and %d", d->norm, d->post);
+  if (!(d->eps >= 0.0) || !std::isfinite((float)d->eps) || !(d->post_eps >= 0.0) || !std::isfinite((float)d->post_eps))
+    return refuse(FIRA_ERR_INVALID_ARG, "an eps is negative or not finite");
+  if (!std::isfinite((float)d->residual_scale) || !std::isfinite((float)d->block_scale)) return refuse(FIRA_ERR_INVALID_ARG, "a scale is not finite");
+  if (p) {
+    const size_t to = size_of(d->param_dtype);
+    if (!aligned(p->gate, to) || !aligned(p->weight, to) || !aligned(p->bias, to) || !aligned(p->post_weight, to) || !aligned(p->post_bias, to))
+      return refuse(FIRA_ERR_INVALID_ARG, "a vector is not aligned to its elements");
+  }
+  return FIRA_OK;
+}
+
+template <typename P>
+FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_block_norm_params* p) {
+  FiraBlockVectors<P> v{};
+  typedef const typename P::raw* at;
+  if (!p) return v;
+  v.gate = (at)p->gate;
+  if (d->norm != FIRA_NO_NORM) { v.w = (at)p->weight; v.b = (at)p->bias; }
+  if (d->post != FIRA_NO_NORM) { v.pw = (at)p->post_weight; v.pb = (at)p->post_bias; }
+  return v;
+}
+
+// Sums of the gradient's workgroups, and the workspace: the sums, then two means of every row.
+int64_t block_parts(const fira_block_norm_desc* d) { return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64)); }
+size_t block_sums_bytes(const fira_block_norm_desc* d) { return up256(4 * block_parts(d) * d->dim * 4); }
+
 }  // namespace
 
 extern "C" {
@@ -160,6 +195,117 @@ fira_status fira_rotary_frequencies(int64_t rotated, double base, int32_t contex
   }
   if (scale) *scale = context == FIRA_ROTARY_BY_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
   return FIRA_OK;
+}
+
+fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, int64_t ld_x, const void* dev_block, int64_t ld_block, const fira_block_norm_params* params,
+                            void* dev_residual, int64_t ld_residual, void* dev_y, int64_t ld_y, float* dev_mean, float* dev_rstd, float* dev_post_mean, float* dev_post_rstd,
+                            void* hip_stream) {
+  if (const fira_status st = check_block(d, params)) return st;
+  if (!d->rows) return FIRA_OK;
+  const size_t size = size_of(d->dtype);
+  FIRA_LEADING(ld_x, d->dim, d->rows);
+  FIRA_LEADING(ld_block, d->dim, d->rows);
+  FIRA_POINTER(dev_x, size);
+  FIRA_POINTER(dev_block, size);
+  if (dev_residual) {
+    FIRA_LEADING(ld_residual, d->dim, d->rows);
+    FIRA_POINTER(dev_residual, size);
+  }
+  if (d->norm == FIRA_NO_NORM && dev_y) return refuse(FIRA_ERR_INVALID_ARG, "y without a norm");
+  if (d->norm != FIRA_NO_NORM) {
+    FIRA_LEADING(ld_y, d->dim, d->rows);
+    FIRA_POINTER(dev_y, size);
+  }
+  if ((dev_residual && (dev_residual == dev_x || dev_residual == dev_block || dev_residual == dev_y)) || (dev_y && (dev_y == dev_x || dev_y == dev_block)))
+    return refuse(FIRA_ERR_INVALID_ARG, "a result is an input, or the other result");
+  if (!aligned(dev_mean, 4) || !aligned(dev_rstd, 4) || !aligned(dev_post_mean, 4) || !aligned(dev_post_rstd, 4)) return refuse(FIRA_ERR_INVALID_ARG, "statistics are not aligned to their elements");
+  const FiraBlockNorm n{d->rows, d->dim, ld_x, ld_block, ld_residual, ld_y, 0, 0, (float)d->eps, (float)d->post_eps, (float)d->block_scale, (float)d->residual_scale, d->norm, d->post};
+  const FiraBlockStats to{dev_mean, dev_rstd, dev_post_mean, dev_post_rstd};
+  with_types(d->dtype, d->param_dtype, [&](auto t, auto p) {
+    typedef decltype(t) T;
+    typedef decltype(p) P;
+    typedef typename T::raw raw;
+    hipLaunchKernelGGL((fira_block_norm_wide_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, (hipStream_t)hip_stream, n, (const raw*)dev_x, (const raw*)dev_block,
+                       block_vectors<P>(d, params), (raw*)dev_residual, (raw*)dev_y, to);
+  });
+  return launched("block norm");
+}
+
+size_t fira_block_norm_gradient_workspace_bytes(const fira_block_norm_desc* d) {
+  if (check_block(d, nullptr)) return 0;
+  return std::max<size_t>(2 * FIRA_UNUSED_WORKSPACE_BYTES, block_sums_bytes(d) + up256(8 * d->rows));
+}
+
+fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* dev_dresidual, int64_t ld_dresidual, const void* dev_dy, int64_t ld_dy, const void* dev_residual,
+                                     int64_t ld_residual, const void* dev_block, int64_t ld_block, const fira_block_norm_params* params, const float* dev_mean, const float* dev_rstd,
+                                     const float* dev_post_mean, const float* dev_post_rstd, void* dev_dx, int64_t ld_dx, void* dev_dblock, int64_t ld_dblock,
+                                     const fira_block_norm_gradients* gradients, int accumulate, void* dev_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const fira_status st = check_block(d, params)) return st;
+  const size_t size = size_of(d->dtype), psize = size_of(d->param_dtype);
+  const fira_block_norm_gradients none{}, &g = gradients ? *gradients : none;
+  if (!aligned(g.gate, psize) || !aligned(g.weight, psize) || !aligned(g.bias, psize) || !aligned(g.post_weight, psize) || !aligned(g.post_bias, psize))
+    return refuse(FIRA_ERR_INVALID_ARG, "a vector's gradient is not aligned to its elements");
+  if (d->norm == FIRA_NO_NORM && (g.weight || g.bias || dev_dy)) return refuse(FIRA_ERR_INVALID_ARG, "gradients of a norm that is not there");
+  if (d->post == FIRA_NO_NORM && (g.post_weight || g.post_bias)) return refuse(FIRA_ERR_INVALID_ARG, "gradients of a post norm that is not there");
+  // (the block's values: for the post norm's gradient, the gate's and the post weight's)
+  const bool block = (d->post != FIRA_NO_NORM && dev_dblock) || g.gate || g.post_weight, sums = g.gate || g.weight || g.bias || g.post_weight || g.post_bias;
+  if (d->rows) {
+    if (dev_dresidual) {
+      FIRA_LEADING(ld_dresidual, d->dim, d->rows);
+      FIRA_POINTER(dev_dresidual, size);
+    }
+    if (d->norm != FIRA_NO_NORM) {
+      FIRA_LEADING(ld_dy, d->dim, d->rows);
+      FIRA_LEADING(ld_residual, d->dim, d->rows);
+      FIRA_POINTER(dev_dy, size);
+      FIRA_POINTER(dev_residual, size);
+      FIRA_POINTER(dev_rstd, 4);
+      if (d->norm == FIRA_LAYER_NORM) FIRA_POINTER(dev_mean, 4);
+    }
+    if (block) {
+      FIRA_LEADING(ld_block, d->dim, d->rows);
+      FIRA_POINTER(dev_block, size);
+    }
+    if (d->post != FIRA_NO_NORM) {
+      FIRA_POINTER(dev_post_rstd, 4);
+      if (d->post == FIRA_LAYER_NORM) FIRA_POINTER(dev_post_mean, 4);
+    }
+    if (dev_dx) {
+      FIRA_LEADING(ld_dx, d->dim, d->rows);
+      FIRA_POINTER(dev_dx, size);
+    }
+    if (dev_dblock) {
+      FIRA_LEADING(ld_dblock, d->dim, d->rows);
+      FIRA_POINTER(dev_dblock, size);
+    }
+    if (dev_dx && dev_dx == dev_dblock) return refuse(FIRA_ERR_INVALID_ARG, "one buffer for two results");
+    for (const void* in : {dev_dresidual, dev_dy, dev_residual, dev_block})
+      if (in && (in == dev_dx || in == dev_dblock)) return refuse(FIRA_ERR_INVALID_ARG, "a result is an input");
+  }
+  if (const fira_status st = check_workspace(dev_workspace, workspace_bytes, fira_block_norm_gradient_workspace_bytes(d))) return st;
+  if ((!sums && (!d->rows || (!dev_dx && !dev_dblock))) || (!d->rows && accumulate)) return FIRA_OK;
+  const FiraBlockNorm n{d->rows, d->dim, ld_dresidual, ld_block, ld_residual, ld_dy, ld_dx, ld_dblock, (float)d->eps, (float)d->post_eps, (float)d->block_scale, (float)d->residual_scale,
+                        d->norm, d->post};
+  const FiraBlockStats stats{(float*)dev_mean, (float*)dev_rstd, (float*)dev_post_mean, (float*)dev_post_rstd};   // (read only)
+  with_types(d->dtype, d->param_dtype, [&](auto t, auto p) {
+    typedef decltype(t) T;
+    typedef decltype(p) P;
+    typedef typename T::raw raw;
+    typedef typename P::raw praw;
+    const FiraBlockVectors<P> v = block_vectors<P>(d, params);
+    const FiraBlockGradients<P> to{(praw*)g.gate, (praw*)g.weight, (praw*)g.bias, (praw*)g.post_weight, (praw*)g.post_bias};
+    const raw *const dr = (const raw*)dev_dresidual, *const dy = (const raw*)dev_dy, *const r = (const raw*)dev_residual, *const b = block ? (const raw*)dev_block : nullptr;
+    const hipStream_t q = (hipStream_t)hip_stream;
+    const int parts = (int)block_parts(d);
+    float* const partial = (float*)dev_workspace;
+    float* const means = (float*)((char*)dev_workspace + block_sums_bytes(d));
+    if (d->rows) hipLaunchKernelGGL((fira_block_norm_wide_rows_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dr, dy, r, b, v, stats, (raw*)dev_dx, (raw*)dev_dblock, means);
+    if (sums) {
+      hipLaunchKernelGGL((fira_block_norm_wide_sums_kernel<T, P>), dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dr, dy, r, b, v, stats, (const float*)means, partial);
+      hipLaunchKernelGGL(fira_block_norm_join_kernel<P>, dim3((d->dim + 255) / 256), dim3(256), 0, q, n, (const float*)partial, parts, v, to, accumulate);
+    }
+  });
+  return launched("block norm gradient");
 }
 
 }  // extern "C"

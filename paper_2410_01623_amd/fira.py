@@ -48,6 +48,7 @@ EXPORTS = (
     "fira_gradient_workspace_bytes", "fira_gradient_norm", "fira_clip_gradients",
     "fira_adamw_scales", "fira_adamw_step",
     "fira_rotary", "fira_rotary_gradient", "fira_rotary_frequencies",
+    "fira_block_norm", "fira_block_norm_gradient_workspace_bytes", "fira_block_norm_gradient",
 )
 
 
@@ -96,6 +97,16 @@ class fira_rotary_desc(ctypes.Structure):
 
 class fira_rotary_heads(ctypes.Structure):
     _fields_ = [("dev_x", ctypes.c_void_p), ("dev_y", ctypes.c_void_p), ("heads", ctypes.c_int64), ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3)]
+
+
+class fira_block_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("eps", ctypes.c_double), ("post_eps", ctypes.c_double), ("residual_scale", ctypes.c_double), ("block_scale", ctypes.c_double)]
+
+
+class fira_block_norm_params(ctypes.Structure):
+    """Also the layout of fira_block_norm_gradients."""
+    _fields_ = [("gate", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p)]
 
 
 class FiraError(RuntimeError):
@@ -208,6 +219,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         call.argtypes = [rotary, heads, ci, vp, vp, vp]
     lib.fira_rotary_frequencies.restype = ci
     lib.fira_rotary_frequencies.argtypes = [c64, cd, ctypes.c_int32, cd, cd, cd, cd, ctypes.POINTER(cd), ctypes.POINTER(cd)]
+    between, vectors = ctypes.POINTER(fira_block_norm_desc), ctypes.POINTER(fira_block_norm_params)
+    lib.fira_block_norm.restype = ci
+    lib.fira_block_norm.argtypes = [between, vp, c64, vp, c64, vectors, vp, c64, vp, c64, vp, vp, vp, vp, vp]
+    lib.fira_block_norm_gradient_workspace_bytes.restype = cz
+    lib.fira_block_norm_gradient_workspace_bytes.argtypes = [between]
+    lib.fira_block_norm_gradient.restype = ci
+    lib.fira_block_norm_gradient.argtypes = [between, vp, c64, vp, c64, vp, c64, vp, c64, vectors, vp, vp, vp, vp, vp, c64, vp, c64, vectors, ci, vp, cz, vp]
     if path is None:
         _lib = lib
     return lib

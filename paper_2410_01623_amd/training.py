@@ -1,6 +1,6 @@
 """The operators around the optimizer step, by the names of their C entry points (include/fira.h): embedding lookup, layer norm
 and root-mean-square norm, each with its gradient, the norm and clipping of a list of gradients, AdamW over a list
-of tensors, and rotary positions.
+of tensors, rotary positions, and the block norm (what stands between two blocks on the residual stream) with its gradient.
 
 As in `fira`, this is argument marshalling: tensors become pointers, sizes and leading dimensions, everything is computed by
 libfira.so, and there is no fallback.  All tensors are on one GPU, bf16 or fp32.  `stream` is the torch stream to enqueue on (default: the
@@ -17,7 +17,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -288,6 +288,137 @@ def fira_layer_norm_gradient(dy: torch.Tensor, x: torch.Tensor, weight: Optional
                                         None if rms else mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), ld_dx, _vector(dweight, dim, "dweight"),
                                         _vector(dbias, dim, "dbias"), bool(accumulate), workspace.data_ptr(), workspace.numel(), _stream(dev)))
     return dx, dweight, dbias
+
+
+class BlockNorm(NamedTuple):
+    """What fira_block_norm gives: the stream after the block, its norm, and both norms' statistics (None where there is no such)."""
+    residual: torch.Tensor
+    y: Optional[torch.Tensor]
+    mean: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+    post_mean: Optional[torch.Tensor]
+    post_rstd: Optional[torch.Tensor]
+
+
+class BlockNormGradients(NamedTuple):
+    """What fira_block_norm_gradient gives; None for vectors that are not there."""
+    dx: torch.Tensor
+    dblock: torch.Tensor
+    dweight: Optional[torch.Tensor]
+    dbias: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dpost_weight: Optional[torch.Tensor]
+    dpost_bias: Optional[torch.Tensor]
+
+
+def _block_desc(x, block, vectors, norm, post, eps, post_eps, residual_scale, block_scale):
+    """Checks what both calls have in common -> (descriptor, pointers of the vectors); vectors: gate, weight, bias, post_weight, post_bias."""
+    if block.shape != x.shape:
+        _refuse(FIRA_ERR_SHAPE, f"the block is {tuple(block.shape)} for a stream of {tuple(x.shape)}")
+    dt = _dtype(x.dtype, "stream")
+    if block.dtype != x.dtype:
+        _refuse(FIRA_ERR_DTYPE, "the block is not of the stream's type")
+    if norm == fira.FIRA_NO_NORM and (vectors[1] is not None or vectors[2] is not None):
+        _refuse(FIRA_ERR_INVALID_ARG, "weight or bias without a norm")
+    if post == fira.FIRA_NO_NORM and (vectors[3] is not None or vectors[4] is not None):
+        _refuse(FIRA_ERR_INVALID_ARG, "post_weight or post_bias without a post norm")
+    dim = x.shape[-1]
+    at = fira.fira_block_norm_params(*(_vector(t, dim, name) for t, name in zip(vectors, ("gate", "weight", "bias", "post_weight", "post_bias"))))
+    rows = x.numel() // dim if dim else 0
+    return fira.fira_block_norm_desc(rows, dim, dt, _param_dtype(dt, *vectors), norm, post, eps, post_eps, residual_scale, block_scale), at
+
+
+def fira_block_norm(x: torch.Tensor, block: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+                    post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, norm: int = fira.FIRA_RMS_NORM, post: int = fira.FIRA_NO_NORM,
+                    eps: float = 1e-5, post_eps: Optional[float] = None, residual_scale: float = 1.0, block_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                    y_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> BlockNorm:
+    """The stream after a block, r = residual_scale x + block_scale gate post_norm(block), and the next block's norm of it, over the last dimension.
+    norm and post: FIRA_LAYER_NORM, FIRA_RMS_NORM or FIRA_NO_NORM; without a norm, y is None, without a post norm the block goes as it is.
+    The vectors, of one type, default to ones (gate, weights) and zeros (biases).  out and y_out take r and y.  post_eps defaults to eps."""
+    lib = fira.load_library()
+    if x.dim() < 1:
+        _refuse(FIRA_ERR_SHAPE, "x has no dimension")
+    vectors = (gate, weight, bias, post_weight, post_bias)
+    dev = _device(x, block, *vectors, out, y_out)
+    d, at = _block_desc(x, block, vectors, norm, post, eps, eps if post_eps is None else post_eps, residual_scale, block_scale)
+    if norm == fira.FIRA_NO_NORM and y_out is not None:
+        _refuse(FIRA_ERR_INVALID_ARG, "y_out without a norm")
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_block_norm(x, block, weight, bias, gate=gate, post_weight=post_weight, post_bias=post_bias, norm=norm, post=post, eps=eps, post_eps=post_eps,
+                                   residual_scale=residual_scale, block_scale=block_scale, out=out, y_out=y_out)
+    x, ld_x = _input(x)
+    block, ld_block = _input(block)
+    out, ld_r = _result(out, x.shape, x.dtype, dev, "out", like=x)
+    y, ld_y = (None, 0) if norm == fira.FIRA_NO_NORM else _result(y_out, x.shape, x.dtype, dev, "y_out", like=x)
+    stat = lambda wanted: torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if wanted else None  # noqa: E731
+    stats = [stat(wanted) for kind in (norm, post) for wanted in (kind == fira.FIRA_LAYER_NORM, kind != fira.FIRA_NO_NORM)]
+    _check(lib.fira_block_norm(d, x.data_ptr(), ld_x, block.data_ptr(), ld_block, at, out.data_ptr(), ld_r, None if y is None else y.data_ptr(), ld_y,
+                               *(None if s is None else s.data_ptr() for s in stats), _stream(dev)))
+    return BlockNorm(out, y, *stats)
+
+
+def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[torch.Tensor], residual: torch.Tensor, block: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                             mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+                             post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, post_mean: Optional[torch.Tensor] = None,
+                             post_rstd: Optional[torch.Tensor] = None, bias: bool = False, norm: int = fira.FIRA_RMS_NORM, post: int = fira.FIRA_NO_NORM,
+                             residual_scale: float = 1.0, block_scale: float = 1.0, dx: Optional[torch.Tensor] = None, dblock: Optional[torch.Tensor] = None,
+                             dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                             dpost_weight: Optional[torch.Tensor] = None, dpost_bias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                             workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> BlockNormGradients:
+    """Gradients of fira_block_norm from those of its residual (None: nothing else uses it) and y (None without a norm).  residual and the statistics are
+    what it gave, the vectors and scales what it was given.  The gradients of the vectors that are there, and with `bias` the norm's, have the vectors' type (bias alone:
+    dbias's, default the stream's); accumulate adds them to what those given hold."""
+    lib = fira.load_library()
+    if residual.dim() < 1:
+        _refuse(FIRA_ERR_SHAPE, "residual has no dimension")
+    vectors = (gate, weight, None, post_weight, post_bias)
+    dev = _device(residual, block, dresidual, dy, *vectors, mean, rstd, post_mean, post_rstd, dx, dblock, dweight, dbias, dgate, dpost_weight, dpost_bias)
+    d, at = _block_desc(residual, block, vectors, norm, post, 0.0, 0.0, residual_scale, block_scale)
+    for t, name in ((dresidual, "dresidual"), (dy, "dy")):
+        if t is not None and (t.shape != residual.shape or t.dtype != residual.dtype):
+            _refuse(FIRA_ERR_SHAPE, f"{name} is {tuple(t.shape)} of {t.dtype} for a stream of {tuple(residual.shape)} of {residual.dtype}")
+    if (dy is None) != (norm == fira.FIRA_NO_NORM):
+        _refuse(FIRA_ERR_INVALID_ARG, "dy without a norm, or a norm without dy")
+    if bias and norm == fira.FIRA_NO_NORM:
+        _refuse(FIRA_ERR_INVALID_ARG, "bias without a norm")
+    for kind, m, r, name in ((norm, mean, rstd, ""), (post, post_mean, post_rstd, "post_")):
+        for t, wanted, what in ((m, kind == fira.FIRA_LAYER_NORM, "mean"), (r, kind != fira.FIRA_NO_NORM, "rstd")):
+            if wanted and (t is None or t.dtype != torch.float32 or t.shape != residual.shape[:-1] or not t.is_contiguous()):
+                _refuse(FIRA_ERR_SHAPE, f"{name}{what} is not a dense fp32 tensor of {tuple(residual.shape[:-1])}")
+    wanted = (gate is not None, weight is not None, bias, post_weight is not None, post_bias is not None)
+    given = (dgate, dweight, dbias, dpost_weight, dpost_bias)
+    ptype = next((t.dtype for t in vectors if t is not None), None) or (dbias.dtype if dbias is not None else residual.dtype)
+    d.param_dtype = _dtype(ptype, "parameter")
+    for w, t, name in zip(wanted, given, ("dgate", "dweight", "dbias", "dpost_weight", "dpost_bias")):
+        if t is not None and not w:
+            _refuse(FIRA_ERR_INVALID_ARG, f"{name} of a vector that is not there")
+        if accumulate and w and t is None:
+            _refuse(FIRA_ERR_INVALID_ARG, f"accumulate without {name}")
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return fira_block_norm_gradient(dresidual, dy, residual, block, weight, mean, rstd, gate=gate, post_weight=post_weight, post_bias=post_bias, post_mean=post_mean,
+                                            post_rstd=post_rstd, bias=bias, norm=norm, post=post, residual_scale=residual_scale, block_scale=block_scale, dx=dx, dblock=dblock,
+                                            dweight=dweight, dbias=dbias, dgate=dgate, dpost_weight=dpost_weight, dpost_bias=dpost_bias, accumulate=accumulate,
+                                            workspace=workspace)
+    residual, ld_r = _input(residual)
+    block, ld_b = _input(block)
+    dresidual, ld_dr = (None, 0) if dresidual is None else _input(dresidual)
+    dy, ld_dy = (None, 0) if dy is None else _input(dy)
+    dx, ld_dx = _result(dx, residual.shape, residual.dtype, dev, "dx", like=residual)
+    dblock, ld_db = _result(dblock, residual.shape, residual.dtype, dev, "dblock", like=residual)
+    dim = residual.shape[-1]
+    grads = [_result(t, (dim,), ptype, dev, "a vector's gradient")[0] if w else None for w, t in zip(wanted, given)]
+    to = fira.fira_block_norm_params(*(_vector(t, dim, "a vector's gradient") for t in grads))
+    workspace = _workspace(workspace, lib.fira_block_norm_gradient_workspace_bytes(d), dev)
+    pointer = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    stats = (mean if norm == fira.FIRA_LAYER_NORM else None, rstd, post_mean if post == fira.FIRA_LAYER_NORM else None, post_rstd)
+    _check(lib.fira_block_norm_gradient(d, pointer(dresidual), ld_dr, pointer(dy), ld_dy, residual.data_ptr(), ld_r, block.data_ptr(), ld_b, at, *map(pointer, stats),
+                                        dx.data_ptr(), ld_dx, dblock.data_ptr(), ld_db, to, bool(accumulate), workspace.data_ptr(), workspace.numel(), _stream(dev)))
+    dgate, dweight, dbias, dpost_weight, dpost_bias = grads
+    return BlockNormGradients(dx, dblock, dweight, dbias, dgate, dpost_weight, dpost_bias)
 
 
 def fira_rotary_frequencies(rotated: int, base: float = 10000.0, *, context: int = fira.FIRA_ROTARY_PLAIN, factor: float = 1.0, trained: float = 4096.0,

@@ -83,3 +83,36 @@ def test_rotary_frequencies(lib):
         assert lib.fira_rotary_frequencies(*args, f, scale) == want
     assert lib.fira_rotary_frequencies(16, 1e4, 0, 1, 1, 1, 2, None, scale) == -1
     assert lib.fira_rotary_frequencies(16, 1e4, 1, 2.0, 0, 0, 0, f, None) == 0 and abs(f[0] - 0.5) < 1e-15
+
+
+def test_block_norm(lib):
+    desc = lambda rows=4, dim=8, dtype=0, param_dtype=1, norm=0, post=1, eps=1e-5, post_eps=1e-5, beta=1.0, alpha=1.0: fira.fira_block_norm_desc(  # noqa: E731
+        rows, dim, dtype, param_dtype, norm, post, eps, post_eps, beta, alpha)
+    Q = [ctypes.c_void_p(4096 * k) for k in range(2, 8)]
+    none, odd = fira.fira_block_norm_params(), fira.fira_block_norm_params(gate=4097)
+    some = fira.fira_block_norm_params(gate=4096)
+    BIG = 1 << 40
+
+    def forward(d=desc(), x=P, ld=8, b=P, lb=8, v=none, r=Q[0], lr=8, y=Q[1], ly=8, stats=(P, P, P, P)):
+        return lib.fira_block_norm(d, x, ld, b, lb, v, r, lr, y, ly, *stats, N)
+
+    def backward(d=desc(), dr=P, ldr=8, dy=P, ly=8, r=P, lr=8, b=P, lb=8, v=none, stats=(P, P, P, P), dx=Q[0], lx=8, db=Q[1], ldb=8, g=none, add=0, ws=P, size=BIG):
+        return lib.fira_block_norm_gradient(d, dr, ldr, dy, ly, r, lr, b, lb, v, *stats, dx, lx, db, ldb, g, add, ws, size, N)
+
+    for d, want in ((None, -1), (desc(rows=-1), -2), (desc(rows=1 << 31), -2), (desc(dim=0), -2), (desc(dim=1 << 31), -2), (desc(dtype=2), -4), (desc(param_dtype=-1), -4), (desc(norm=3), -1),
+                    (desc(post=-1), -1), (desc(eps=-1.0), -1), (desc(post_eps=math.inf), -1), (desc(beta=math.nan), -1), (desc(alpha=1e60), -1)):
+        assert forward(d) == want and backward(d) == want and lib.fira_block_norm_gradient_workspace_bytes(d) == 0
+    for kw, want in ((dict(x=N), -1), (dict(b=N), -1), (dict(x=ODD), -1), (dict(ld=7), -2), (dict(lb=7), -2), (dict(lr=7), -2), (dict(ly=7), -2), (dict(y=N), -1), (dict(r=P), -1), (dict(y=P), -1),
+                     (dict(y=Q[0]), -1), (dict(v=odd), -1), (dict(stats=(ODD, P, P, P)), -1), (dict(d=desc(norm=2)), -1)):
+        assert forward(**kw) == want, kw
+        assert len(lib.fira_last_error(None)) > 0
+    for kw, want in ((dict(dr=ODD), -1), (dict(ldr=7), -2), (dict(dy=N), -1), (dict(ly=7), -2), (dict(r=N), -1), (dict(lr=7), -2), (dict(b=N), -1), (dict(lb=7), -2), (dict(v=odd), -1), (dict(g=odd), -1),
+                     (dict(stats=(N, P, P, P)), -1), (dict(stats=(P, N, P, P)), -1), (dict(stats=(P, P, P, N)), -1), (dict(d=desc(post=0), stats=(P, P, N, P)), -1), (dict(lx=7), -2),
+                     (dict(ldb=7), -2), (dict(dx=ODD), -1), (dict(dx=P), -1), (dict(db=P), -1), (dict(dx=Q[1]), -1), (dict(d=desc(norm=2)), -1),
+                     (dict(d=desc(norm=2), dy=N, g=fira.fira_block_norm_params(weight=4096)), -1), (dict(d=desc(post=2), g=fira.fira_block_norm_params(post_bias=4096)), -1),
+                     (dict(ws=N), -5), (dict(size=lib.fira_block_norm_gradient_workspace_bytes(desc()) - 1), -5), (dict(ws=ctypes.c_void_p(4096 + 128)), -5)):
+        assert backward(**kw) == want, kw
+    assert forward(desc(rows=0), N, 0, N, 0, none, N, 0, N, 0, (N,) * 4) == 0
+    assert backward(desc(rows=0), N, 0, N, 0, N, 0, N, 0, none, (N,) * 4, N, 0, N, 0, none, 0) == 0
+    assert backward(desc(rows=0), N, 0, N, 0, N, 0, N, 0, none, (N,) * 4, N, 0, N, 0, some, 1) == 0      # nothing to add
+    assert backward(dx=N, db=N) == 0                       # nothing asked for
