@@ -4,19 +4,36 @@
 
 constexpr int kAdamBlock = 256;       // values that share a scale
 
-struct FiraAdamTensor {
-  void* w;
+// A piece of a tensor: n values, of the tensor's rows one after the other, from a whole block on.
+struct FiraAdamSpan {
+  void* w;                 // where the row of the first value begins, or with cols == 0 (no gaps) the value itself
   const void* g;
   void *m, *v;
   float *m_scale, *v_scale;
-  long long n, cols, ld_w, ld_g;
+  long long ld_w, ld_g;
   double weight_decay;
-  unsigned seed;
+  unsigned n, cols, col0;  // col0: the first value's column
+  unsigned first, seed;    // first: its place in the tensor, modulo 2^32
+  int tile0;               // first tile of this piece
 };
+constexpr int kAdamSpans = 40;        // a launch's pieces travel as kernel arguments, of which there are 4 KB
+constexpr int kAdamUnroll = 2;        // vectors of a thread that are on their way together
+constexpr int kAdamWorkgroups = 2048;
+struct FiraAdamSpans {
+  FiraAdamSpan s[kAdamSpans];
+  int count, tiles;
+  int each;                // tiles of a workgroup
+  int last;                // the call's last launch: counts the step
+};
+// Values of a thread's vector and of a tile: 16 bytes of the widest type that is streamed.
+template <typename T, typename R, bool EIGHT>
+constexpr int kAdamWidth = EIGHT ? kWidth<T, R> : 4;
+
 struct FiraAdamHp {
   double lr, log_beta1, log_beta2, max_norm;
   float b1, b2, omb1, omb2, eps;
 };
+static_assert(sizeof(FiraAdamSpans) + sizeof(FiraAdamHp) + 64 <= 4096, "kernel arguments");
 
 // What a step multiplies by: 1 / (1 - b1^t) and the learning rate, 1 / sqrt(1 - b2^t), the factor that cuts the gradients, and t.
 struct FiraAdamFactors {
@@ -76,49 +93,210 @@ __device__ __forceinline__ void adam_update(const FiraAdamHp& hp, const FiraAdam
   w = w * decay - (m * f.m) / (root * f.v + hp.eps);
 }
 
-// A workgroup for 256 values at a time, a value to a thread.
-template <typename T, typename R, bool EIGHT>
-__global__ __launch_bounds__(kAdamBlock) void fira_adamw_kernel(FiraAdamTensor a, FiraAdamHp hp, const float* lr, const float* norm, const long long* taken) {
-  __shared__ float most[2][4];
-  const FiraAdamFactors f = adam_factors(hp, lr, norm, *as_global(taken));
-  const float decay = (float)(1.0 - f.lr * a.weight_decay);
-  const unsigned key = adam_mix(adam_mix(a.seed) + f.t);
-  for (long long b = blockIdx.x; b * kAdamBlock < a.n; b += gridDim.x) {
-    const long long i = b * kAdamBlock + threadIdx.x;
-    const bool here = i < a.n;
-    const long long row = here ? i / a.cols : 0, col = here ? i - row * a.cols : 0;
-    typename T::raw* const to = (typename T::raw*)a.w + row * a.ld_w + col;
-    float w = 0.0f, m = 0.0f, v = 0.0f, root = 0.0f;
-    if (here) {
-      w = load1<T>(to);
-      if (EIGHT) {
-        m = adam_value(*as_global((const unsigned char*)a.m + i)) * *as_global(a.m_scale + b);
-        root = adam_value(*as_global((const unsigned char*)a.v + i)) * *as_global(a.v_scale + b);
-        v = root * root;
-      } else {
-        m = *as_global((const float*)a.m + i);
-        v = *as_global((const float*)a.v + i);
+// W values of type T in their stored form, one by one.
+template <typename T, int W>
+__device__ __forceinline__ void adam_set(Raw<T, W>& x, int k, typename T::raw value) {
+  if constexpr (sizeof(typename T::raw) == 4) x.a[k / 4][k % 4] = value;
+  else x.a[0][k / 2] = k & 1 ? (x.a[0][k / 2] & 0xffffu) | (unsigned)value << 16 : (x.a[0][k / 2] & 0xffff0000u) | value;
+}
+
+// Largest over the lanes that share a block.
+template <int LANES>
+__device__ __forceinline__ float adam_most(float x) {
+#pragma unroll
+  for (int d = LANES / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+  return x;
+}
+
+// A thread's values on their way: weights and gradients as they are stored, and the states, which have no gaps.
+template <typename T, typename R, bool EIGHT, int W>
+struct AdamVector {
+  Raw<T, W> w;
+  Raw<R, W> g;
+  unsigned m8[W / 4], v8[W / 4];
+  f32x4 m, v;
+  float ms, vs;
+  unsigned j, row, col;    // place in the piece; row counted from the piece's first
+  int here;                // values of the vector inside the piece
+  bool whole;              // all W there, and neighbours
+
+  __device__ __forceinline__ void load(const FiraAdamSpan& s, unsigned at) {
+    j = at;
+    here = j < s.n ? (int)min((unsigned)W, s.n - j) : 0;
+    row = 0;
+    col = j;
+    if (s.cols) {
+      const unsigned c = s.col0 + j;
+      row = c / s.cols;
+      col = c - row * s.cols;
+    }
+    whole = here == W && (!s.cols || s.cols - col >= W);
+    const typename T::raw* const pw = (const typename T::raw*)s.w + row * s.ld_w + col;
+    const typename R::raw* const pg = (const typename R::raw*)s.g + row * s.ld_g + col;
+    if (whole) {
+      w.stream(pw);
+      g.stream(pg);
+    } else if (here) {
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        long long ow = k, og = k;
+        if (k < here && s.cols) {
+          const unsigned down = (col + k) / s.cols;
+          ow += down * (s.ld_w - s.cols);
+          og += down * (s.ld_g - s.cols);
+        }
+        adam_set<T, W>(w, k, k < here ? *as_global(pw + ow) : (typename T::raw)0);
+        adam_set<R, W>(g, k, k < here ? *as_global(pg + og) : (typename R::raw)0);
       }
-      adam_update(hp, f, decay, load1<R>((const typename R::raw*)a.g + row * a.ld_g + col), w, m, v, root);
-      store1<T>(to, w);
     }
-    if (!EIGHT) {
-      if (here) { *as_global((float*)a.m + i) = m; *as_global((float*)a.v + i) = v; }
-      continue;
+    if constexpr (EIGHT) {
+      typedef unsigned __attribute__((aligned(1))) u32_a1;
+      const unsigned char *const pm = (const unsigned char*)s.m + j, *const pv = (const unsigned char*)s.v + j;
+      if (here == W) {
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) {
+          m8[k] = __builtin_nontemporal_load((gptr<const u32_a1>)as_global(pm + 4 * k));
+          v8[k] = __builtin_nontemporal_load((gptr<const u32_a1>)as_global(pv + 4 * k));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) m8[k] = v8[k] = 0;
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          if (k < here) {
+            m8[k / 4] |= (unsigned)*as_global(pm + k) << 8 * (k % 4);
+            v8[k / 4] |= (unsigned)*as_global(pv + k) << 8 * (k % 4);
+          }
+      }
+      ms = here ? *as_global(s.m_scale + j / kAdamBlock) : 0.0f;
+      vs = here ? *as_global(s.v_scale + j / kAdamBlock) : 0.0f;
+    } else {
+      const float *const pm = (const float*)s.m + j, *const pv = (const float*)s.v + j;
+      if (here == W) {
+        m = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global(pm));
+        v = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global(pv));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          m[k] = k < here ? *as_global(pm + k) : 0.0f;
+          v[k] = k < here ? *as_global(pv + k) : 0.0f;
+        }
+      }
     }
-    float mm = adam_size(m), mv = adam_size(root);
-    for (int d = 32; d; d >>= 1) { mm = fmaxf(mm, __shfl_xor(mm, d, 64)); mv = fmaxf(mv, __shfl_xor(mv, d, 64)); }
-    if ((threadIdx.x & 63) == 0) { most[0][threadIdx.x >> 6] = mm; most[1][threadIdx.x >> 6] = mv; }
-    __syncthreads();
-    mm = fmaxf(fmaxf(most[0][0], most[0][1]), fmaxf(most[0][2], most[0][3]));
-    mv = fmaxf(fmaxf(most[1][0], most[1][1]), fmaxf(most[1][2], most[1][3]));
-    __syncthreads();
-    if (here) {
-      const unsigned random = adam_mix((unsigned)i + key);
-      *as_global((unsigned char*)a.m + i) = (unsigned char)adam_code<false>(m, adam_up(mm), random & 0xffffu);
-      *as_global((unsigned char*)a.v + i) = (unsigned char)adam_code<true>(root, adam_up(mv), random >> 16);
+  }
+
+  __device__ __forceinline__ void step(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, unsigned key) {
+    float ow[W], om[W], ov[W], root[W];
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      ow[k] = w.get(k);
+      if constexpr (EIGHT) {
+        // (an immediate picks the byte)
+        const float held[2] = {byte_value(m8[k / 4], k % 4), byte_value(v8[k / 4], k % 4)};
+        om[k] = held[0] * ms;
+        root[k] = held[1] * vs;
+        ov[k] = root[k] * root[k];
+      } else {
+        om[k] = m[k];
+        ov[k] = v[k];
+      }
+      adam_update(hp, f, decay, g.get(k), ow[k], om[k], ov[k], root[k]);
     }
-    if (threadIdx.x == 0) { *as_global(a.m_scale + b) = adam_scale(mm); *as_global(a.v_scale + b) = adam_scale(mv); }
+    typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
+    if (whole) {
+      store_w<T, W, true>(pw, ow);
+    } else {
+#pragma unroll
+      for (int k = 0; k < W; ++k)
+        if (k < here) store1<T>(pw + k + (s.cols ? (col + k) / s.cols * (s.ld_w - s.cols) : 0), ow[k]);
+    }
+    if constexpr (EIGHT) {
+      constexpr int LANES = kAdamBlock / W;
+      float mm = 0.0f, mv = 0.0f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        mm = fmaxf(mm, k < here ? adam_size(om[k]) : 0.0f);
+        mv = fmaxf(mv, k < here ? adam_size(root[k]) : 0.0f);
+      }
+      mm = adam_most<LANES>(mm);
+      mv = adam_most<LANES>(mv);
+      const float up_m = adam_up(mm), up_v = adam_up(mv);
+      unsigned cm[W / 4] = {}, cv[W / 4] = {};
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const unsigned random = adam_mix(s.first + j + k + key);
+        cm[k / 4] |= adam_code<false>(om[k], up_m, random & 0xffffu) << 8 * (k % 4);
+        cv[k / 4] |= adam_code<true>(root[k], up_v, random >> 16) << 8 * (k % 4);
+      }
+      unsigned char *const pm = (unsigned char*)s.m + j, *const pv = (unsigned char*)s.v + j;
+      if (here == W) {
+        typedef unsigned __attribute__((aligned(1))) u32_a1;
+#pragma unroll
+        for (int k = 0; k < W / 4; ++k) {
+          __builtin_nontemporal_store(cm[k], (gptr<u32_a1>)as_global(pm + 4 * k));
+          __builtin_nontemporal_store(cv[k], (gptr<u32_a1>)as_global(pv + 4 * k));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          if (k < here) {
+            *as_global(pm + k) = (unsigned char)(cm[k / 4] >> 8 * (k % 4));
+            *as_global(pv + k) = (unsigned char)(cv[k / 4] >> 8 * (k % 4));
+          }
+      }
+      if (here && j % kAdamBlock == 0) {
+        *as_global(s.m_scale + j / kAdamBlock) = adam_scale(mm);
+        *as_global(s.v_scale + j / kAdamBlock) = adam_scale(mv);
+      }
+    } else {
+      float *const pm = (float*)s.m + j, *const pv = (float*)s.v + j;
+      if (here == W) {
+        store_w<FiraStoredF32, W, true>(pm, om);
+        store_w<FiraStoredF32, W, true>(pv, ov);
+      } else {
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          if (k < here) { *as_global(pm + k) = om[k]; *as_global(pv + k) = ov[k]; }
+      }
+    }
+  }
+
+  static __device__ __forceinline__ float byte_value(unsigned codes, int k) {
+    switch (k) {
+      case 0: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 0);
+      case 1: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 1);
+      case 2: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 2);
+      default: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 3);
+    }
+  }
+};
+
+// A workgroup takes tiles that adjoin, of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
+template <typename T, typename R, bool EIGHT>
+__global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {
+  constexpr int W = kAdamWidth<T, R, EIGHT>, TILE = 256 * W * kAdamUnroll;
+  __shared__ FiraAdamFactors shared;
+  if (threadIdx.x == 0) shared = adam_factors(hp, lr, norm, *as_global(counter));
+  __syncthreads();
+  const FiraAdamFactors f = shared;
+  const int from = blockIdx.x * l.each, until = min(from + l.each, l.tiles);
+  int k = 0;                                             // the last piece that does not begin after the first tile
+#pragma unroll 1
+  for (int step = 32; step; step >>= 1)
+    if (k + step < l.count && l.s[k + step].tile0 <= from) k += step;
+#pragma unroll 1
+  for (int tile = from; tile < until; ++tile) {
+    while (k + 1 < l.count && l.s[k + 1].tile0 <= tile) ++k;
+    k = __builtin_amdgcn_readfirstlane(k);
+    const FiraAdamSpan& s = l.s[k];
+    const unsigned first = (unsigned)(tile - s.tile0) * TILE;
+    AdamVector<T, R, EIGHT, W> x[kAdamUnroll];
+#pragma unroll
+    for (int u = 0; u < kAdamUnroll; ++u) x[u].load(s, first + (u * 256 + threadIdx.x) * W);
+    const float decay = (float)(1.0 - f.lr * s.weight_decay);
+    const unsigned key = adam_mix(adam_mix(s.seed) + f.t);
+#pragma unroll
+    for (int u = 0; u < kAdamUnroll; ++u) x[u].step(s, hp, f, decay, key);
   }
 }
 

@@ -28,6 +28,51 @@ fira_status check_adamw_hparams(const fira_adamw_hparams* hp, bool norm) {
   return FIRA_OK;
 }
 
+// Cuts a tensor into pieces that the kernel takes: from a whole block on, up to 2^30 values.
+constexpr int64_t kAdamPiece = 1 << 30;
+template <typename F>
+void cut_adamw(const fira_adamw_desc& d, void* w, const void* g, const fira_adamw_state& s, F piece) {
+  const int64_t n = d.rows * d.cols;
+  const bool dense = d.rows == 1 || (d.ld_w == d.cols && d.ld_g == d.cols);
+  const bool eight = d.state_type == FIRA_STATE_E4M3;
+  for (int64_t i = 0; i < n; i += kAdamPiece) {
+    const int64_t row = dense ? 0 : i / d.cols, col = dense ? 0 : i % d.cols, b = i / kAdamBlock;
+    const int64_t at_w = dense ? i : row * d.ld_w, at_g = dense ? i : row * d.ld_g;
+    piece(FiraAdamSpan{(char*)w + at_w * size_of(d.dtype), (const char*)g + at_g * size_of(d.grad_dtype), (char*)s.m + i * (eight ? 1 : 4), (char*)s.v + i * (eight ? 1 : 4),
+                       eight ? s.m_scale + b : nullptr, eight ? s.v_scale + b : nullptr, d.ld_w, d.ld_g, d.weight_decay, (unsigned)std::min(kAdamPiece, n - i),
+                       dense ? 0u : (unsigned)d.cols, (unsigned)col, (unsigned)i, d.seed, 0});
+  }
+}
+
+// Calls f(types, states in 8 bits, pieces) for every launch that the list takes, types by types.
+template <typename F>
+void for_each_adamw_launch(const fira_adamw_desc* d, int count, void* const* W, const void* const* G, const fira_adamw_state* state, F f) {
+  for (int kind = 0; kind < 8; ++kind) {
+    const int in = kind & 1, grad = kind >> 1 & 1, eight = kind >> 2;
+    with_types(in, grad, [&](auto t, auto r) {
+      with_flag(eight, [&](auto e) {
+        constexpr int64_t tile = 256 * kAdamUnroll * kAdamWidth<decltype(t), decltype(r), decltype(e)::value>;
+        FiraAdamSpans l{};
+        auto flush = [&] {
+          l.each = (l.tiles + kAdamWorkgroups - 1) / kAdamWorkgroups;
+          if (l.count) f(t, r, e, (const FiraAdamSpans&)l);
+          l.count = l.tiles = 0;
+        };
+        for (int i = 0; i < count; ++i) {
+          if (d[i].dtype != in || d[i].grad_dtype != grad || (d[i].state_type == FIRA_STATE_E4M3) != (eight != 0)) continue;
+          cut_adamw(d[i], W[i], G[i], state[i], [&](FiraAdamSpan s) {
+            s.tile0 = l.tiles;
+            l.s[l.count++] = s;
+            l.tiles += (int)((s.n + tile - 1) / tile);     // (2^30 values are 2^20 tiles at most)
+            if (l.count == kAdamSpans) flush();
+          });
+        }
+        flush();
+      });
+    });
+  }
+}
+
 // Whether the elements of a result are apart: strides in the order of their size, each at least what those before it span.  span: of all.
 bool strides_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t dim, bool result, int64_t* span) {
   int order[3] = {0, 1, 2};
@@ -154,18 +199,10 @@ fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adam
   const hipStream_t q = (hipStream_t)hip_stream;
   const FiraAdamHp h{hp->lr, std::log(hp->beta1), std::log(hp->beta2), hp->max_norm, (float)hp->beta1, (float)hp->beta2, (float)(1.0 - hp->beta1), (float)(1.0 - hp->beta2),
                      (float)hp->eps};
-  for (int i = 0; i < count; ++i) {
-    const int64_t n = d[i].rows * d[i].cols;
-    if (!n) continue;
-    const fira_adamw_state& s = dev_state[i];
-    const FiraAdamTensor a{dev_W[i], dev_G[i], s.m, s.v, s.m_scale, s.v_scale, n, d[i].cols, d[i].ld_w, d[i].ld_g, d[i].weight_decay, d[i].seed};
-    with_types(d[i].dtype, d[i].grad_dtype, [&](auto t, auto r) {
-      with_flag(d[i].state_type == FIRA_STATE_E4M3, [&](auto eight) {
-        hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value>), dim3(std::min<int64_t>((n + kAdamBlock - 1) / kAdamBlock, 1 << 20)),
-                           dim3(kAdamBlock), 0, q, a, h, dev_lr, dev_norm, (const long long*)dev_t);
-      });
-    });
-  }
+  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, const FiraAdamSpans& l) {
+    hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value>), dim3((l.tiles + l.each - 1) / l.each), dim3(256), 0, q, l, h, dev_lr, dev_norm,
+                       (long long*)dev_t);
+  });
   hipLaunchKernelGGL(fira_adamw_count_kernel<>, dim3(1), dim3(1), 0, q, (long long*)dev_t);
   return launched("AdamW step");
 }
