@@ -66,31 +66,13 @@ __host__ __device__ __forceinline__ unsigned adam_mix(unsigned x) {
   return x ^ x >> 16;
 }
 
-// The e4m3 code of x (times `up` in [0, 448], but for what is not finite: NaN), rounded up where `random` says so: it is added below the three bits of
-// mantissa that are kept, after which the rest is cut off.  Subnormal codes have the steps of the lowest normal ones, [2^-6, 2^-5), and are counted there.
-// FLOOR: what is above zero stays so.
-template <bool FLOOR>
-__device__ __forceinline__ unsigned adam_code(float x, float up, unsigned random) {
-  const float a = fminf(fabsf(x) * up, 448.0f);
-  const bool below = a < 0x1p-6f;
-  unsigned code = ((__float_as_uint(below ? a + 0x1p-6f : a) + (random << 4) + 8u) >> 20) - (below ? 968u : 960u);
-  if (FLOOR) code = a > 0.0f ? max(code, 1u) : code;
-  code |= __float_as_uint(x) >> 31 << 7;
-  return fabsf(x) < INFINITY ? code : 127u;
-}
-__device__ __forceinline__ float adam_value(unsigned code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
-__device__ __forceinline__ float adam_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
-__device__ __forceinline__ float adam_up(float most) { return most < 0x1p-100f ? 0.0f : 448.0f / most; }
-__device__ __forceinline__ float adam_scale(float most) { return most < 0x1p-100f ? 0.0f : most / 448.0f; }
-
-// New moments and weight of one value; root = sqrt(v).  Each product and sum is rounded by itself, so that the moments are what elementary operations in fp32 give.
-__device__ __forceinline__ void adam_update(const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, float g, float& w, float& m, float& v, float& root) {
+// New moments and weight of one value with states in fp32.  Each product and sum is rounded by itself, so that the moments are what elementary operations give.
+__device__ __forceinline__ void adam_update(const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, float g, float& w, float& m, float& v) {
 #pragma clang fp contract(off)
   g *= f.cut;
   m = m * hp.b1 + g * hp.omb1;
   v = v * hp.b2 + g * g * hp.omb2;
-  root = sqrtf(v);
-  w = w * decay - (m * f.m) / (root * f.v + hp.eps);
+  w = w * decay - (m * f.m) / (sqrtf(v) * f.v + hp.eps);
 }
 
 // W values of type T in their stored form, one by one.
@@ -100,12 +82,62 @@ __device__ __forceinline__ void adam_set(Raw<T, W>& x, int k, typename T::raw va
   else x.a[0][k / 2] = k & 1 ? (x.a[0][k / 2] & 0xffffu) | (unsigned)value << 16 : (x.a[0][k / 2] & 0xffff0000u) | value;
 }
 
-// Largest over the lanes that share a block.
+// Largest over the lanes that share a block, of floats that are not negative, as bits: what is not finite is larger than all that is.
+template <int OFF>
+__device__ __forceinline__ unsigned max_xor(unsigned x) {
+  if constexpr (OFF < 16) {
+    return max(x, __float_as_uint(lane_xor<OFF>(__uint_as_float(x))));
+  } else {
+    const u32x2_s s = OFF == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max((unsigned)s[0], (unsigned)s[1]);
+  }
+}
 template <int LANES>
-__device__ __forceinline__ float adam_most(float x) {
-#pragma unroll
-  for (int d = LANES / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+__device__ __forceinline__ unsigned adam_most(unsigned x) {
+  x = max_xor<1>(max_xor<2>(max_xor<4>(max_xor<8>(max_xor<16>(x)))));
+  if constexpr (LANES == 64) x = max_xor<32>(x);
   return x;
+}
+
+// a / b, correctly rounded but for what leaves fp32's range on the way.
+__device__ __forceinline__ float adam_quotient(float a, float b) {
+  const float r = __builtin_amdgcn_rcpf(b);
+  float q = a * r;
+  q = __builtin_fmaf(__builtin_fmaf(-b, q, a), r, q);
+  return __builtin_amdgcn_div_fixupf(q, b, a);
+}
+
+// The same with states in 8 bits, S times the moment m and root of v (and by S less what they are multiplied with).  The root instruction is off by at most 2 u and has
+// subnormals as zero.
+struct AdamScaled {
+  float cut, fm, fv;
+  __device__ __forceinline__ AdamScaled(const FiraAdamFactors& f, float S) : cut(f.cut * S), fm(f.m / S), fv(f.v / S) {}
+  __device__ __forceinline__ void update(const FiraAdamHp& hp, float decay, float g, float& w, float& m, float& root) const {
+#pragma clang fp contract(off)
+    g *= cut;
+    m = m * hp.b1 + g * hp.omb1;
+    root = __builtin_amdgcn_sqrtf(root * root * hp.b2 + g * g * hp.omb2);
+    w = w * decay - adam_quotient(m * fm, root * fv + hp.eps);
+  }
+};
+
+// Four values' e4m3 codes in an unsigned.  The conversion adds the high 20 bits of `random` below the three bits of mantissa that it keeps and cuts the rest off, in
+// steps of 2^-9 below 2^-6.  (An immediate picks the byte.)
+__device__ __forceinline__ float adam_value(unsigned codes, int k) {
+  switch (k) {
+    case 0: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 0);
+    case 1: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 1);
+    case 2: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 2);
+    default: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 3);
+  }
+}
+__device__ __forceinline__ unsigned adam_put(unsigned codes, float x, unsigned random, int k) {
+  switch (k) {
+    case 0: return (unsigned)__builtin_amdgcn_cvt_sr_fp8_f32(x, (int)random, (int)codes, 0);
+    case 1: return (unsigned)__builtin_amdgcn_cvt_sr_fp8_f32(x, (int)random, (int)codes, 1);
+    case 2: return (unsigned)__builtin_amdgcn_cvt_sr_fp8_f32(x, (int)random, (int)codes, 2);
+    default: return (unsigned)__builtin_amdgcn_cvt_sr_fp8_f32(x, (int)random, (int)codes, 3);
+  }
 }
 
 // A thread's values on their way: weights and gradients as they are stored, and the states, which have no gaps.
@@ -118,7 +150,13 @@ struct AdamVector {
   float ms, vs;
   unsigned j, row, col;    // place in the piece; row counted from the piece's first
   int here;                // values of the vector inside the piece
-  bool whole;              // all W there, and neighbours
+  bool all_whole;          // all W there, and neighbours, in every lane
+
+  static __device__ __forceinline__ void stream_bytes(unsigned (&to)[W / 4], const unsigned char* p) {
+    typedef unsigned __attribute__((aligned(1))) u32_a1;
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) to[k] = __builtin_nontemporal_load((gptr<const u32_a1>)as_global(p + 4 * k));
+  }
 
   __device__ __forceinline__ void load(const FiraAdamSpan& s, unsigned at) {
     j = at;
@@ -130,143 +168,153 @@ struct AdamVector {
       row = c / s.cols;
       col = c - row * s.cols;
     }
-    whole = here == W && (!s.cols || s.cols - col >= W);
+    all_whole = __all(here == W && (!s.cols || s.cols - col >= W));
     const typename T::raw* const pw = (const typename T::raw*)s.w + row * s.ld_w + col;
     const typename R::raw* const pg = (const typename R::raw*)s.g + row * s.ld_g + col;
-    if (whole) {
+    if (all_whole) {
       w.stream(pw);
       g.stream(pg);
-    } else if (here) {
+      if constexpr (EIGHT) {
+        stream_bytes(m8, (const unsigned char*)s.m + j);
+        stream_bytes(v8, (const unsigned char*)s.v + j);
+        ms = *as_global(s.m_scale + j / kAdamBlock);
+        vs = *as_global(s.v_scale + j / kAdamBlock);
+      } else {
+        m = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.m + j));
+        v = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.v + j));
+      }
+      return;
+    }
+    // (value by value, zeros where there are none)
 #pragma unroll
-      for (int k = 0; k < W; ++k) {
-        long long ow = k, og = k;
-        if (k < here && s.cols) {
-          const unsigned down = (col + k) / s.cols;
-          ow += down * (s.ld_w - s.cols);
-          og += down * (s.ld_g - s.cols);
-        }
-        adam_set<T, W>(w, k, k < here ? *as_global(pw + ow) : (typename T::raw)0);
-        adam_set<R, W>(g, k, k < here ? *as_global(pg + og) : (typename R::raw)0);
+    for (int k = 0; k < W; ++k) {
+      const bool is = k < here;
+      const unsigned down = is && s.cols ? (col + k) / s.cols : 0;
+      adam_set<T, W>(w, k, is ? *as_global(pw + k + down * (s.ld_w - s.cols)) : (typename T::raw)0);
+      adam_set<R, W>(g, k, is ? *as_global(pg + k + down * (s.ld_g - s.cols)) : (typename R::raw)0);
+      if constexpr (EIGHT) {
+        if (k % 4 == 0) m8[k / 4] = v8[k / 4] = 0;
+        m8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.m + j + k) : 0u) << 8 * (k % 4);
+        v8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.v + j + k) : 0u) << 8 * (k % 4);
+      } else {
+        m[k] = is ? *as_global((const float*)s.m + j + k) : 0.0f;
+        v[k] = is ? *as_global((const float*)s.v + j + k) : 0.0f;
       }
     }
     if constexpr (EIGHT) {
-      typedef unsigned __attribute__((aligned(1))) u32_a1;
-      const unsigned char *const pm = (const unsigned char*)s.m + j, *const pv = (const unsigned char*)s.v + j;
-      if (here == W) {
-#pragma unroll
-        for (int k = 0; k < W / 4; ++k) {
-          m8[k] = __builtin_nontemporal_load((gptr<const u32_a1>)as_global(pm + 4 * k));
-          v8[k] = __builtin_nontemporal_load((gptr<const u32_a1>)as_global(pv + 4 * k));
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < W / 4; ++k) m8[k] = v8[k] = 0;
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-          if (k < here) {
-            m8[k / 4] |= (unsigned)*as_global(pm + k) << 8 * (k % 4);
-            v8[k / 4] |= (unsigned)*as_global(pv + k) << 8 * (k % 4);
-          }
-      }
       ms = here ? *as_global(s.m_scale + j / kAdamBlock) : 0.0f;
       vs = here ? *as_global(s.v_scale + j / kAdamBlock) : 0.0f;
-    } else {
-      const float *const pm = (const float*)s.m + j, *const pv = (const float*)s.v + j;
-      if (here == W) {
-        m = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global(pm));
-        v = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global(pv));
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          m[k] = k < here ? *as_global(pm + k) : 0.0f;
-          v[k] = k < here ? *as_global(pv + k) : 0.0f;
-        }
-      }
     }
   }
 
-  __device__ __forceinline__ void step(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, unsigned key) {
-    float ow[W], om[W], ov[W], root[W];
+  // Calls f(k, place of value k of the weights) for the values that are there.
+  template <typename F>
+  __device__ __forceinline__ void each(const FiraAdamSpan& s, F f) const {
+    typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+      if (k < here) f(k, pw + k + (s.cols ? (col + k) / s.cols * (s.ld_w - s.cols) : 0));
+  }
+
+  __device__ __forceinline__ void step_f32(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay) {
+    float ow[W], om[W], ov[W];
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       ow[k] = w.get(k);
-      if constexpr (EIGHT) {
-        // (an immediate picks the byte)
-        const float held[2] = {byte_value(m8[k / 4], k % 4), byte_value(v8[k / 4], k % 4)};
-        om[k] = held[0] * ms;
-        root[k] = held[1] * vs;
-        ov[k] = root[k] * root[k];
-      } else {
-        om[k] = m[k];
-        ov[k] = v[k];
-      }
-      adam_update(hp, f, decay, g.get(k), ow[k], om[k], ov[k], root[k]);
+      om[k] = m[k];
+      ov[k] = v[k];
+      adam_update(hp, f, decay, g.get(k), ow[k], om[k], ov[k]);
     }
-    typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
-    if (whole) {
-      store_w<T, W, true>(pw, ow);
+    if (all_whole) {
+      store_w<T, W, true>((typename T::raw*)s.w + row * s.ld_w + col, ow);
+      store_w<FiraStoredF32, W, true>((float*)s.m + j, om);
+      store_w<FiraStoredF32, W, true>((float*)s.v + j, ov);
     } else {
-#pragma unroll
-      for (int k = 0; k < W; ++k)
-        if (k < here) store1<T>(pw + k + (s.cols ? (col + k) / s.cols * (s.ld_w - s.cols) : 0), ow[k]);
-    }
-    if constexpr (EIGHT) {
-      constexpr int LANES = kAdamBlock / W;
-      float mm = 0.0f, mv = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        mm = fmaxf(mm, k < here ? adam_size(om[k]) : 0.0f);
-        mv = fmaxf(mv, k < here ? adam_size(root[k]) : 0.0f);
-      }
-      mm = adam_most<LANES>(mm);
-      mv = adam_most<LANES>(mv);
-      const float up_m = adam_up(mm), up_v = adam_up(mv);
-      unsigned cm[W / 4] = {}, cv[W / 4] = {};
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const unsigned random = adam_mix(s.first + j + k + key);
-        cm[k / 4] |= adam_code<false>(om[k], up_m, random & 0xffffu) << 8 * (k % 4);
-        cv[k / 4] |= adam_code<true>(root[k], up_v, random >> 16) << 8 * (k % 4);
-      }
-      unsigned char *const pm = (unsigned char*)s.m + j, *const pv = (unsigned char*)s.v + j;
-      if (here == W) {
-        typedef unsigned __attribute__((aligned(1))) u32_a1;
-#pragma unroll
-        for (int k = 0; k < W / 4; ++k) {
-          __builtin_nontemporal_store(cm[k], (gptr<u32_a1>)as_global(pm + 4 * k));
-          __builtin_nontemporal_store(cv[k], (gptr<u32_a1>)as_global(pv + 4 * k));
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-          if (k < here) {
-            *as_global(pm + k) = (unsigned char)(cm[k / 4] >> 8 * (k % 4));
-            *as_global(pv + k) = (unsigned char)(cv[k / 4] >> 8 * (k % 4));
-          }
-      }
-      if (here && j % kAdamBlock == 0) {
-        *as_global(s.m_scale + j / kAdamBlock) = adam_scale(mm);
-        *as_global(s.v_scale + j / kAdamBlock) = adam_scale(mv);
-      }
-    } else {
-      float *const pm = (float*)s.m + j, *const pv = (float*)s.v + j;
-      if (here == W) {
-        store_w<FiraStoredF32, W, true>(pm, om);
-        store_w<FiraStoredF32, W, true>(pv, ov);
-      } else {
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-          if (k < here) { *as_global(pm + k) = om[k]; *as_global(pv + k) = ov[k]; }
-      }
+      each(s, [&](int k, typename T::raw* to) {
+        store1<T>(to, ow[k]);
+        *as_global((float*)s.m + j + k) = om[k];
+        *as_global((float*)s.v + j + k) = ov[k];
+      });
     }
   }
 
-  static __device__ __forceinline__ float byte_value(unsigned codes, int k) {
-    switch (k) {
-      case 0: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 0);
-      case 1: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 1);
-      case 2: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 2);
-      default: return __builtin_amdgcn_cvt_f32_fp8((int)codes, 3);
+  // All that is of the gradients' size is held times 2^32, so that small squares stay above what the root instruction has as zero; where a product leaves fp32's range
+  // for that, the value is worked out again without.
+  __device__ __forceinline__ void step_e4m3(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, unsigned key) {
+    constexpr int LANES = kAdamBlock / W;
+    constexpr float kMost = 0x1p120f;
+    float S = 0x1p32f;
+    const AdamScaled scaled(f, S);
+    float ow[W], om[W], root[W];
+    unsigned bm = 0, bv = 0;
+    const float sm = ms * S, sv = vs * S;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      ow[k] = w.get(k);
+      om[k] = adam_value(m8[k / 4], k % 4) * sm;
+      root[k] = adam_value(v8[k / 4], k % 4) * sv;
+      scaled.update(hp, decay, g.get(k), ow[k], om[k], root[k]);
+      bm = max(bm, __float_as_uint(om[k]) & 0x7fffffffu);
+      bv = max(bv, __float_as_uint(root[k]));
+    }
+    bm = adam_most<LANES>(bm);
+    bv = adam_most<LANES>(bv);
+    bool lost_m[W] = {}, lost_v[W] = {};                   // what is not finite
+    if (__any(max(bm, bv) >= __float_as_uint(kMost))) {
+      const AdamScaled plain(f, 1.0f);
+      bm = bv = 0;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const bool fine = fabsf(om[k]) < INFINITY && root[k] < INFINITY;
+        float w1 = w.get(k), m1 = adam_value(m8[k / 4], k % 4) * ms, r1 = adam_value(v8[k / 4], k % 4) * vs;
+        plain.update(hp, decay, g.get(k), w1, m1, r1);
+        ow[k] = fine ? ow[k] : w1;
+        om[k] = fine ? om[k] * (1.0f / S) : m1;
+        root[k] = fine ? root[k] * (1.0f / S) : r1;
+        lost_m[k] = !(fabsf(om[k]) < INFINITY);
+        lost_v[k] = !(root[k] < INFINITY);
+        bm = max(bm, lost_m[k] ? 0u : __float_as_uint(om[k]) & 0x7fffffffu);
+        bv = max(bv, lost_v[k] ? 0u : __float_as_uint(root[k]));
+      }
+      bm = adam_most<LANES>(bm);
+      bv = adam_most<LANES>(bv);
+      S = 1.0f;
+    }
+    const float mm = __uint_as_float(bm), mv = __uint_as_float(bv);
+    const bool none_m = mm < 0x1p-100f * S, none_v = mv < 0x1p-100f * S;
+    // (the reciprocal instruction has results below 2^-126 as zero)
+    const float down_m = mm < kMost ? 1.0f : 0x1p-32f, down_v = mv < kMost ? 1.0f : 0x1p-32f;
+    const float up_m = none_m ? 0.0f : adam_quotient(448.0f, mm * down_m) * down_m, up_v = none_v ? 0.0f : adam_quotient(448.0f, mv * down_v) * down_v;
+    unsigned cm[W / 4] = {}, cv[W / 4] = {};
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const unsigned random = adam_mix(s.first + j + k + key);
+      const float a = __builtin_amdgcn_fmed3f(om[k] * up_m, -448.0f, 448.0f);
+      float b = fminf(root[k] * up_v, 448.0f);
+      b = b > 0.0f ? fmaxf(b, 0x1p-9f) : b;              // the smallest code, which is not rounded down
+      cm[k / 4] = adam_put(cm[k / 4], a, random << 16 | 0x8000u, k % 4);
+      cv[k / 4] = adam_put(cv[k / 4], b, (random & 0xffff0000u) | 0x8000u, k % 4);
+      if (lost_m[k]) cm[k / 4] |= 127u << 8 * (k % 4);
+      if (lost_v[k]) cv[k / 4] |= 127u << 8 * (k % 4);
+    }
+    if (all_whole) {
+      typedef unsigned __attribute__((aligned(1))) u32_a1;
+      store_w<T, W, true>((typename T::raw*)s.w + row * s.ld_w + col, ow);
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) {
+        __builtin_nontemporal_store(cm[k], (gptr<u32_a1>)as_global((unsigned char*)s.m + j + 4 * k));
+        __builtin_nontemporal_store(cv[k], (gptr<u32_a1>)as_global((unsigned char*)s.v + j + 4 * k));
+      }
+    } else {
+      each(s, [&](int k, typename T::raw* to) {
+        store1<T>(to, ow[k]);
+        *as_global((unsigned char*)s.m + j + k) = (unsigned char)(cm[k / 4] >> 8 * (k % 4));
+        *as_global((unsigned char*)s.v + j + k) = (unsigned char)(cv[k / 4] >> 8 * (k % 4));
+      });
+    }
+    if (here && j % kAdamBlock == 0) {
+      *as_global(s.m_scale + j / kAdamBlock) = none_m ? 0.0f : adam_quotient(mm, 448.0f) / S;
+      *as_global(s.v_scale + j / kAdamBlock) = none_v ? 0.0f : adam_quotient(mv, 448.0f) / S;
     }
   }
 };
@@ -296,7 +344,10 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
     const float decay = (float)(1.0 - f.lr * s.weight_decay);
     const unsigned key = adam_mix(adam_mix(s.seed) + f.t);
 #pragma unroll
-    for (int u = 0; u < kAdamUnroll; ++u) x[u].step(s, hp, f, decay, key);
+    for (int u = 0; u < kAdamUnroll; ++u) {
+      if constexpr (EIGHT) x[u].step_e4m3(s, hp, f, decay, key);
+      else x[u].step_f32(s, hp, f, decay);
+    }
   }
 }
 
