@@ -11,18 +11,23 @@ struct FiraAdamSpan {
   void *m, *v;
   float *m_scale, *v_scale;
   long long ld_w, ld_g;
-  double weight_decay;
+  double per_col;          // 1 / cols
+  float weight_decay;
   unsigned n, cols, col0;  // col0: the first value's column
   unsigned first, seed;    // first: its place in the tensor, modulo 2^32
   int tile0;               // first tile of this piece
+  int stream;              // results that begin at whole lines, and go past the caches: 1 weights, 2 states
 };
-constexpr int kAdamSpans = 40;        // a launch's pieces travel as kernel arguments, of which there are 4 KB
-constexpr int kAdamUnroll = 2;        // vectors of a thread that are on their way together
-constexpr int kAdamWorkgroups = 2048;
+constexpr int kAdamSpans = 36;        // a launch's pieces travel as kernel arguments, of which there are 4 KB
+// Vectors of a thread that are on their way together, and workgroups of a launch at most: with states in 8 bits a value has five times the arithmetic a byte.
+// us with one vector and 4096 workgroups, two and 16384: 60m 298 and 269, embeddings in 8 bits 276 and 288, 511 x 1377 and the like in 8 bits with rows apart 60 and 72.
+template <bool EIGHT>
+constexpr int kAdamUnroll = EIGHT ? 1 : 2;
+template <bool EIGHT>
+constexpr int kAdamWorkgroups = EIGHT ? 4096 : 16384;
 struct FiraAdamSpans {
   FiraAdamSpan s[kAdamSpans];
   int count, tiles;
-  int each;                // tiles of a workgroup
   int last;                // the call's last launch: counts the step
 };
 // Values of a thread's vector and of a tile: 16 bytes of the widest type that is streamed.
@@ -75,11 +80,52 @@ __device__ __forceinline__ void adam_update(const FiraAdamHp& hp, const FiraAdam
   w = w * decay - (m * f.m) / (sqrtf(v) * f.v + hp.eps);
 }
 
+enum { kStreamed, kWhole, kEnd, kApart };
+
+// Calls f with whether to stream as a constant, which where rows are apart is known at run time only.  What the compiler finds twice, with and without
+// streaming, it makes one of plain stores: the empty statements keep it from that.
+template <int PLACE, typename F>
+__device__ __forceinline__ void either_way(bool stream, F f) {
+  if (PLACE == kStreamed || (PLACE == kApart && stream)) {
+    asm volatile("" ::: "memory");
+    f(std::true_type{});
+    asm volatile("" ::: "memory");
+  } else {
+    f(std::false_type{});
+  }
+}
+
 // W values of type T in their stored form, one by one.
 template <typename T, int W>
 __device__ __forceinline__ void adam_set(Raw<T, W>& x, int k, typename T::raw value) {
   if constexpr (sizeof(typename T::raw) == 4) x.a[k / 4][k % 4] = value;
   else x.a[0][k / 2] = k & 1 ? (x.a[0][k / 2] & 0xffffu) | (unsigned)value << 16 : (x.a[0][k / 2] & 0xffff0000u) | value;
+}
+
+// Values back .. back + W of a and then b, left in a.
+template <typename T, int W>
+__device__ __forceinline__ void adam_joined(Raw<T, W>& a, const Raw<T, W>& b, int back) {
+  constexpr bool F32 = sizeof(typename T::raw) == 4;
+  constexpr int N = F32 ? W : W / 2;                       // 32-bit words
+  unsigned x[2 * N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (F32) { x[i] = __float_as_uint(a.a[i / 4][i % 4]); x[N + i] = __float_as_uint(b.a[i / 4][i % 4]); }
+    else { x[i] = a.a[0][i]; x[N + i] = b.a[0][i]; }
+  }
+  const int words = F32 ? back : back / 2;                 // 0 to N - 1
+#pragma unroll
+  for (int by = N / 2; by; by /= 2)
+#pragma unroll
+    for (int i = 0; i < 2 * N - by; ++i) x[i] = words & by ? x[i + by] : x[i];
+  if constexpr (!F32)
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = back & 1 ? __builtin_amdgcn_alignbit(x[i + 1], x[i], 16) : x[i];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (F32) a.a[i / 4][i % 4] = __uint_as_float(x[i]);
+    else a.a[0][i] = x[i];
+  }
 }
 
 // Largest over the lanes that share a block, of floats that are not negative, as bits: what is not finite is larger than all that is.
@@ -141,8 +187,11 @@ __device__ __forceinline__ unsigned adam_put(unsigned codes, float x, unsigned r
 }
 
 // A thread's values on their way: weights and gradients as they are stored, and the states, which have no gaps.
-template <typename T, typename R, bool EIGHT, int W>
+// PLACE: whole vectors of a piece without gaps, whose results go past the caches (kStreamed) or not (kWhole); such vectors or a part of one at the piece's end (kEnd); of a piece
+// whose rows are apart (kApart).
+template <typename T, typename R, bool EIGHT, int W, int PLACE>
 struct AdamVector {
+  static constexpr bool APART = PLACE == kApart, FULL = PLACE == kStreamed || PLACE == kWhole;
   Raw<T, W> w;
   Raw<R, W> g;
   unsigned m8[W / 4], v8[W / 4];
@@ -150,7 +199,7 @@ struct AdamVector {
   float ms, vs;
   unsigned j, row, col;    // place in the piece; row counted from the piece's first
   int here;                // values of the vector inside the piece
-  bool all_whole;          // all W there, and neighbours, in every lane
+  bool whole;              // all W there, and neighbours
 
   static __device__ __forceinline__ void stream_bytes(unsigned (&to)[W / 4], const unsigned char* p) {
     typedef unsigned __attribute__((aligned(1))) u32_a1;
@@ -160,50 +209,74 @@ struct AdamVector {
 
   __device__ __forceinline__ void load(const FiraAdamSpan& s, unsigned at) {
     j = at;
-    here = j < s.n ? (int)min((unsigned)W, s.n - j) : 0;
+    here = FULL ? W : j < s.n ? (int)min((unsigned)W, s.n - j) : 0;
     row = 0;
     col = j;
-    if (s.cols) {
+    if constexpr (APART) {
+      // (c + 1/2) / cols is 1 / (2 cols) from a whole number at least, which fp64 keeps apart
       const unsigned c = s.col0 + j;
-      row = c / s.cols;
+      row = (unsigned)(((double)c + 0.5) * s.per_col);
       col = c - row * s.cols;
     }
-    all_whole = __all(here == W && (!s.cols || s.cols - col >= W));
+    whole = here == W && (!APART || s.cols - col >= W);
     const typename T::raw* const pw = (const typename T::raw*)s.w + row * s.ld_w + col;
     const typename R::raw* const pg = (const typename R::raw*)s.g + row * s.ld_g + col;
-    if (all_whole) {
+    auto vectors = [&] {
       w.stream(pw);
       g.stream(pg);
-      if constexpr (EIGHT) {
-        stream_bytes(m8, (const unsigned char*)s.m + j);
-        stream_bytes(v8, (const unsigned char*)s.v + j);
-        ms = *as_global(s.m_scale + j / kAdamBlock);
-        vs = *as_global(s.v_scale + j / kAdamBlock);
-      } else {
-        m = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.m + j));
-        v = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.v + j));
-      }
+      stream_states(s);
+    };
+    if constexpr (FULL) {
+      vectors();
       return;
     }
-    // (value by value, zeros where there are none)
+    if (whole) vectors();
+    if (APART && !whole && here == W && s.cols >= W) {
+      // the end of a row and the beginning of the next
+      const int back = (int)(col + W - s.cols);
+      Raw<T, W> w2;
+      Raw<R, W> g2;
+      w.stream(pw - back);
+      g.stream(pg - back);
+      w2.stream(pw + (s.ld_w - (long long)col));
+      g2.stream(pg + (s.ld_g - (long long)col));
+      stream_states(s);
+      adam_joined<T, W>(w, w2, back);
+      adam_joined<R, W>(g, g2, back);
+    }
+    if (here < W || (APART && !whole && s.cols < W)) {
+      // value by value, zeros where there are none
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const bool is = k < here;
-      const unsigned down = is && s.cols ? (col + k) / s.cols : 0;
-      adam_set<T, W>(w, k, is ? *as_global(pw + k + down * (s.ld_w - s.cols)) : (typename T::raw)0);
-      adam_set<R, W>(g, k, is ? *as_global(pg + k + down * (s.ld_g - s.cols)) : (typename R::raw)0);
+      for (int k = 0; k < W; ++k) {
+        const bool is = k < here;
+        const unsigned down = APART && is ? (col + k) / s.cols : 0u;
+        adam_set<T, W>(w, k, is ? *as_global(pw + k + down * (s.ld_w - s.cols)) : (typename T::raw)0);
+        adam_set<R, W>(g, k, is ? *as_global(pg + k + down * (s.ld_g - s.cols)) : (typename R::raw)0);
+        if constexpr (EIGHT) {
+          if (k % 4 == 0) m8[k / 4] = v8[k / 4] = 0;
+          m8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.m + j + k) : 0u) << 8 * (k % 4);
+          v8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.v + j + k) : 0u) << 8 * (k % 4);
+        } else {
+          m[k] = is ? *as_global((const float*)s.m + j + k) : 0.0f;
+          v[k] = is ? *as_global((const float*)s.v + j + k) : 0.0f;
+        }
+      }
       if constexpr (EIGHT) {
-        if (k % 4 == 0) m8[k / 4] = v8[k / 4] = 0;
-        m8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.m + j + k) : 0u) << 8 * (k % 4);
-        v8[k / 4] |= (is ? (unsigned)*as_global((const unsigned char*)s.v + j + k) : 0u) << 8 * (k % 4);
-      } else {
-        m[k] = is ? *as_global((const float*)s.m + j + k) : 0.0f;
-        v[k] = is ? *as_global((const float*)s.v + j + k) : 0.0f;
+        ms = here ? *as_global(s.m_scale + j / kAdamBlock) : 0.0f;
+        vs = here ? *as_global(s.v_scale + j / kAdamBlock) : 0.0f;
       }
     }
+  }
+
+  __device__ __forceinline__ void stream_states(const FiraAdamSpan& s) {
     if constexpr (EIGHT) {
-      ms = here ? *as_global(s.m_scale + j / kAdamBlock) : 0.0f;
-      vs = here ? *as_global(s.v_scale + j / kAdamBlock) : 0.0f;
+      stream_bytes(m8, (const unsigned char*)s.m + j);
+      stream_bytes(v8, (const unsigned char*)s.v + j);
+      ms = *as_global(s.m_scale + j / kAdamBlock);
+      vs = *as_global(s.v_scale + j / kAdamBlock);
+    } else {
+      m = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.m + j));
+      v = __builtin_nontemporal_load((gptr<const f32x4_a4>)as_global((const float*)s.v + j));
     }
   }
 
@@ -211,9 +284,25 @@ struct AdamVector {
   template <typename F>
   __device__ __forceinline__ void each(const FiraAdamSpan& s, F f) const {
     typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
+    const bool one = s.cols >= W;                          // (no second end of a row then)
 #pragma unroll
     for (int k = 0; k < W; ++k)
-      if (k < here) f(k, pw + k + (s.cols ? (col + k) / s.cols * (s.ld_w - s.cols) : 0));
+      if (k < here) f(k, pw + k + (!APART ? 0u : one ? (unsigned)(col + k >= s.cols) : (col + k) / s.cols) * (s.ld_w - s.cols));
+  }
+
+  __device__ __forceinline__ void put_weights(const FiraAdamSpan& s, const float (&x)[W]) const {
+    typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
+    either_way<PLACE>(s.stream & 1, [&](auto stream) { store_w<T, W, decltype(stream)::value>(pw, x); });
+  }
+  static __device__ __forceinline__ void put_bytes(unsigned char* p, const unsigned (&x)[W / 4], bool stream) {
+    typedef unsigned __attribute__((aligned(1))) u32_a1;
+    either_way<PLACE>(stream, [&](auto past) {
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) {
+        if constexpr (decltype(past)::value) __builtin_nontemporal_store(x[k], (gptr<u32_a1>)as_global(p + 4 * k));
+        else *(gptr<u32_a1>)as_global(p + 4 * k) = x[k];
+      }
+    });
   }
 
   __device__ __forceinline__ void step_f32(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay) {
@@ -225,10 +314,15 @@ struct AdamVector {
       ov[k] = v[k];
       adam_update(hp, f, decay, g.get(k), ow[k], om[k], ov[k]);
     }
-    if (all_whole) {
-      store_w<T, W, true>((typename T::raw*)s.w + row * s.ld_w + col, ow);
-      store_w<FiraStoredF32, W, true>((float*)s.m + j, om);
-      store_w<FiraStoredF32, W, true>((float*)s.v + j, ov);
+    auto vectors = [&] {
+      put_weights(s, ow);
+      either_way<PLACE>(s.stream & 2, [&](auto stream) {
+        store_w<FiraStoredF32, W, decltype(stream)::value>((float*)s.m + j, om);
+        store_w<FiraStoredF32, W, decltype(stream)::value>((float*)s.v + j, ov);
+      });
+    };
+    if (FULL || whole) {
+      vectors();
     } else {
       each(s, [&](int k, typename T::raw* to) {
         store1<T>(to, ow[k]);
@@ -297,14 +391,13 @@ struct AdamVector {
       if (lost_m[k]) cm[k / 4] |= 127u << 8 * (k % 4);
       if (lost_v[k]) cv[k / 4] |= 127u << 8 * (k % 4);
     }
-    if (all_whole) {
-      typedef unsigned __attribute__((aligned(1))) u32_a1;
-      store_w<T, W, true>((typename T::raw*)s.w + row * s.ld_w + col, ow);
-#pragma unroll
-      for (int k = 0; k < W / 4; ++k) {
-        __builtin_nontemporal_store(cm[k], (gptr<u32_a1>)as_global((unsigned char*)s.m + j + 4 * k));
-        __builtin_nontemporal_store(cv[k], (gptr<u32_a1>)as_global((unsigned char*)s.v + j + 4 * k));
-      }
+    auto vectors = [&] {
+      put_weights(s, ow);
+      put_bytes((unsigned char*)s.m + j, cm, s.stream & 2);
+      put_bytes((unsigned char*)s.v + j, cv, s.stream & 2);
+    };
+    if (FULL || whole) {
+      vectors();
     } else {
       each(s, [&](int k, typename T::raw* to) {
         store1<T>(to, ow[k]);
@@ -319,35 +412,50 @@ struct AdamVector {
   }
 };
 
-// A workgroup takes tiles that adjoin, of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
+// A workgroup takes every gridDim.x-th tile of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
 template <typename T, typename R, bool EIGHT>
 __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {
-  constexpr int W = kAdamWidth<T, R, EIGHT>, TILE = 256 * W * kAdamUnroll;
+  constexpr int W = kAdamWidth<T, R, EIGHT>, TILE = 256 * W * kAdamUnroll<EIGHT>;
   __shared__ FiraAdamFactors shared;
+  // (the other wavefronts' first loads are on their way meanwhile)
   if (threadIdx.x == 0) shared = adam_factors(hp, lr, norm, *as_global(counter));
-  __syncthreads();
-  const FiraAdamFactors f = shared;
-  const int from = blockIdx.x * l.each, until = min(from + l.each, l.tiles);
-  int k = 0;                                             // the last piece that does not begin after the first tile
+  bool ready = false;
+  FiraAdamFactors f;
+  int k = 0;
 #pragma unroll 1
-  for (int step = 32; step; step >>= 1)
-    if (k + step < l.count && l.s[k + step].tile0 <= from) k += step;
-#pragma unroll 1
-  for (int tile = from; tile < until; ++tile) {
+  for (int tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
     while (k + 1 < l.count && l.s[k + 1].tile0 <= tile) ++k;
     k = __builtin_amdgcn_readfirstlane(k);
     const FiraAdamSpan& s = l.s[k];
     const unsigned first = (unsigned)(tile - s.tile0) * TILE;
-    AdamVector<T, R, EIGHT, W> x[kAdamUnroll];
+    // vectors that are on their way together: one where there are ends to look for, which take registers and branches
+    auto work = [&](auto place, auto together) {
+      constexpr int N = decltype(together)::value;
+#pragma unroll 1
+      for (int u0 = 0; u0 < kAdamUnroll<EIGHT>; u0 += N) {
+        AdamVector<T, R, EIGHT, W, decltype(place)::value> x[N];
 #pragma unroll
-    for (int u = 0; u < kAdamUnroll; ++u) x[u].load(s, first + (u * 256 + threadIdx.x) * W);
-    const float decay = (float)(1.0 - f.lr * s.weight_decay);
-    const unsigned key = adam_mix(adam_mix(s.seed) + f.t);
+        for (int u = 0; u < N; ++u) x[u].load(s, first + ((u0 + u) * 256 + threadIdx.x) * W);
+        if (!ready) {
+          __syncthreads();
+          f = shared;
+          ready = true;
+        }
+        const float decay = (float)(1.0 - f.lr * (double)s.weight_decay);
+        const unsigned key = adam_mix(adam_mix(s.seed) + f.t);
 #pragma unroll
-    for (int u = 0; u < kAdamUnroll; ++u) {
-      if constexpr (EIGHT) x[u].step_e4m3(s, hp, f, decay, key);
-      else x[u].step_f32(s, hp, f, decay);
-    }
+        for (int u = 0; u < N; ++u) {
+          if constexpr (EIGHT) x[u].step_e4m3(s, hp, f, decay, key);
+          else x[u].step_f32(s, hp, f, decay);
+        }
+      }
+    };
+    typedef std::integral_constant<int, kAdamUnroll<EIGHT>> All;
+    typedef std::integral_constant<int, 1> One;
+    if (s.cols) work(std::integral_constant<int, kApart>{}, One{});
+    else if (s.n - first < (unsigned)TILE) work(std::integral_constant<int, kEnd>{}, One{});
+    else if (s.stream == 3) work(std::integral_constant<int, kStreamed>{}, All{});
+    else work(std::integral_constant<int, kWhole>{}, All{});
   }
 }
 
