@@ -59,7 +59,7 @@ void for_each_adamw_launch(const fira_adamw_desc* d, int count, void* const* W, 
         constexpr int64_t tile = 256 * kAdamUnroll<decltype(e)::value> * kAdamWidth<decltype(t), decltype(r), decltype(e)::value>;
         FiraAdamSpans l{};
         auto flush = [&] {
-          if (l.count) f(t, r, e, (const FiraAdamSpans&)l);
+          if (l.count) f(t, r, e, l);
           l.count = l.tiles = 0;
         };
         for (int i = 0; i < count; ++i) {
@@ -203,11 +203,15 @@ fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adam
   const hipStream_t q = (hipStream_t)hip_stream;
   const FiraAdamHp h{hp->lr, std::log(hp->beta1), std::log(hp->beta2), hp->max_norm, (float)hp->beta1, (float)hp->beta2, (float)(1.0 - hp->beta1), (float)(1.0 - hp->beta2),
                      (float)hp->eps};
-  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, const FiraAdamSpans& l) {
-    hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value>), dim3(std::min(l.tiles, kAdamWorkgroups<decltype(eight)::value>)), dim3(256), 0, q, l, h, dev_lr, dev_norm,
-                       (long long*)dev_t);
+  int launches = 0, at = 0;
+  bool counted = false;
+  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto, auto, auto, FiraAdamSpans&) { ++launches; });
+  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, FiraAdamSpans& l) {
+    const int workgroups = std::min(l.tiles, kAdamWorkgroups<decltype(eight)::value>);
+    l.counts = counted = ++at == launches && workgroups <= kAdamCounting;
+    hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value>), dim3(workgroups), dim3(256), 0, q, l, h, dev_lr, dev_norm, (long long*)dev_t);
   });
-  hipLaunchKernelGGL(fira_adamw_count_kernel<>, dim3(1), dim3(1), 0, q, (long long*)dev_t);
+  if (!counted) hipLaunchKernelGGL(fira_adamw_count_kernel<>, dim3(1), dim3(1), 0, q, (long long*)dev_t);
   return launched("AdamW step");
 }
 
