@@ -19,10 +19,117 @@ struct FiraBlockStats {
   float *mean, *rstd, *post_mean, *post_rstd;
 };
 
-// Sum over a workgroup of 1024.
-__device__ __forceinline__ float wide_sum(float x, float* part) { return block_sum(x, part); }
+// A row is held in registers as in fira_layer_norm.h: THREADS threads, NV vectors of W values to a thread.  Bound by memory.
+template <typename T, typename P, int W, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm_kernel(FiraBlockNorm n, const typename T::raw* x, const typename T::raw* b, FiraBlockVectors<P> vec,
+                                                                                        typename T::raw* r, typename T::raw* y, FiraBlockStats to) {
+  constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
+  __shared__ float part[2][16][2];
+  const int me = threadIdx.x % THREADS;
+  const float dim = (float)n.dim;
+  int turn = 0;
+  for (long long row0 = (long long)blockIdx.x * GROUPS; row0 < n.rows; row0 += (long long)gridDim.x * GROUPS) {
+    const long long row = row0 + threadIdx.x / THREADS;
+    const bool here = row < n.rows;
+    const long long at = here ? row : n.rows - 1;
+    Raw<T, W> xs[NV], bs[NV];
+    int skip[NV];                                          // values of a vector that are not this thread's
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      bs[v].stream(b + at * n.ld_b + c.at);
+      xs[v].stream(x + at * n.ld_x + c.at);
+      skip[v] = v < NV / 2 ? 0 : c.any ? c.skip : W;
+    }
+    float u[NV][W];
+    auto sum = [&](auto f) {
+      float s = 0.0f, none = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) s += v < NV / 2 || j >= skip[v] ? f(u[v][j]) : 0.0f;
+      row_sums<THREADS>(s, none, part, turn++);
+      return s;
+    };
+    // u -= its mean; 1 / the deviation that is left
+    auto stats = [&](int kind, float eps, float& mu, float& rs) {
+      mu = 0.0f;
+      if (kind == kLayer) {
+        mu = sum([](float x) { return x; }) / dim;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < W; ++j) u[v][j] -= mu;
+      }
+      rs = 1.0f / sqrtf(sum([](float x) { return x * x; }) / dim + eps);
+    };
+    auto times = [&](const typename P::raw* w) {
+      if (!w) return;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        Raw<P, W> ws;
+        ws.load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+#pragma unroll
+        for (int j = 0; j < W; ++j) u[v][j] *= ws.get(j);
+      }
+    };
+    auto plus = [&](const typename P::raw* w) {
+      if (!w) return;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        Raw<P, W> ws;
+        ws.load(w + Columns<W>((long long)(v * THREADS + me) * W, n.dim).at);
+#pragma unroll
+        for (int j = 0; j < W; ++j) u[v][j] += ws.get(j);
+      }
+    };
+    auto put = [&](typename T::raw* out, long long ld) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+        if (here && c.any) store_w<T, W, true>(out + row * ld + c.at, u[v]);
+      }
+    };
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) u[v][j] = bs[v].get(j);
+    float pm = 0.0f, ps = 1.0f, mu = 0.0f, rs = 1.0f;
+    if (n.post != kNone) {
+      stats(n.post, n.post_eps, pm, ps);
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) u[v][j] *= ps;
+      times(vec.pw);
+      plus(vec.pb);
+    }
+    times(vec.gate);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) u[v][j] = n.beta * xs[v].get(j) + n.alpha * u[v][j];
+    if (r) put(r, n.ld_r);
+    if (n.norm != kNone) {
+      stats(n.norm, n.eps, mu, rs);
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) u[v][j] *= rs;
+      times(vec.w);
+      plus(vec.b);
+      put(y, n.ld_y);
+    }
+    if (here && me == 0) {
+      if (to.mean && n.norm == kLayer) *as_global(to.mean + row) = mu;
+      if (to.rstd && n.norm != kNone) *as_global(to.rstd + row) = rs;
+      if (to.post_mean && n.post == kLayer) *as_global(to.post_mean + row) = pm;
+      if (to.post_rstd && n.post != kNone) *as_global(to.post_rstd + row) = ps;
+    }
+  }
+}
 
-// A workgroup for a row, which it reads again for every sum.
+// Rows wider than kNormWidest: a workgroup for a row, which it reads again for every sum.
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void fira_block_norm_wide_kernel(FiraBlockNorm n, const typename T::raw* x, const typename T::raw* b, FiraBlockVectors<P> v, typename T::raw* r,
                                                                     typename T::raw* y, FiraBlockStats to) {
@@ -33,7 +140,7 @@ __global__ __launch_bounds__(1024) void fira_block_norm_wide_kernel(FiraBlockNor
     auto total = [&](auto f) {
       float s = 0.0f;
       for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) s += f(c);
-      return wide_sum(s, part);
+      return block_sum(s, part);
     };
     // mean and 1 / deviation of f
     auto stats = [&](int kind, float eps, auto f, float& mu, float& rs) {
@@ -111,7 +218,7 @@ __global__ __launch_bounds__(1024) void fira_block_norm_wide_rows_kernel(FiraBlo
     auto total = [&](auto f) {
       float s = 0.0f;
       for (long long c = threadIdx.x; c < n.dim; c += blockDim.x) s += f(c);
-      return wide_sum(s, part);
+      return block_sum(s, part);
     };
     const float s1 = n.norm == kLayer ? total([&](long long c) { return at.g(v, c); }) / dim : 0.0f;
     const float s2 = n.norm != kNone ? total([&](long long c) { return at.g(v, c) * at.h(c); }) / dim : 0.0f;

@@ -270,8 +270,18 @@ fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, in
     typedef decltype(t) T;
     typedef decltype(p) P;
     typedef typename T::raw raw;
-    hipLaunchKernelGGL((fira_block_norm_wide_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, (hipStream_t)hip_stream, n, (const raw*)dev_x, (const raw*)dev_block,
-                       block_vectors<P>(d, params), (raw*)dev_residual, (raw*)dev_y, to);
+    const FiraBlockVectors<P> v = block_vectors<P>(d, params);
+    const hipStream_t q = (hipStream_t)hip_stream;
+    if (d->dim > kNormWidest) {
+      hipLaunchKernelGGL((fira_block_norm_wide_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, (const raw*)dev_x, (const raw*)dev_block, v,
+                         (raw*)dev_residual, (raw*)dev_y, to);
+      return;
+    }
+    with_row_shape<T, 16>(d->dim, [&](auto width, auto threads, auto nv) {
+      constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
+      hipLaunchKernelGGL((fira_block_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)), dim3(std::max(256, THREADS)), 0, q, n,
+                         (const raw*)dev_x, (const raw*)dev_block, v, (raw*)dev_residual, (raw*)dev_y, to);
+    });
   });
   return launched("block norm");
 }
