@@ -179,6 +179,163 @@ __global__ __launch_bounds__(1024) void fira_block_norm_wide_kernel(FiraBlockNor
   }
 }
 
+// What the gradient's kernel holds of a row: its values as they are stored, and the statistics.
+template <typename T, int W, int NV>
+struct BlockRowHeld {
+  Raw<T, W> dr[NV], dy[NV], r[NV], b[NV];
+  float mu, rs, pm, ps;
+};
+
+// t = dr + rstd (g - mean g - h mean(g h)), g = w dy;  dx = beta t;  q = alpha gate t pw,  db = rstd' (q - mean q - h' mean(q h')).  One pass as in fira_layer_norm_gradient_kernel: a workgroup takes
+// every gridDim.x-th row, or set of rows side by side, the next one's values on their way, and adds up its columns of dy h, dy, t h' and t, of which the vectors' gradients are
+// made (block_vector_gradients): gate and post norm need no sums of their own.  partial: [4][gridDim.x][dim], of which `sums` (bits) are wanted.  Bound by memory.
+constexpr int kBlockWidest = 8192;      // of the gradient's rows in registers, 16 values a thread
+template <typename T, typename P, int W, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm_gradient_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
+                                                                                                 const typename T::raw* b, FiraBlockVectors<P> vec, FiraBlockStats stats,
+                                                                                                 typename T::raw* dx, typename T::raw* db, float* partial, int sums) {
+  constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
+  constexpr int BUFS = NV * W > 8 || THREADS > 512 ? 1 : 2;      // (there are no registers for two rows then)
+  __shared__ float part[2][16][2];
+  __shared__ float joined[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? THREADS * W : 1];
+  const int me = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
+  const float dim = (float)n.dim;
+  const bool pre = n.norm != kNone, post = n.post != kNone, block = b != nullptr;
+  Raw<P, W> ws[NV], gs[NV], pws[NV];
+  int skip[NV];                                          // values of a vector that are not this thread's
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+    if (vec.w) ws[v].load(vec.w + c.at);
+    if (vec.gate) gs[v].load(vec.gate + c.at);
+    if (vec.pw) pws[v].load(vec.pw + c.at);
+    skip[v] = v < NV / 2 ? 0 : c.any ? c.skip : W;
+  }
+  float s0[NV][W] = {}, s1[NV][W] = {}, s2[NV][W] = {}, s3[NV][W] = {};
+  BlockRowHeld<T, W, NV> rows[BUFS];
+  const long long step = (long long)gridDim.x * GROUPS;
+  auto load = [&](int to, long long row) {
+    row = min(row, n.rows - 1);
+    BlockRowHeld<T, W, NV>& x = rows[to];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const long long c = Columns<W>((long long)(v * THREADS + me) * W, n.dim).at;
+      if (pre) { x.dy[v].stream(dy + row * n.ld_y + c); x.r[v].stream(r + row * n.ld_r + c); }
+      if (dr) x.dr[v].stream(dr + row * n.ld_x + c);
+      if (block) x.b[v].stream(b + row * n.ld_b + c);
+    }
+    x.mu = n.norm == kLayer ? *as_global(stats.mean + row) : 0.0f;
+    x.rs = pre ? *as_global(stats.rstd + row) : 1.0f;
+    x.pm = n.post == kLayer ? *as_global(stats.post_mean + row) : 0.0f;
+    x.ps = post ? *as_global(stats.post_rstd + row) : 1.0f;
+  };
+  int turn = 0;
+  auto work = [&](int of, long long row0) {
+    const BlockRowHeld<T, W, NV>& x = rows[of];
+    const long long row = row0 + group;
+    const bool here = row < n.rows;
+    float t[NV][W];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < W; ++j) t[v][j] = dr ? x.dr[v].get(j) : 0.0f;
+    if (pre) {
+      float a1 = 0.0f, a2 = 0.0f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float d = x.dy[v].get(j), h = (x.r[v].get(j) - x.mu) * x.rs, g = vec.w ? d * ws[v].get(j) : d;
+          const bool own = v < NV / 2 || j >= skip[v];
+          a1 += own ? g : 0.0f;
+          a2 = own ? __builtin_fmaf(g, h, a2) : a2;
+          s0[v][j] = here ? __builtin_fmaf(d, h, s0[v][j]) : s0[v][j];
+          s1[v][j] += here ? d : 0.0f;
+        }
+      row_sums<THREADS>(a1, a2, part, turn++);
+      a1 = n.norm == kLayer ? a1 / dim : 0.0f;
+      a2 /= dim;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float d = x.dy[v].get(j), h = (x.r[v].get(j) - x.mu) * x.rs, g = vec.w ? d * ws[v].get(j) : d;
+          t[v][j] += x.rs * (g - __builtin_fmaf(h, a2, a1));
+        }
+    }
+    float q1 = 0.0f, q2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        o[j] = n.beta * t[v][j];
+        const float hb = block ? (x.b[v].get(j) - x.pm) * x.ps : 0.0f;
+        s2[v][j] = here ? __builtin_fmaf(t[v][j], hb, s2[v][j]) : s2[v][j];
+        s3[v][j] += here ? t[v][j] : 0.0f;
+        t[v][j] *= n.alpha;
+        if (vec.gate) t[v][j] *= gs[v].get(j);
+        if (vec.pw) t[v][j] *= pws[v].get(j);
+        const bool own = v < NV / 2 || j >= skip[v];
+        q1 += own ? t[v][j] : 0.0f;
+        q2 = own ? __builtin_fmaf(t[v][j], hb, q2) : q2;
+      }
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      if (dx && here && c.any) store_w<T, W, true>(dx + row * n.ld_dx + c.at, o);
+    }
+    if (!db) return;
+    if (post) {
+      row_sums<THREADS>(q1, q2, part, turn++);
+      q1 = n.post == kLayer ? q1 / dim : 0.0f;
+      q2 /= dim;
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = post ? x.ps * (t[v][j] - __builtin_fmaf((x.b[v].get(j) - x.pm) * x.ps, q2, q1)) : t[v][j];
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      if (here && c.any) store_w<T, W, true>(db + row * n.ld_db + c.at, o);
+    }
+  };
+  // (two rows a turn, so that which registers hold which is known to the compiler)
+  long long row0 = (long long)blockIdx.x * GROUPS;
+  if constexpr (BUFS == 1) {
+    for (; row0 < n.rows; row0 += step) { load(0, row0 + group); work(0, row0); }
+  } else {
+    load(0, row0 + group);
+    for (; row0 < n.rows; row0 += 2 * step) {
+      load(1, row0 + step + group);
+      work(0, row0);
+      if (row0 + step >= n.rows) break;
+      load(0, row0 + 2 * step + group);
+      work(1, row0 + step);
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 4; ++which) {
+    if (!(sums >> which & 1)) continue;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float (&s)[W] = which == 0 ? s0[v] : which == 1 ? s1[v] : which == 2 ? s2[v] : s3[v];
+      if constexpr (GROUPS > 1) {
+        __syncthreads();
+        if (group)
+#pragma unroll
+          for (int j = 0; j < W; ++j) joined[group - 1][j * THREADS + me] = s[j];
+        __syncthreads();
+        if (group) continue;
+#pragma unroll 4
+        for (int k = 0; k < GROUPS - 1; ++k)
+#pragma unroll
+          for (int j = 0; j < W; ++j) s[j] += joined[k][j * THREADS + me];
+      }
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      if (c.any) store_w<FiraStoredF32, W>(partial + ((long long)which * gridDim.x + blockIdx.x) * n.dim + c.at, s);
+    }
+  }
+}
+
 // What the gradient's kernels read of a row's values.
 template <typename T, typename P>
 struct BlockRow {
@@ -205,8 +362,7 @@ struct BlockRow {
   __device__ __forceinline__ float hb(long long c) const { return b ? (load1<T>(b + c) - pm) * ps : 0.0f; }
 };
 
-// t = dr + rstd (g - mean g - h mean(g h)), g = w dy;  dx = beta t;  q = alpha gate t pw,  db = rstd' (q - mean q - h' mean(q h')).  A workgroup for a row; means: of g and g h of every row,
-// for the sums over rows.
+// Rows wider than kBlockWidest: a workgroup for a row, which it reads again for every sum.  means: of g and g h of every row, for the sums over rows.
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void fira_block_norm_wide_rows_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
                                                                          const typename T::raw* b, FiraBlockVectors<P> v, FiraBlockStats stats, typename T::raw* dx,
@@ -277,12 +433,47 @@ __device__ __forceinline__ void block_vector_gradients(const FiraBlockNorm& n, c
   put(to.pw, n.alpha * (gate * s[2]));
   put(to.pb, n.alpha * (gate * s[3]));
 }
+// Sums of the parts, for 16 columns a workgroup: four lanes of four columns, a part of the parts to each of the 64 sets of four lanes.
 template <typename P>
-__global__ __launch_bounds__(256) void fira_block_norm_join_kernel(FiraBlockNorm n, const float* partial, int parts, FiraBlockVectors<P> v, FiraBlockGradients<P> to, int accumulate) {
-  const long long c = blockIdx.x * 256LL + threadIdx.x;
-  if (c >= n.dim) return;
-  float s[4] = {};
-  for (int k = 0; k < 4; ++k)
-    for (int p = 0; p < parts; ++p) s[k] += *as_global(partial + ((long long)k * parts + p) * n.dim + c);
-  block_vector_gradients(n, v, to, s, c, accumulate);
+__global__ __launch_bounds__(256) void fira_block_norm_join_kernel(FiraBlockNorm n, const float* partial, int parts, int sums, FiraBlockVectors<P> v, FiraBlockGradients<P> to,
+                                                                   int accumulate) {
+  constexpr int SETS = 64, N = 4;
+  __shared__ float all[SETS][4][17];
+  const int lane = threadIdx.x % 4, set = threadIdx.x / 4;
+  const long long c0 = blockIdx.x * 16LL;
+  const int cols = (int)min(16LL, n.dim - c0);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float s[4] = {};
+    if (sums >> k & 1)
+      for (int p0 = set; p0 < parts; p0 += SETS * N) {
+        float x[N][4];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float* const from = partial + ((long long)k * parts + min(p0 + SETS * i, parts - 1)) * n.dim + c0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[i][j] = *as_global(from + min(j * 4 + lane, cols - 1));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (p0 + SETS * i < parts)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] += x[i][j];
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) all[set][k][j * 4 + lane] = s[j];
+  }
+  __syncthreads();
+  // a wavefront for each sum, four lanes to a column
+  const int k = threadIdx.x >> 6, c = threadIdx.x & 15, quarter = (threadIdx.x & 63) >> 4;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < SETS / 4; ++i) s += all[quarter * (SETS / 4) + i][k][c];
+  s = add_xor<16>(add_xor<32>(s));
+  __syncthreads();
+  if (quarter == 0) all[0][k][c] = s;
+  __syncthreads();
+  if (threadIdx.x >= cols) return;
+  const float found[4] = {all[0][0][c], all[0][1][c], all[0][2][c], all[0][3][c]};
+  block_vector_gradients(n, v, to, found, c0 + c, accumulate);
 }

@@ -170,8 +170,10 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
   return v;
 }
 
-// Sums of the gradient's workgroups, and the workspace: the sums, then two means of every row.
-int64_t block_parts(const fira_block_norm_desc* d) { return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64)); }
+// Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
+int64_t block_parts(const fira_block_norm_desc* d) {
+  return std::max<int64_t>(1, d->dim > kBlockWidest ? std::min<int64_t>(d->rows, 64) : row_parts(d->rows, d->dim, d->dtype));
+}
 size_t block_sums_bytes(const fira_block_norm_desc* d) { return up256(4 * block_parts(d) * d->dim * 4); }
 
 }  // namespace
@@ -288,7 +290,7 @@ fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, in
 
 size_t fira_block_norm_gradient_workspace_bytes(const fira_block_norm_desc* d) {
   if (check_block(d, nullptr)) return 0;
-  return std::max<size_t>(2 * FIRA_UNUSED_WORKSPACE_BYTES, block_sums_bytes(d) + up256(8 * d->rows));
+  return std::max<size_t>(2 * FIRA_UNUSED_WORKSPACE_BYTES, block_sums_bytes(d) + (d->dim > kBlockWidest ? up256(8 * d->rows) : 0));
 }
 
 fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* dev_dresidual, int64_t ld_dresidual, const void* dev_dy, int64_t ld_dy, const void* dev_residual,
@@ -354,11 +356,24 @@ fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* 
     const int parts = (int)block_parts(d);
     float* const partial = (float*)dev_workspace;
     float* const means = (float*)((char*)dev_workspace + block_sums_bytes(d));
-    if (d->rows) hipLaunchKernelGGL((fira_block_norm_wide_rows_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dr, dy, r, b, v, stats, (raw*)dev_dx, (raw*)dev_dblock, means);
-    if (sums) {
-      hipLaunchKernelGGL((fira_block_norm_wide_sums_kernel<T, P>), dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dr, dy, r, b, v, stats, (const float*)means, partial);
-      hipLaunchKernelGGL(fira_block_norm_join_kernel<P>, dim3((d->dim + 255) / 256), dim3(256), 0, q, n, (const float*)partial, parts, v, to, accumulate);
+    // (which of the sums of dy h, dy, t h' and t are wanted)
+    const int wanted = (g.weight ? 1 : 0) | (g.bias ? 2 : 0) | (g.gate || g.post_weight ? 4 : 0) | ((g.gate && v.pb) || g.post_bias ? 8 : 0);
+    if (!d->rows) {                                        // (nothing to add up)
+    } else if (d->dim > kBlockWidest) {
+      hipLaunchKernelGGL((fira_block_norm_wide_rows_kernel<T, P>), dim3(std::min<int64_t>(d->rows, 1 << 20)), dim3(1024), 0, q, n, dr, dy, r, b, v, stats, (raw*)dev_dx, (raw*)dev_dblock, means);
+      if (sums) hipLaunchKernelGGL((fira_block_norm_wide_sums_kernel<T, P>), dim3((d->dim + 255) / 256, parts), dim3(256), 0, q, n, dr, dy, r, b, v, stats, (const float*)means, partial);
+    } else {
+      auto launch = [&](auto width, auto threads, auto nv) {
+        constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+        hipLaunchKernelGGL((fira_block_norm_gradient_kernel<T, P, W, THREADS, NV>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dr, dy, r, b, v, stats, (raw*)dev_dx, (raw*)dev_dblock,
+                           partial, wanted);
+      };
+      if (d->dim > kBlockWidest / 2) launch(Int<kWidth<T>>{}, Int<kBlockWidest / 16>{}, Int<16 / kWidth<T>>{});
+      else with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
+        if constexpr (decltype(threads)::value <= 512) launch(width, threads, nv);
+      });
     }
+    if (sums) hipLaunchKernelGGL(fira_block_norm_join_kernel<P>, dim3((d->dim + 15) / 16), dim3(256), 0, q, n, (const float*)partial, d->rows ? parts : 0, wanted, v, to, accumulate);
   });
   return launched("block norm gradient");
 }
