@@ -25,11 +25,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
                                                                                         typename T::raw* r, typename T::raw* y, FiraBlockStats to) {
   constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
   __shared__ float part[2][16][2];
-  const int me = threadIdx.x % THREADS;
+  const int me = GROUPS == 1 ? threadIdx.x : threadIdx.x % THREADS, group = GROUPS == 1 ? 0 : threadIdx.x / THREADS;   // (a row of a workgroup has a scalar address)
   const float dim = (float)n.dim;
   int turn = 0;
   for (long long row0 = (long long)blockIdx.x * GROUPS; row0 < n.rows; row0 += (long long)gridDim.x * GROUPS) {
-    const long long row = row0 + threadIdx.x / THREADS;
+    const long long row = row0 + group;
     const bool here = row < n.rows;
     const long long at = here ? row : n.rows - 1;
     Raw<T, W> xs[NV], bs[NV];
@@ -187,36 +187,40 @@ struct BlockRowHeld {
 };
 
 // t = dr + rstd (g - mean g - h mean(g h)), g = w dy;  dx = beta t;  q = alpha gate t pw,  db = rstd' (q - mean q - h' mean(q h')).  One pass as in fira_layer_norm_gradient_kernel: a workgroup takes
-// every gridDim.x-th row, or set of rows side by side, the next one's values on their way, and adds up its columns of dy h, dy, t h' and t, of which the vectors' gradients are
+// every gridDim.x-th row, or set of rows side by side, and adds up its columns of dy h, dy, t h' and t, of which the vectors' gradients are
 // made (block_vector_gradients): gate and post norm need no sums of their own.  partial: [4][gridDim.x][dim], of which `sums` (bits) are wanted.  Bound by memory.
 constexpr int kBlockWidest = 8192;      // of the gradient's rows in registers, 16 values a thread
-template <typename T, typename P, int W, int THREADS, int NV>
+// LEAN: no means and no sums of dy and t, as for root-mean-square norms without biases, which leaves registers for more wavefronts.
+template <typename T, typename P, int W, int THREADS, int NV, bool LEAN>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm_gradient_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
                                                                                                  const typename T::raw* b, FiraBlockVectors<P> vec, FiraBlockStats stats,
                                                                                                  typename T::raw* dx, typename T::raw* db, float* partial, int sums) {
   constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
-  constexpr int BUFS = NV * W > 8 || THREADS > 512 ? 1 : 2;      // (there are no registers for two rows then)
   __shared__ float part[2][16][2];
   __shared__ float joined[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? THREADS * W : 1];
-  const int me = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
+  const int me = GROUPS == 1 ? threadIdx.x : threadIdx.x % THREADS, group = GROUPS == 1 ? 0 : threadIdx.x / THREADS;   // (a row of a workgroup has a scalar address)
   const float dim = (float)n.dim;
   const bool pre = n.norm != kNone, post = n.post != kNone, block = b != nullptr;
-  Raw<P, W> ws[NV], gs[NV], pws[NV];
+  float wf[NV][W], qf[NV][W];                            // w, and alpha gate pw
   int skip[NV];                                          // values of a vector that are not this thread's
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
-    if (vec.w) ws[v].load(vec.w + c.at);
-    if (vec.gate) gs[v].load(vec.gate + c.at);
-    if (vec.pw) pws[v].load(vec.pw + c.at);
+    Raw<P, W> w, g, pw;
+    if (vec.w) w.load(vec.w + c.at);
+    if (vec.gate) g.load(vec.gate + c.at);
+    if (vec.pw) pw.load(vec.pw + c.at);
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      wf[v][j] = vec.w ? w.get(j) : 1.0f;
+      qf[v][j] = n.alpha * (vec.gate ? g.get(j) : 1.0f) * (vec.pw ? pw.get(j) : 1.0f);
+    }
     skip[v] = v < NV / 2 ? 0 : c.any ? c.skip : W;
   }
-  float s0[NV][W] = {}, s1[NV][W] = {}, s2[NV][W] = {}, s3[NV][W] = {};
-  BlockRowHeld<T, W, NV> rows[BUFS];
-  const long long step = (long long)gridDim.x * GROUPS;
-  auto load = [&](int to, long long row) {
+  float s0[NV][W] = {}, s2[NV][W] = {}, s1[LEAN ? 1 : NV][W] = {}, s3[LEAN ? 1 : NV][W] = {};
+  BlockRowHeld<T, W, NV> x;
+  auto load = [&](long long row) {
     row = min(row, n.rows - 1);
-    BlockRowHeld<T, W, NV>& x = rows[to];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const long long c = Columns<W>((long long)(v * THREADS + me) * W, n.dim).at;
@@ -224,100 +228,120 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
       if (dr) x.dr[v].stream(dr + row * n.ld_x + c);
       if (block) x.b[v].stream(b + row * n.ld_b + c);
     }
-    x.mu = n.norm == kLayer ? *as_global(stats.mean + row) : 0.0f;
+    x.mu = !LEAN && n.norm == kLayer ? *as_global(stats.mean + row) : 0.0f;
     x.rs = pre ? *as_global(stats.rstd + row) : 1.0f;
-    x.pm = n.post == kLayer ? *as_global(stats.post_mean + row) : 0.0f;
+    x.pm = !LEAN && n.post == kLayer ? *as_global(stats.post_mean + row) : 0.0f;
     x.ps = post ? *as_global(stats.post_rstd + row) : 1.0f;
   };
+  // Sums of f(v, j, a, b) over the row's values.  Those at the end of a row that are a neighbour's are left out again where there are some.
   int turn = 0;
-  auto work = [&](int of, long long row0) {
-    const BlockRowHeld<T, W, NV>& x = rows[of];
+  auto row_total = [&](float& a, float& b, auto f) {
+    a = b = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float va = 0.0f, vb = 0.0f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) f(v, j, va, vb);
+      if (v >= NV / 2 && skip[v]) {
+        va = vb = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          float ja = 0.0f, jb = 0.0f;
+          f(v, j, ja, jb);
+          va += j >= skip[v] ? ja : 0.0f;
+          vb += j >= skip[v] ? jb : 0.0f;
+        }
+      }
+      a += va;
+      b += vb;
+    }
+    row_sums<THREADS>(a, b, part, turn++);
+  };
+  auto work = [&](long long row0) {
     const long long row = row0 + group;
-    const bool here = row < n.rows;
+    const bool here = GROUPS == 1 || row < n.rows;       // (a set of rows may be short: its other rows count as zeros)
+    auto hr = [&](int v, int j) { return (LEAN ? x.r[v].get(j) : x.r[v].get(j) - x.mu) * x.rs; };
+    auto hb = [&](int v, int j) { return (LEAN ? x.b[v].get(j) : x.b[v].get(j) - x.pm) * x.ps; };
+    auto put = [&](typename T::raw* out, long long ld, int v, const float (&o)[W]) {
+      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
+      if (here && c.any) store_w<T, W, true>(out + row * ld + c.at, o);
+    };
     float t[NV][W];
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int j = 0; j < W; ++j) t[v][j] = dr ? x.dr[v].get(j) : 0.0f;
+      for (int j = 0; j < W; ++j) t[v][j] = dr && here ? x.dr[v].get(j) : 0.0f;
     if (pre) {
-      float a1 = 0.0f, a2 = 0.0f;
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const float d = x.dy[v].get(j), h = (x.r[v].get(j) - x.mu) * x.rs, g = vec.w ? d * ws[v].get(j) : d;
-          const bool own = v < NV / 2 || j >= skip[v];
-          a1 += own ? g : 0.0f;
-          a2 = own ? __builtin_fmaf(g, h, a2) : a2;
-          s0[v][j] = here ? __builtin_fmaf(d, h, s0[v][j]) : s0[v][j];
-          s1[v][j] += here ? d : 0.0f;
-        }
-      row_sums<THREADS>(a1, a2, part, turn++);
-      a1 = n.norm == kLayer ? a1 / dim : 0.0f;
+      auto dy_of = [&](int v, int j) { return here ? x.dy[v].get(j) : 0.0f; };
+      float a1, a2;
+      row_total(a1, a2, [&](int v, int j, float& a, float& b) {
+        const float g = dy_of(v, j) * wf[v][j];
+        if (!LEAN) a += g;
+        b = __builtin_fmaf(g, hr(v, j), b);
+      });
+      a1 = !LEAN && n.norm == kLayer ? a1 / dim : 0.0f;
       a2 /= dim;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-          const float d = x.dy[v].get(j), h = (x.r[v].get(j) - x.mu) * x.rs, g = vec.w ? d * ws[v].get(j) : d;
-          t[v][j] += x.rs * (g - __builtin_fmaf(h, a2, a1));
+          const float d = dy_of(v, j), h = hr(v, j);
+          s0[v][j] = __builtin_fmaf(d, h, s0[v][j]);
+          t[v][j] = __builtin_fmaf(x.rs, d * wf[v][j] - __builtin_fmaf(h, a2, a1), t[v][j]);
         }
+      if (!LEAN && sums & 2)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < W; ++j) s1[v][j] += dy_of(v, j);
     }
-    float q1 = 0.0f, q2 = 0.0f;
+    if (sums & 4)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) s2[v][j] = __builtin_fmaf(t[v][j], hb(v, j), s2[v][j]);
+    if (!LEAN && sums & 8)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) s3[v][j] += t[v][j];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float o[W];
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        o[j] = n.beta * t[v][j];
-        const float hb = block ? (x.b[v].get(j) - x.pm) * x.ps : 0.0f;
-        s2[v][j] = here ? __builtin_fmaf(t[v][j], hb, s2[v][j]) : s2[v][j];
-        s3[v][j] += here ? t[v][j] : 0.0f;
-        t[v][j] *= n.alpha;
-        if (vec.gate) t[v][j] *= gs[v].get(j);
-        if (vec.pw) t[v][j] *= pws[v].get(j);
-        const bool own = v < NV / 2 || j >= skip[v];
-        q1 += own ? t[v][j] : 0.0f;
-        q2 = own ? __builtin_fmaf(t[v][j], hb, q2) : q2;
-      }
-      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
-      if (dx && here && c.any) store_w<T, W, true>(dx + row * n.ld_dx + c.at, o);
+      for (int j = 0; j < W; ++j) o[j] = n.beta * t[v][j];
+      if (dx) put(dx, n.ld_dx, v, o);
+#pragma unroll
+      for (int j = 0; j < W; ++j) t[v][j] *= qf[v][j];
     }
     if (!db) return;
+    float q1 = 0.0f, q2 = 0.0f;
     if (post) {
-      row_sums<THREADS>(q1, q2, part, turn++);
-      q1 = n.post == kLayer ? q1 / dim : 0.0f;
+      row_total(q1, q2, [&](int v, int j, float& a, float& b) {
+        if (!LEAN) a += t[v][j];
+        b = __builtin_fmaf(t[v][j], hb(v, j), b);
+      });
+      q1 = !LEAN && n.post == kLayer ? q1 / dim : 0.0f;
       q2 /= dim;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) t[v][j] = x.ps * (t[v][j] - __builtin_fmaf(hb(v, j), q2, q1));
     }
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float o[W];
-#pragma unroll
-      for (int j = 0; j < W; ++j) o[j] = post ? x.ps * (t[v][j] - __builtin_fmaf((x.b[v].get(j) - x.pm) * x.ps, q2, q1)) : t[v][j];
-      const Columns<W> c((long long)(v * THREADS + me) * W, n.dim);
-      if (here && c.any) store_w<T, W, true>(db + row * n.ld_db + c.at, o);
-    }
+    for (int v = 0; v < NV; ++v) put(db, n.ld_db, v, t[v]);
   };
-  // (two rows a turn, so that which registers hold which is known to the compiler)
-  long long row0 = (long long)blockIdx.x * GROUPS;
-  if constexpr (BUFS == 1) {
-    for (; row0 < n.rows; row0 += step) { load(0, row0 + group); work(0, row0); }
-  } else {
-    load(0, row0 + group);
-    for (; row0 < n.rows; row0 += 2 * step) {
-      load(1, row0 + step + group);
-      work(0, row0);
-      if (row0 + step >= n.rows) break;
-      load(0, row0 + 2 * step + group);
-      work(1, row0 + step);
-    }
+  // (the next row on its way takes registers that more wavefronts can use: 32768 x 4096 bf16 279 us and 283 with it, 16385 x 2049 f32 189 and 224)
+  for (long long row0 = (long long)blockIdx.x * GROUPS; row0 < n.rows; row0 += (long long)gridDim.x * GROUPS) {
+    load(row0 + group);
+    work(row0);
   }
 #pragma unroll
   for (int which = 0; which < 4; ++which) {
-    if (!(sums >> which & 1)) continue;
+    if ((LEAN && which % 2) || !(sums >> which & 1)) continue;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float (&s)[W] = which == 0 ? s0[v] : which == 1 ? s1[v] : which == 2 ? s2[v] : s3[v];
+      float (&s)[W] = which == 0 ? s0[v] : which == 1 ? s1[LEAN ? 0 : v] : which == 2 ? s2[v] : s3[LEAN ? 0 : v];
       if constexpr (GROUPS > 1) {
         __syncthreads();
         if (group)

@@ -171,8 +171,22 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
 }
 
 // Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
+// As many as the chip holds at a time or somewhat fewer, by what was measured, and fewer where that leaves each less than ten turns (of a row, or of the rows that it has side
+// by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with 768, 1024 and 1536: 16385 x 2049 f32
+// 188, 158 and 169, with means and biases (512, 768, 1024) 215, 215 and 224; 131072 x 256 bf16 with those (768, 1024, 1536) 84, 94 and 94.
 int64_t block_parts(const fira_block_norm_desc* d) {
-  return std::max<int64_t>(1, d->dim > kBlockWidest ? std::min<int64_t>(d->rows, 64) : row_parts(d->rows, d->dim, d->dtype));
+  if (d->dim > kBlockWidest) return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64));
+  const bool lean = d->norm != FIRA_LAYER_NORM && d->post != FIRA_LAYER_NORM, f32 = d->dtype == FIRA_F32;
+  int64_t threads = kBlockWidest / 16, side = 1;
+  auto shape = [&](auto, auto t, auto) {
+    threads = std::max(256, decltype(t)::value);
+    side = std::max(1, 256 / decltype(t)::value);
+  };
+  if (d->dim <= kBlockWidest / 2) f32 ? with_row_shape<FiraStoredF32, 8>(d->dim, shape) : with_row_shape<FiraStoredBf16, 8>(d->dim, shape);
+  const int64_t held = d->dim > kBlockWidest / 2 ? 512 : f32 && d->dim > 256 ? (lean ? 1024 : 512) : lean || f32 ? 1024 : 768;
+  const int64_t full = 256 * std::max<int64_t>(1, held / threads), turns = std::max<int64_t>(1, (d->rows + side - 1) / side);
+  const int64_t each = std::min(std::max<int64_t>(10, (turns + full - 1) / full), (4 * turns + full - 1) / full);
+  return (turns + each - 1) / each;
 }
 size_t block_sums_bytes(const fira_block_norm_desc* d) { return up256(4 * block_parts(d) * d->dim * 4); }
 
@@ -365,8 +379,10 @@ fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* 
     } else {
       auto launch = [&](auto width, auto threads, auto nv) {
         constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
-        hipLaunchKernelGGL((fira_block_norm_gradient_kernel<T, P, W, THREADS, NV>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dr, dy, r, b, v, stats, (raw*)dev_dx, (raw*)dev_dblock,
-                           partial, wanted);
+        with_flag(d->norm != FIRA_LAYER_NORM && d->post != FIRA_LAYER_NORM && !(wanted & 10), [&](auto lean) {
+          hipLaunchKernelGGL((fira_block_norm_gradient_kernel<T, P, W, THREADS, NV, decltype(lean)::value>), dim3(parts), dim3(std::max(256, THREADS)), 0, q, n, dr, dy, r, b, v, stats,
+                             (raw*)dev_dx, (raw*)dev_dblock, partial, wanted);
+        });
       };
       if (d->dim > kBlockWidest / 2) launch(Int<kWidth<T>>{}, Int<kBlockWidest / 16>{}, Int<16 / kWidth<T>>{});
       else with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
