@@ -123,20 +123,80 @@ fira_status check_rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, 
   return FIRA_OK;
 }
 
+// How the kernel cuts its work up, in units of `pairs` or `width` values, at most `most` units a workgroup.
+void cut_rotary(FiraRotary& r, int64_t heads, int64_t copied, int pairs, int width, unsigned most) {
+  r.turned = r.half / pairs;
+  r.units = r.turned + (unsigned)(copied / width);
+  r.all = (unsigned)heads * r.units;
+  r.chunk = std::min(r.all, most);
+  r.chunks = (r.all + r.chunk - 1) / r.chunk;
+  r.tile = std::max(1u, std::min({most / r.chunk, kRotaryTile, kRotaryTable / (unsigned)r.half}));
+  r.per_chunk = (unsigned)((((uint64_t)1 << 32) + r.chunk - 1) / r.chunk);
+  r.per_units = (unsigned)((((uint64_t)1 << 32) + r.units - 1) / r.units);
+}
+
 fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int count, const double* frequencies, const void* positions, float sign, void* hip_stream) {
   if (const fira_status st = check_rotary(d, h, count, frequencies, positions)) return st;
   if (!d->batch || !d->length) return FIRA_OK;
+  FiraRotary r{};
+  r.tokens = (unsigned)(d->batch * d->length);
+  r.length = (unsigned)d->length;
+  r.position_stride = d->position_stride;
+  r.half = (int)(d->rotated / 2);
+  r.rotated = (int)d->rotated;
+  r.scale = (float)d->scale;
+  r.sign = sign;
+  const bool interleaved = d->layout == FIRA_ROTARY_INTERLEAVED;
+  r.wide = d->position_type == FIRA_I64;
+  int64_t heads = 0;
+  bool in_place = true;
   for (int i = 0; i < count; ++i) {
-    const int64_t total = d->batch * d->length * h[i].heads * (d->dim - d->rotated / 2);
-    if (!total) continue;
-    FiraRotary r{d->batch, d->length, h[i].heads, d->dim, d->rotated, d->position_stride, {}, {}, (float)d->scale, sign, d->layout == FIRA_ROTARY_INTERLEAVED, d->position_type == FIRA_I64};
-    for (int k = 0; k < 3; ++k) { r.xs[k] = h[i].x_stride[k]; r.ys[k] = h[i].y_stride[k]; }
-    with_types(d->dtype, d->dtype, [&](auto t, auto) {
-      typedef typename decltype(t)::raw raw;
-      hipLaunchKernelGGL(fira_rotary_kernel<decltype(t)>, dim3(std::min<int64_t>((total + 255) / 256, 1 << 20)), dim3(256), 0, (hipStream_t)hip_stream, r, (const raw*)h[i].dev_x,
-                         (raw*)h[i].dev_y, frequencies, positions);
-    });
+    if (!h[i].heads) continue;
+    FiraRotaryTensor& t = r.t[r.count];
+    t = {h[i].dev_x, h[i].dev_y, {}, {}};
+    for (int k = 0; k < 3; ++k) { t.xs[k] = h[i].x_stride[k]; t.ys[k] = h[i].y_stride[k]; }
+    r.first[r.count++] = (int)heads;
+    heads += h[i].heads;
+    in_place = in_place && h[i].dev_x == h[i].dev_y;
   }
+  if (!heads) return FIRA_OK;
+  const int64_t copied = in_place ? 0 : d->dim - d->rotated, total = (int64_t)r.tokens * heads * (r.half + copied);
+  const hipStream_t q = (hipStream_t)hip_stream;
+  with_types(d->dtype, d->dtype, [&](auto t, auto) {
+    typedef decltype(t) T;
+    // (a head's units are below 2^15, and those of all heads below 2^21, so that their products stay in 32 bits)
+    if ((unsigned)r.half > kRotaryTable || r.half + copied > 1 << 15 || heads * (r.half + copied) > 1 << 21) {
+      for (int k = 0; k < r.count; ++k) {
+        const int64_t n = (k + 1 < r.count ? r.first[k + 1] : heads) - r.first[k];
+        hipLaunchKernelGGL(fira_rotary_wide_kernel<T>, dim3(std::min<int64_t>((r.tokens * n * (r.half + copied) + 255) / 256, 1 << 20)), dim3(256), 0, q, r, k, (unsigned)n, (unsigned)copied,
+                           interleaved, frequencies, positions);
+      }
+      return;
+    }
+    auto launch = [&](auto width, auto each, auto inter) {
+      constexpr int W = decltype(width)::value, N = decltype(each)::value;
+      constexpr bool INTER = decltype(inter)::value;
+      cut_rotary(r, heads, copied, INTER && W > 1 ? W / 2 : W, W, 256 * N);
+      // (a launch has less than 2^32 threads)
+      const int64_t step = (int64_t)((1 << 24) - 1) / r.chunks * r.tile;
+      for (int64_t at = 0; at < r.tokens; at += step) {
+        r.token0 = (unsigned)at;
+        hipLaunchKernelGGL((fira_rotary_kernel<T, W, N, INTER>), dim3((std::min<int64_t>(step, r.tokens - at) + r.tile - 1) / r.tile * r.chunks), dim3(256), 0, q, r, frequencies, positions);
+      }
+    };
+    // (few units are spread over more workgroups)
+    auto many = [&](auto width) {
+      with_flag(interleaved, [&](auto inter) {
+        if (total / decltype(width)::value > 1 << 19) launch(width, Int<4>{}, inter);
+        else launch(width, Int<1>{}, inter);
+      });
+    };
+    constexpr int W = kWidth<T>;
+    const int64_t turned = interleaved ? d->rotated : r.half;
+    if (turned % W == 0 && copied % W == 0) many(Int<W>{});
+    else if (turned % 4 == 0 && copied % 4 == 0) many(Int<4>{});
+    else many(Int<1>{});
+  });
   return launched("rotary positions");
 }
 

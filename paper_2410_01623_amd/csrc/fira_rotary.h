@@ -2,12 +2,31 @@
 #pragma once
 #include "fira_rows.h"
 
-struct FiraRotary {
-  long long batch, length, heads, dim, rotated, position_stride;
+constexpr int kRotaryTensors = 4;
+struct FiraRotaryTensor {
+  const void* x;
+  void* y;
   long long xs[3], ys[3];        // strides of sequences, tokens and heads
-  float scale, sign;             // sign: -1 for the gradient
-  int interleaved, wide;         // wide: positions of 64 bits
 };
+struct FiraRotary {
+  FiraRotaryTensor t[kRotaryTensors];
+  int first[kRotaryTensors];     // first head of each tensor, of all tensors' heads one after the other
+  int count;
+  unsigned token0, tokens;       // first token of a launch, and tokens of all sequences
+  unsigned length;               // of a sequence
+  long long position_stride;
+  int half, rotated;
+  float scale, sign;             // sign: -1 for the gradient
+  int wide;                      // positions of 64 bits
+  // A unit is what a thread turns or copies at a time: W pairs as two vectors of W values, where pairs are interleaved one vector of W values (two with W = 1), or one that is
+  // copied.  (Two neighbouring vectors a lane leave every load half a line: 65536 tokens of 32 heads of 128, bf16, interleaved 254 us so and 184 with one.)  A workgroup
+  // takes `tile` tokens and of each `chunk` of the units of all heads.
+  unsigned units, turned;        // of a head, and those of them that are turned
+  unsigned all, tile, chunk, chunks;
+  unsigned per_chunk, per_units; // 2^32 / chunk and 2^32 / units, rounded up
+};
+constexpr unsigned kRotaryTile = 128;         // most tokens of a workgroup
+constexpr unsigned kRotaryTable = 2048;       // most pairs of all its tokens
 
 // cos and sin of position times frequency, times the scale.  The angle is brought to a part of a turn in fp64; what is left fits fp32.
 __device__ __forceinline__ void rotary_turn(long long position, double frequency, float scale, float sign, float& c, float& s) {
@@ -17,30 +36,120 @@ __device__ __forceinline__ void rotary_turn(long long position, double frequency
   c = scale * cs;
   s = sign * scale * sn;
 }
-__device__ __forceinline__ long long rotary_position(const FiraRotary& r, const void* positions, long long batch, long long token) {
-  if (!positions) return token;
-  const long long i = batch * r.position_stride + token;
-  return r.wide ? *as_global((const long long*)positions + i) : (long long)*as_global((const int*)positions + i);
-}
+// x / d for x d < 2^32
+__device__ __forceinline__ unsigned rotary_quotient(unsigned x, unsigned d, unsigned per_d) { return d == 1 ? x : __umulhi(x, per_d); }
 
-// A thread for a pair, or for a value that is copied.
-template <typename T>
-__global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const typename T::raw* x, typename T::raw* y, const double* frequencies, const void* positions) {
-  const long long half = r.rotated / 2, units = half + r.dim - r.rotated, total = r.batch * r.length * r.heads * units;
-  for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
-    const long long u = i % units, head = i / units % r.heads, token = i / units / r.heads % r.length, batch = i / units / r.heads / r.length;
-    const typename T::raw* const from = x + batch * r.xs[0] + token * r.xs[1] + head * r.xs[2];
-    typename T::raw* const to = y + batch * r.ys[0] + token * r.ys[1] + head * r.ys[2];
-    if (u >= half) {
-      const long long c = r.rotated + u - half;
-      to[c] = from[c];
+// The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  Bound by memory.
+template <typename T, int W, int N, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const double* frequencies, const void* positions) {
+  typedef typename T::raw raw;
+  constexpr bool TWO = !INTERLEAVED || W == 1;             // a unit has two vectors
+  constexpr int PAIRS = TWO ? W : W / 2;
+  __shared__ long long place[kRotaryTile];
+  __shared__ unsigned long long from[kRotaryTensors][kRotaryTile], to[kRotaryTensors][kRotaryTile];
+  __shared__ __attribute__((aligned(16))) float cosines[kRotaryTable], sines[kRotaryTable];
+  const unsigned t0 = r.token0 + blockIdx.x / r.chunks * r.tile, c0 = blockIdx.x % r.chunks * r.chunk;
+  const unsigned tokens = min(r.tile, r.tokens - t0), here = min(r.chunk, r.all - c0), head0 = c0 / r.units, unit0 = c0 - head0 * r.units;
+  for (unsigned i = threadIdx.x; i < tokens * (unsigned)r.count; i += 256) {
+    const unsigned k = i / tokens, t = i - k * tokens, batch = (t0 + t) / r.length, token = t0 + t - batch * r.length;
+    const FiraRotaryTensor& x = r.t[k];
+    from[k][t] = (unsigned long long)x.x + (batch * x.xs[0] + token * x.xs[1]) * (long long)sizeof(raw);
+    to[k][t] = (unsigned long long)x.y + (batch * x.ys[0] + token * x.ys[1]) * (long long)sizeof(raw);
+    if (k) continue;
+    const long long p = batch * r.position_stride + token;
+    place[t] = !positions ? (long long)token : r.wide ? *as_global((const long long*)positions + p) : (long long)*as_global((const int*)positions + p);
+  }
+  __syncthreads();
+  Raw<T, W> a[N], b[N];
+  raw* out[N];
+  unsigned unit[N], row[N];
+  bool is[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const unsigned i = n * 256 + threadIdx.x, t = rotary_quotient(i, r.chunk, r.per_chunk), c = i - t * r.chunk;
+    is[n] = t < tokens && c < here;
+    if (!is[n]) continue;
+    const unsigned head = rotary_quotient(unit0 + c, r.units, r.per_units);
+    unsigned h = head0 + head, k = 0;
+    unit[n] = unit0 + c - head * r.units;
+    row[n] = t;
+    long long xh = r.t[0].xs[2], yh = r.t[0].ys[2];
+#pragma unroll
+    for (int j = 1; j < kRotaryTensors; ++j)
+      if (j < r.count && h >= (unsigned)r.first[j]) { k = j; xh = r.t[j].xs[2]; yh = r.t[j].ys[2]; }
+    h -= k ? (unsigned)(k == 1 ? r.first[1] : k == 2 ? r.first[2] : r.first[3]) : 0u;
+    const raw* const in = (const raw*)from[k][t] + h * xh;
+    out[n] = (raw*)to[k][t] + h * yh;
+    if (unit[n] < r.turned) {
+      const unsigned at = unit[n] * W * (INTERLEAVED && TWO ? 2 : 1);
+      a[n].stream(in + at);
+      if (TWO) b[n].stream(in + at + (INTERLEAVED ? 1 : r.half));
+      out[n] += at;
+    } else {
+      const unsigned at = r.rotated + (unit[n] - r.turned) * W;
+      a[n].stream(in + at);
+      out[n] += at;
+    }
+  }
+  for (unsigned i = threadIdx.x; i < tokens * (unsigned)r.half; i += 256) {
+    const unsigned t = i / (unsigned)r.half, j = i - t * (unsigned)r.half;
+    rotary_turn(place[t], *as_global(frequencies + j), r.scale, r.sign, cosines[i], sines[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (!is[n]) continue;
+    float p[W], q[W];
+    if (unit[n] >= r.turned) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) p[j] = a[n].get(j);
+      store_w<T, W, true>(out[n], p);
       continue;
     }
+    const float *const c = cosines + row[n] * r.half + unit[n] * PAIRS, *const s = sines + row[n] * r.half + unit[n] * PAIRS;
+    if constexpr (!TWO) {
+#pragma unroll
+      for (int j = 0; j < W; j += 2) {
+        const float x = a[n].get(j), y = a[n].get(j + 1);
+        p[j] = x * c[j / 2] - y * s[j / 2];
+        p[j + 1] = x * s[j / 2] + y * c[j / 2];
+      }
+      store_w<T, W, true>(out[n], p);
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float x = a[n].get(j), y = b[n].get(j);
+        p[j] = x * c[j] - y * s[j];
+        q[j] = x * s[j] + y * c[j];
+      }
+      store_w<T, W, true>(out[n], p);
+      store_w<T, W, true>(out[n] + (INTERLEAVED ? 1 : r.half), q);
+    }
+  }
+}
+
+// Heads of which more than kRotaryTable pairs are turned: a thread for a pair, or for a value that is copied, of tensor k.
+template <typename T>
+__global__ __launch_bounds__(256) void fira_rotary_wide_kernel(FiraRotary r, int k, unsigned heads, unsigned copied, int interleaved, const double* frequencies, const void* positions) {
+  typedef typename T::raw raw;
+  const FiraRotaryTensor& x = r.t[k];
+  const unsigned long long units = (unsigned)r.half + copied, total = units * heads * r.tokens;
+  for (unsigned long long i = blockIdx.x * 256ULL + threadIdx.x; i < total; i += gridDim.x * 256ULL) {
+    const unsigned u = (unsigned)(i % units), head = (unsigned)(i / units % heads), all = (unsigned)(i / units / heads), batch = all / r.length, token = all - batch * r.length;
+    const raw* const in = (const raw*)x.x + batch * x.xs[0] + token * x.xs[1] + head * x.xs[2];
+    raw* const out = (raw*)x.y + batch * x.ys[0] + token * x.ys[1] + head * x.ys[2];
+    if (u >= (unsigned)r.half) {
+      const unsigned c = r.rotated + u - r.half;
+      *as_global(out + c) = *as_global(in + c);
+      continue;
+    }
+    const long long p = batch * r.position_stride + token;
     float c, s;
-    rotary_turn(rotary_position(r, positions, batch, token), *as_global(frequencies + u), r.scale, r.sign, c, s);
-    const long long ia = r.interleaved ? 2 * u : u, ib = r.interleaved ? 2 * u + 1 : u + half;
-    const float a = load1<T>(from + ia), b = load1<T>(from + ib);
-    store1<T>(to + ia, a * c - b * s);
-    store1<T>(to + ib, a * s + b * c);
+    rotary_turn(!positions ? (long long)token : r.wide ? *as_global((const long long*)positions + p) : (long long)*as_global((const int*)positions + p), *as_global(frequencies + u), r.scale,
+                r.sign, c, s);
+    const unsigned ia = interleaved ? 2 * u : u, ib = interleaved ? 2 * u + 1 : u + r.half;
+    const float a = load1<T>(in + ia), b = load1<T>(in + ib);
+    store1<T>(out + ia, a * c - b * s);
+    store1<T>(out + ib, a * s + b * c);
   }
 }
