@@ -181,7 +181,10 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
       const int64_t step = (int64_t)((1 << 24) - 1) / r.chunks * r.tile;
       for (int64_t at = 0; at < r.tokens; at += step) {
         r.token0 = (unsigned)at;
-        hipLaunchKernelGGL((fira_rotary_kernel<T, W, N, INTER>), dim3((std::min<int64_t>(step, r.tokens - at) + r.tile - 1) / r.tile * r.chunks), dim3(256), 0, q, r, frequencies, positions);
+        with_flag(INTER || r.half * size_of(d->dtype) >= 128, [&](auto stream) {
+          hipLaunchKernelGGL((fira_rotary_kernel<T, W, N, INTER, INTER || decltype(stream)::value>), dim3((std::min<int64_t>(step, r.tokens - at) + r.tile - 1) / r.tile * r.chunks),
+                             dim3(256), 0, q, r, frequencies, positions);
+        });
       }
     };
     // (few units are spread over more workgroups)

@@ -39,8 +39,9 @@ __device__ __forceinline__ void rotary_turn(long long position, double frequency
 // x / d for x d < 2^32
 __device__ __forceinline__ unsigned rotary_quotient(unsigned x, unsigned d, unsigned per_d) { return d == 1 ? x : __umulhi(x, per_d); }
 
-// The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  Bound by memory.
-template <typename T, int W, int N, bool INTERLEAVED>
+// The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  STREAM: past the caches, but for halves
+// of less than a line, which the caches put together (131072 tokens of 64 heads of 64, bf16: 438 us and 392 with them; heads of 128: 184 and 199).  Bound by memory.
+template <typename T, int W, int N, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const double* frequencies, const void* positions) {
   typedef typename T::raw raw;
   constexpr bool TWO = !INTERLEAVED || W == 1;             // a unit has two vectors
@@ -60,6 +61,10 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     place[t] = !positions ? (long long)token : r.wide ? *as_global((const long long*)positions + p) : (long long)*as_global((const int*)positions + p);
   }
   __syncthreads();
+  auto fetch = [](Raw<T, W>& v, const raw* p) {
+    if constexpr (STREAM) v.stream(p);
+    else v.load(p);
+  };
   Raw<T, W> a[N], b[N];
   raw* out[N];
   unsigned unit[N], row[N];
@@ -82,12 +87,12 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     out[n] = (raw*)to[k][t] + h * yh;
     if (unit[n] < r.turned) {
       const unsigned at = unit[n] * W * (INTERLEAVED && TWO ? 2 : 1);
-      a[n].stream(in + at);
-      if (TWO) b[n].stream(in + at + (INTERLEAVED ? 1 : r.half));
+      fetch(a[n], in + at);
+      if (TWO) fetch(b[n], in + at + (INTERLEAVED ? 1 : r.half));
       out[n] += at;
     } else {
       const unsigned at = r.rotated + (unit[n] - r.turned) * W;
-      a[n].stream(in + at);
+      fetch(a[n], in + at);
       out[n] += at;
     }
   }
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     if (unit[n] >= r.turned) {
 #pragma unroll
       for (int j = 0; j < W; ++j) p[j] = a[n].get(j);
-      store_w<T, W, true>(out[n], p);
+      store_w<T, W, STREAM>(out[n], p);
       continue;
     }
     const float *const c = cosines + row[n] * r.half + unit[n] * PAIRS, *const s = sines + row[n] * r.half + unit[n] * PAIRS;
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
         p[j] = x * c[j / 2] - y * s[j / 2];
         p[j + 1] = x * s[j / 2] + y * c[j / 2];
       }
-      store_w<T, W, true>(out[n], p);
+      store_w<T, W, STREAM>(out[n], p);
     } else {
 #pragma unroll
       for (int j = 0; j < W; ++j) {
@@ -122,8 +127,8 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
         p[j] = x * c[j] - y * s[j];
         q[j] = x * s[j] + y * c[j];
       }
-      store_w<T, W, true>(out[n], p);
-      store_w<T, W, true>(out[n] + (INTERLEAVED ? 1 : r.half), q);
+      store_w<T, W, STREAM>(out[n], p);
+      store_w<T, W, STREAM>(out[n] + (INTERLEAVED ? 1 : r.half), q);
     }
   }
 }
