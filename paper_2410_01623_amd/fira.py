@@ -96,7 +96,9 @@ class fira_rotary_desc(ctypes.Structure):
 
 
 class fira_rotary_heads(ctypes.Structure):
-    _fields_ = [("dev_x", ctypes.c_void_p), ("dev_y", ctypes.c_void_p), ("heads", ctypes.c_int64), ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3)]
+    """x_stride[3] and y_stride[3] as six fields, which are set at once."""
+    _fields_ = [("dev_x", ctypes.c_void_p), ("dev_y", ctypes.c_void_p), ("heads", ctypes.c_int64),
+                *((f"{t}_stride_{of}", ctypes.c_int64) for t in "xy" for of in ("batch", "token", "head"))]
 
 
 class fira_block_norm_desc(ctypes.Structure):

@@ -17,6 +17,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
@@ -311,21 +312,61 @@ class BlockNormGradients(NamedTuple):
     dpost_bias: Optional[torch.Tensor]
 
 
-def _block_desc(x, block, vectors, norm, post, eps, post_eps, residual_scale, block_scale):
-    """Checks what both calls have in common -> (descriptor, pointers of the vectors); vectors: gate, weight, bias, post_weight, post_bias."""
-    if block.shape != x.shape:
-        _refuse(FIRA_ERR_SHAPE, f"the block is {tuple(block.shape)} for a stream of {tuple(x.shape)}")
+def _block_desc(x, block, gate, weight, bias, post_weight, post_bias, norm, post, eps, post_eps, residual_scale, block_scale):
+    """Checks what both calls have in common -> (descriptor, pointers of the vectors, their type or None)."""
+    shape = x.shape
+    if block.shape != shape:
+        _refuse(FIRA_ERR_SHAPE, f"the block is {tuple(block.shape)} for a stream of {tuple(shape)}")
     dt = _dtype(x.dtype, "stream")
     if block.dtype != x.dtype:
         _refuse(FIRA_ERR_DTYPE, "the block is not of the stream's type")
-    if norm == fira.FIRA_NO_NORM and (vectors[1] is not None or vectors[2] is not None):
+    if norm == fira.FIRA_NO_NORM and (weight is not None or bias is not None):
         _refuse(FIRA_ERR_INVALID_ARG, "weight or bias without a norm")
-    if post == fira.FIRA_NO_NORM and (vectors[3] is not None or vectors[4] is not None):
+    if post == fira.FIRA_NO_NORM and (post_weight is not None or post_bias is not None):
         _refuse(FIRA_ERR_INVALID_ARG, "post_weight or post_bias without a post norm")
-    dim = x.shape[-1]
-    at = fira.fira_block_norm_params(*(_vector(t, dim, name) for t, name in zip(vectors, ("gate", "weight", "bias", "post_weight", "post_bias"))))
-    rows = x.numel() // dim if dim else 0
-    return fira.fira_block_norm_desc(rows, dim, dt, _param_dtype(dt, *vectors), norm, post, eps, post_eps, residual_scale, block_scale), at
+    dim = shape[-1]
+    pdt = _param_dtype(dt, gate, weight, bias, post_weight, post_bias)
+    at = fira.fira_block_norm_params(_vector(gate, dim, "gate"), _vector(weight, dim, "weight"), _vector(bias, dim, "bias"), _vector(post_weight, dim, "post_weight"),
+                                     _vector(post_bias, dim, "post_bias"))
+    return fira.fira_block_norm_desc(x.numel() // dim if dim else 0, dim, dt, pdt, norm, post, eps, post_eps, residual_scale, block_scale), at
+
+
+def _pointer(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _statistics(x, kind, dev):
+    """-> (mean, rstd) of a norm, uninitialised; None for what it has not"""
+    if kind == fira.FIRA_NO_NORM:
+        return None, None
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    return torch.empty_like(rstd) if kind == fira.FIRA_LAYER_NORM else None, rstd
+
+
+def _check_statistics(x, kind, mean, rstd, name):
+    """-> (mean, rstd) as the library wants them"""
+    if kind == fira.FIRA_NO_NORM:
+        return None, None
+    if kind != fira.FIRA_LAYER_NORM:
+        mean = None
+    for t, wanted in ((rstd, True), (mean, kind == fira.FIRA_LAYER_NORM)):
+        if wanted and (t is None or t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous()):
+            _refuse(FIRA_ERR_SHAPE, f"the {name}'s statistics are not dense fp32 tensors of {tuple(x.shape[:-1])}")
+    return mean, rstd
+
+
+def _vector_gradient(given, wanted, like, dim, dtype, dev, accumulate, name):
+    if not wanted:
+        if given is not None:
+            _refuse(FIRA_ERR_INVALID_ARG, f"{name} of a vector that is not there")
+        return None
+    if given is None:
+        if accumulate:
+            _refuse(FIRA_ERR_INVALID_ARG, f"accumulate without {name}")
+        return torch.empty(dim, dtype=dtype, device=dev) if like is None else torch.empty_like(like)
+    if given.shape != (dim,) or given.dtype != dtype or not given.is_contiguous():
+        _refuse(FIRA_ERR_SHAPE, f"{name} is not a dense vector of {dim} of {dtype}")
+    return given
 
 
 def fira_block_norm(x: torch.Tensor, block: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
@@ -338,9 +379,8 @@ def fira_block_norm(x: torch.Tensor, block: torch.Tensor, weight: Optional[torch
     lib = fira.load_library()
     if x.dim() < 1:
         _refuse(FIRA_ERR_SHAPE, "x has no dimension")
-    vectors = (gate, weight, bias, post_weight, post_bias)
-    dev = _device(x, block, *vectors, out, y_out)
-    d, at = _block_desc(x, block, vectors, norm, post, eps, eps if post_eps is None else post_eps, residual_scale, block_scale)
+    dev = _device(x, block, gate, weight, bias, post_weight, post_bias, out, y_out)
+    d, at = _block_desc(x, block, gate, weight, bias, post_weight, post_bias, norm, post, eps, eps if post_eps is None else post_eps, residual_scale, block_scale)
     if norm == fira.FIRA_NO_NORM and y_out is not None:
         _refuse(FIRA_ERR_INVALID_ARG, "y_out without a norm")
     elsewhere = _elsewhere(dev, stream)
@@ -352,11 +392,11 @@ def fira_block_norm(x: torch.Tensor, block: torch.Tensor, weight: Optional[torch
     block, ld_block = _input(block)
     out, ld_r = _result(out, x.shape, x.dtype, dev, "out", like=x)
     y, ld_y = (None, 0) if norm == fira.FIRA_NO_NORM else _result(y_out, x.shape, x.dtype, dev, "y_out", like=x)
-    stat = lambda wanted: torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if wanted else None  # noqa: E731
-    stats = [stat(wanted) for kind in (norm, post) for wanted in (kind == fira.FIRA_LAYER_NORM, kind != fira.FIRA_NO_NORM)]
-    _check(lib.fira_block_norm(d, x.data_ptr(), ld_x, block.data_ptr(), ld_block, at, out.data_ptr(), ld_r, None if y is None else y.data_ptr(), ld_y,
-                               *(None if s is None else s.data_ptr() for s in stats), _stream(dev)))
-    return BlockNorm(out, y, *stats)
+    mean, rstd = _statistics(x, norm, dev)
+    post_mean, post_rstd = _statistics(x, post, dev)
+    _check(lib.fira_block_norm(d, x.data_ptr(), ld_x, block.data_ptr(), ld_block, at, out.data_ptr(), ld_r, _pointer(y), ld_y, _pointer(mean), _pointer(rstd), _pointer(post_mean),
+                               _pointer(post_rstd), _stream(dev)))
+    return BlockNorm(out, y, mean, rstd, post_mean, post_rstd)
 
 
 def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[torch.Tensor], residual: torch.Tensor, block: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -373,9 +413,8 @@ def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[tor
     lib = fira.load_library()
     if residual.dim() < 1:
         _refuse(FIRA_ERR_SHAPE, "residual has no dimension")
-    vectors = (gate, weight, None, post_weight, post_bias)
-    dev = _device(residual, block, dresidual, dy, *vectors, mean, rstd, post_mean, post_rstd, dx, dblock, dweight, dbias, dgate, dpost_weight, dpost_bias)
-    d, at = _block_desc(residual, block, vectors, norm, post, 0.0, 0.0, residual_scale, block_scale)
+    dev = _device(residual, block, dresidual, dy, gate, weight, post_weight, post_bias, mean, rstd, post_mean, post_rstd, dx, dblock, dweight, dbias, dgate, dpost_weight, dpost_bias)
+    d, at = _block_desc(residual, block, gate, weight, None, post_weight, post_bias, norm, post, 0.0, 0.0, residual_scale, block_scale)
     for t, name in ((dresidual, "dresidual"), (dy, "dy")):
         if t is not None and (t.shape != residual.shape or t.dtype != residual.dtype):
             _refuse(FIRA_ERR_SHAPE, f"{name} is {tuple(t.shape)} of {t.dtype} for a stream of {tuple(residual.shape)} of {residual.dtype}")
@@ -383,19 +422,10 @@ def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[tor
         _refuse(FIRA_ERR_INVALID_ARG, "dy without a norm, or a norm without dy")
     if bias and norm == fira.FIRA_NO_NORM:
         _refuse(FIRA_ERR_INVALID_ARG, "bias without a norm")
-    for kind, m, r, name in ((norm, mean, rstd, ""), (post, post_mean, post_rstd, "post_")):
-        for t, wanted, what in ((m, kind == fira.FIRA_LAYER_NORM, "mean"), (r, kind != fira.FIRA_NO_NORM, "rstd")):
-            if wanted and (t is None or t.dtype != torch.float32 or t.shape != residual.shape[:-1] or not t.is_contiguous()):
-                _refuse(FIRA_ERR_SHAPE, f"{name}{what} is not a dense fp32 tensor of {tuple(residual.shape[:-1])}")
-    wanted = (gate is not None, weight is not None, bias, post_weight is not None, post_bias is not None)
-    given = (dgate, dweight, dbias, dpost_weight, dpost_bias)
-    ptype = next((t.dtype for t in vectors if t is not None), None) or (dbias.dtype if dbias is not None else residual.dtype)
-    d.param_dtype = _dtype(ptype, "parameter")
-    for w, t, name in zip(wanted, given, ("dgate", "dweight", "dbias", "dpost_weight", "dpost_bias")):
-        if t is not None and not w:
-            _refuse(FIRA_ERR_INVALID_ARG, f"{name} of a vector that is not there")
-        if accumulate and w and t is None:
-            _refuse(FIRA_ERR_INVALID_ARG, f"accumulate without {name}")
+    mean, rstd = _check_statistics(residual, norm, mean, rstd, "norm")
+    post_mean, post_rstd = _check_statistics(residual, post, post_mean, post_rstd, "post norm")
+    if gate is None and weight is None and post_weight is None and post_bias is None and dbias is not None:
+        d.param_dtype = _dtype(dbias.dtype, "parameter")
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
         with elsewhere:
@@ -409,15 +439,17 @@ def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[tor
     dy, ld_dy = (None, 0) if dy is None else _input(dy)
     dx, ld_dx = _result(dx, residual.shape, residual.dtype, dev, "dx", like=residual)
     dblock, ld_db = _result(dblock, residual.shape, residual.dtype, dev, "dblock", like=residual)
-    dim = residual.shape[-1]
-    grads = [_result(t, (dim,), ptype, dev, "a vector's gradient")[0] if w else None for w, t in zip(wanted, given)]
-    to = fira.fira_block_norm_params(*(_vector(t, dim, "a vector's gradient") for t in grads))
+    dim, ptype = residual.shape[-1], torch.float32 if d.param_dtype == FIRA_F32 else torch.bfloat16
+    dgate = _vector_gradient(dgate, gate is not None, gate, dim, ptype, dev, accumulate, "dgate")
+    dweight = _vector_gradient(dweight, weight is not None, weight, dim, ptype, dev, accumulate, "dweight")
+    dbias = _vector_gradient(dbias, bias, weight, dim, ptype, dev, accumulate, "dbias")
+    dpost_weight = _vector_gradient(dpost_weight, post_weight is not None, post_weight, dim, ptype, dev, accumulate, "dpost_weight")
+    dpost_bias = _vector_gradient(dpost_bias, post_bias is not None, post_bias, dim, ptype, dev, accumulate, "dpost_bias")
+    to = fira.fira_block_norm_params(_pointer(dgate), _pointer(dweight), _pointer(dbias), _pointer(dpost_weight), _pointer(dpost_bias))
     workspace = _workspace(workspace, lib.fira_block_norm_gradient_workspace_bytes(d), dev)
-    pointer = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    stats = (mean if norm == fira.FIRA_LAYER_NORM else None, rstd, post_mean if post == fira.FIRA_LAYER_NORM else None, post_rstd)
-    _check(lib.fira_block_norm_gradient(d, pointer(dresidual), ld_dr, pointer(dy), ld_dy, residual.data_ptr(), ld_r, block.data_ptr(), ld_b, at, *map(pointer, stats),
-                                        dx.data_ptr(), ld_dx, dblock.data_ptr(), ld_db, to, bool(accumulate), workspace.data_ptr(), workspace.numel(), _stream(dev)))
-    dgate, dweight, dbias, dpost_weight, dpost_bias = grads
+    _check(lib.fira_block_norm_gradient(d, _pointer(dresidual), ld_dr, _pointer(dy), ld_dy, residual.data_ptr(), ld_r, block.data_ptr(), ld_b, at, _pointer(mean), _pointer(rstd),
+                                        _pointer(post_mean), _pointer(post_rstd), dx.data_ptr(), ld_dx, dblock.data_ptr(), ld_db, to, bool(accumulate), workspace.data_ptr(),
+                                        workspace.numel(), _stream(dev)))
     return BlockNormGradients(dx, dblock, dweight, dbias, dgate, dpost_weight, dpost_bias)
 
 
@@ -451,8 +483,10 @@ def fira_rotary_gradient(dq: torch.Tensor, dk: Optional[torch.Tensor], positions
 def _heads(t: torch.Tensor):
     """Strides of sequences, tokens and heads of t, or None if it has no such."""
     shape, strides = t.shape, t.stride()
-    if shape[-1] > 1 and strides[-1] != 1:
+    if strides[-1] != 1 and shape[-1] > 1:
         return None
+    if len(shape) == 4:
+        return strides[:3]
     batch = 0
     need = None            # stride that the next dimension outwards has to have
     for size, stride in zip(reversed(shape[:-3]), reversed(strides[:-3])):
@@ -466,26 +500,29 @@ def _heads(t: torch.Tensor):
     return batch, strides[-3], strides[-2]
 
 
+_ONE_OR_TWO = [None, fira.fira_rotary_heads * 1, fira.fira_rotary_heads * 2]
+
+
 def _rotary(name, q, k, positions, frequencies, interleaved, scale, q_out, k_out, stream):
     lib = fira.load_library()
+    shape = q.shape
     if k is None and k_out is not None:
         _refuse(FIRA_ERR_INVALID_ARG, "k_out without k")
-    for t in (q, k):
-        if t is not None and (t.dim() < 3 or t.shape[:-2] != q.shape[:-2] or t.shape[-1] != q.shape[-1]):
-            _refuse(FIRA_ERR_SHAPE, f"queries are {tuple(q.shape)}, keys {None if k is None else tuple(k.shape)}")
+    if len(shape) < 3 or (k is not None and (k.dim() < 3 or k.shape[:-2] != shape[:-2] or k.shape[-1] != shape[-1])):
+        _refuse(FIRA_ERR_SHAPE, f"queries are {tuple(shape)}, keys {None if k is None else tuple(k.shape)}")
     dev = _device(q, k, positions, frequencies, q_out, k_out)
     dt = _dtype(q.dtype, "q")
     if k is not None and k.dtype != q.dtype:
         _refuse(FIRA_ERR_DTYPE, "k is not of q's type")
     if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
         _refuse(FIRA_ERR_DTYPE, "frequencies are not a dense fp64 vector")
-    length, (heads, dim) = q.shape[-3], q.shape[-2:]
+    length = shape[-3]
     stride = 0
     if positions is not None:
         if positions.dtype not in _IDS:
             _refuse(FIRA_ERR_DTYPE, "positions are neither int32 nor int64")
-        if positions.shape != q.shape[:-2] and positions.shape != (length,):
-            _refuse(FIRA_ERR_SHAPE, f"positions are {tuple(positions.shape)} for tokens of {tuple(q.shape[:-2])}")
+        if positions.shape != shape[:-2] and positions.shape != (length,):
+            _refuse(FIRA_ERR_SHAPE, f"positions are {tuple(positions.shape)} for tokens of {tuple(shape[:-2])}")
         stride = length if positions.dim() > 1 else 0
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
@@ -493,32 +530,34 @@ def _rotary(name, q, k, positions, frequencies, interleaved, scale, q_out, k_out
             return _rotary(name, q, k, positions, frequencies, interleaved, scale, q_out, k_out, None)
     if positions is not None:
         positions = positions.contiguous()
-    rows = fira.fira_rotary_heads * (1 if k is None else 2)
-    h, outs, keep = rows(), [], []
-    for i, (x, given) in enumerate(((q, q_out), (k, k_out))):
-        if x is None:
-            outs.append(None)
-            continue
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev) if given is None else given
+    q, q_out, heads = _turned(q, q_out)
+    if k is None:
+        h = _ONE_OR_TWO[1](heads)
+    else:
+        k, k_out, more = _turned(k, k_out)
+        h = _ONE_OR_TWO[2](heads, more)
+    batch = shape[0] if len(shape) == 4 else math.prod(shape[:-3])
+    d = fira.fira_rotary_desc(batch, length, shape[-1], 2 * frequencies.shape[0], dt, interleaved and 1 or 0, FIRA_I64 if positions is None else _IDS[positions.dtype], stride, scale)
+    _check(getattr(lib, name)(d, h, len(h), frequencies.data_ptr(), None if positions is None else positions.data_ptr(), _stream(dev)))
+    return q_out, k_out
+
+
+def _turned(x, out):
+    """-> (x, copied if it has to be, its result, the descriptor of both)"""
+    at = _heads(x)
+    if at is None:
+        x = x.contiguous()
+        at = _heads(x)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        to = _heads(out) if not at[0] or not x.is_contiguous() else at
+    else:
         if out.shape != x.shape or out.dtype != x.dtype:
-            _refuse(FIRA_ERR_SHAPE, f"result {i} is {tuple(out.shape)} of {out.dtype}, not {tuple(x.shape)} of {x.dtype}")
+            _refuse(FIRA_ERR_SHAPE, f"a result is {tuple(out.shape)} of {out.dtype}, not {tuple(x.shape)} of {x.dtype}")
         to = _heads(out)
         if to is None:
-            _refuse(FIRA_ERR_SHAPE, f"result {i} has no strides of sequences, tokens and heads")
-        at = _heads(x)
-        if at is None:
-            x = x.contiguous()
-            at = _heads(x)
-        keep.append(x)
-        h[i] = fira.fira_rotary_heads(x.data_ptr(), out.data_ptr(), x.shape[-2], (ctypes.c_int64 * 3)(*at), (ctypes.c_int64 * 3)(*to))
-        outs.append(out)
-    batch = 1
-    for n in q.shape[:-3]:
-        batch *= n
-    d = fira.fira_rotary_desc(batch, length, dim, 2 * frequencies.shape[0], dt, fira.FIRA_ROTARY_INTERLEAVED if interleaved else fira.FIRA_ROTARY_HALVES,
-                              FIRA_I64 if positions is None else _IDS[positions.dtype], stride, scale)
-    _check(getattr(lib, name)(d, h, len(h), frequencies.data_ptr(), None if positions is None else positions.data_ptr(), _stream(dev)))
-    return outs[0], outs[1]
+            _refuse(FIRA_ERR_SHAPE, "a result has no strides of sequences, tokens and heads")
+    return x, out, fira.fira_rotary_heads(x.data_ptr(), out.data_ptr(), x.shape[-2], *at, *to)
 
 
 class GradientList:

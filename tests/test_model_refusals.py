@@ -58,8 +58,7 @@ def test_adamw_lists_of_cpu_tensors():
 def test_rotary(lib):
     desc = lambda batch=2, length=3, dim=16, rotated=8, dtype=0, layout=0, position_type=1, position_stride=3, scale=1.0: fira.fira_rotary_desc(  # noqa: E731
         batch, length, dim, rotated, dtype, layout, position_type, position_stride, scale)
-    strides = ctypes.c_int64 * 3
-    heads = lambda x=P, y=ctypes.c_void_p(8192), n=4, xs=(192, 64, 16), ys=(192, 64, 16): (fira.fira_rotary_heads * 1)(fira.fira_rotary_heads(x, y, n, strides(*xs), strides(*ys)))  # noqa: E731
+    heads = lambda x=P, y=ctypes.c_void_p(8192), n=4, xs=(192, 64, 16), ys=(192, 64, 16): (fira.fira_rotary_heads * 1)(fira.fira_rotary_heads(x, y, n, *xs, *ys))  # noqa: E731
     for call in (lib.fira_rotary, lib.fira_rotary_gradient):
         for d, want in ((None, -1), (desc(batch=-1), -2), (desc(length=-1), -2), (desc(batch=1 << 20, length=1 << 20), -2), (desc(dim=0), -2), (desc(dim=(1 << 16) + 1), -2), (desc(rotated=0), -2),
                         (desc(rotated=7), -2), (desc(rotated=18), -2), (desc(dtype=2), -4), (desc(position_type=2), -4), (desc(layout=2), -1), (desc(scale=math.nan), -1), (desc(scale=1e60), -1),
