@@ -18,7 +18,7 @@ struct FiraAdamSpan {
   int tile0;               // first tile of this piece
   int stream;              // results that begin at whole lines, and go past the caches: 1 weights, 2 states
 };
-constexpr int kAdamSpans = 36;        // a launch's pieces travel as kernel arguments, of which there are 4 KB
+constexpr int kAdamSpans = 36;        // (a lane for each.)  A launch's pieces travel as kernel arguments, of which there are 4 KB
 // Vectors of a thread that are on their way together, and workgroups of a launch at most: with states in 8 bits a value has five times the arithmetic a byte.
 // us with one vector and 4096 workgroups, two and 16384: 60m 298 and 269, embeddings in 8 bits 276 and 288, 511 x 1377 and the like in 8 bits with rows apart 60 and 72.
 template <bool EIGHT>
@@ -47,13 +47,14 @@ struct FiraAdamFactors {
   unsigned t;
   long long taken;
 };
-__device__ __forceinline__ FiraAdamFactors adam_factors(const FiraAdamHp& hp, const float* lr, const float* norm, long long taken) {
-  FiraAdamFactors f;
-  const double t = (double)(taken + 1);
-  f.lr = lr ? (double)*as_global(lr) : hp.lr;
+// Called by two lanes or more: one for each beta.
+__device__ __forceinline__ void adam_factors(FiraAdamFactors& f, const FiraAdamHp& hp, const float* lr, const float* norm, long long taken) {
   // (1 - b^t, without the cancellation of a beta next to one)
-  f.m = (float)(f.lr / -expm1(t * hp.log_beta1));
-  f.v = (float)(1.0 / sqrt(-expm1(t * hp.log_beta2)));
+  const double rest = -expm1((double)(taken + 1) * (threadIdx.x ? hp.log_beta2 : hp.log_beta1));
+  if (threadIdx.x == 1) f.v = (float)(1.0 / sqrt(rest));
+  if (threadIdx.x) return;
+  f.lr = lr ? (double)*as_global(lr) : hp.lr;
+  f.m = (float)(f.lr / rest);
   f.cut = 1.0f;
   if (norm) {
     const float x = *as_global(norm);
@@ -61,7 +62,6 @@ __device__ __forceinline__ FiraAdamFactors adam_factors(const FiraAdamHp& hp, co
   }
   f.t = (unsigned)(taken + 1);
   f.taken = taken;
-  return f;
 }
 
 // A hash of 32 bits; the constants are the fractions of the roots of two and three.
@@ -420,14 +420,13 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
   constexpr int W = kAdamWidth<T, R, EIGHT>, TILE = 256 * W * kAdamUnroll<EIGHT>;
   __shared__ FiraAdamFactors shared;
   // (the other wavefronts' first loads are on their way meanwhile)
-  if (threadIdx.x == 0) shared = adam_factors(hp, lr, norm, *as_global(counter));
+  if (threadIdx.x < 2) adam_factors(shared, hp, lr, norm, *as_global(counter));
   bool ready = false;
   FiraAdamFactors f;
-  int k = 0;
+  const int lane = threadIdx.x & 63, begins = lane < l.count ? l.s[lane].tile0 : 0x7fffffff;
 #pragma unroll 1
   for (int tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
-    while (k + 1 < l.count && l.s[k + 1].tile0 <= tile) ++k;
-    k = __builtin_amdgcn_readfirstlane(k);
+    const int k = __builtin_amdgcn_readfirstlane(__popcll(__ballot(begins <= tile)) - 1);      // the last piece that does not begin after the tile
     const FiraAdamSpan& s = l.s[k];
     const unsigned first = (unsigned)(tile - s.tile0) * TILE;
     // vectors that are on their way together: one where there are ends to look for, which take registers and branches

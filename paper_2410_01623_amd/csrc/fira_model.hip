@@ -233,6 +233,23 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
   return v;
 }
 
+// Calls f with the constants that a row of `dim` <= MOST values is held by, as with_row_shape; in steps of less than a factor of two above 2048, where lanes without a value
+// cost most (2049 columns: XX).  FORWARD: 16 values a thread where that is enough.
+template <typename T, bool FORWARD, typename F>
+void with_block_shape(int64_t dim, F f) {
+  constexpr int W = kWidth<T>, N = 8 / W;
+  if (dim <= 2048) with_row_shape<T, FORWARD ? 16 : 8>(dim, f);
+  else if (dim <= 2560) f(Int<W>{}, Int<320>{}, Int<N>{});
+  else if (dim <= 3584) f(Int<W>{}, Int<448>{}, Int<N>{});
+  else if (dim <= 4096) f(Int<W>{}, Int<FORWARD ? 256 : 512>{}, Int<FORWARD ? 2 * N : N>{});
+  else if (dim <= 5120) f(Int<W>{}, Int<320>{}, Int<2 * N>{});
+  else if (dim <= 6144) f(Int<W>{}, Int<384>{}, Int<2 * N>{});
+  else if (dim <= 7168) f(Int<W>{}, Int<448>{}, Int<2 * N>{});
+  else if (!FORWARD || dim <= 8192) f(Int<W>{}, Int<512>{}, Int<2 * N>{});
+  else if constexpr (FORWARD) f(Int<W>{}, Int<1024>{}, Int<2 * N>{});
+}
+static_assert(kBlockWidest == 8192 && kNormWidest == 16384, "shapes");
+
 // Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
 // As many as the chip holds at a time or somewhat fewer, by what was measured, and fewer where that leaves each less than ten turns (of a row, or of the rows that it has side
 // by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with 768, 1024 and 1536: 16385 x 2049 f32
@@ -240,12 +257,12 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
 int64_t block_parts(const fira_block_norm_desc* d) {
   if (d->dim > kBlockWidest) return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64));
   const bool lean = d->norm != FIRA_LAYER_NORM && d->post != FIRA_LAYER_NORM, f32 = d->dtype == FIRA_F32;
-  int64_t threads = kBlockWidest / 16, side = 1;
+  int64_t threads = 0, side = 1;
   auto shape = [&](auto, auto t, auto) {
     threads = std::max(256, decltype(t)::value);
     side = std::max(1, 256 / decltype(t)::value);
   };
-  if (d->dim <= kBlockWidest / 2) f32 ? with_row_shape<FiraStoredF32, 8>(d->dim, shape) : with_row_shape<FiraStoredBf16, 8>(d->dim, shape);
+  f32 ? with_block_shape<FiraStoredF32, false>(d->dim, shape) : with_block_shape<FiraStoredBf16, false>(d->dim, shape);
   const int64_t held = d->dim > kBlockWidest / 2 ? 512 : f32 && d->dim > 256 ? (lean ? 1024 : 512) : lean || f32 ? 1024 : 768;
   const int64_t full = 256 * std::max<int64_t>(1, held / threads), turns = std::max<int64_t>(1, (d->rows + side - 1) / side);
   const int64_t each = std::min(std::max<int64_t>(10, (turns + full - 1) / full), (4 * turns + full - 1) / full);
@@ -356,7 +373,7 @@ fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, in
                          (raw*)dev_residual, (raw*)dev_y, to);
       return;
     }
-    with_row_shape<T, 16>(d->dim, [&](auto width, auto threads, auto nv) {
+    with_block_shape<T, true>(d->dim, [&](auto width, auto threads, auto nv) {
       constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
       hipLaunchKernelGGL((fira_block_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)), dim3(std::max(256, THREADS)), 0, q, n,
                          (const raw*)dev_x, (const raw*)dev_block, v, (raw*)dev_residual, (raw*)dev_y, to);
@@ -447,10 +464,7 @@ fira_status fira_block_norm_gradient(const fira_block_norm_desc* d, const void* 
                              (raw*)dev_dx, (raw*)dev_dblock, partial, wanted);
         });
       };
-      if (d->dim > kBlockWidest / 2) launch(Int<kWidth<T>>{}, Int<kBlockWidest / 16>{}, Int<16 / kWidth<T>>{});
-      else with_row_shape<T, 8>(d->dim, [&](auto width, auto threads, auto nv) {
-        if constexpr (decltype(threads)::value <= 512) launch(width, threads, nv);
-      });
+      with_block_shape<T, false>(d->dim, launch);
     }
     if (sums) hipLaunchKernelGGL(fira_block_norm_join_kernel<P>, dim3((d->dim + 15) / 16), dim3(256), 0, q, n, (const float*)partial, d->rows ? parts : 0, wanted, v, to, accumulate);
   });
