@@ -201,7 +201,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
   const int me = GROUPS == 1 ? threadIdx.x : threadIdx.x % THREADS, group = GROUPS == 1 ? 0 : threadIdx.x / THREADS;   // (a row of a workgroup has a scalar address)
   const float dim = (float)n.dim;
   const bool pre = n.norm != kNone, post = n.post != kNone, block = b != nullptr;
-  float wf[NV][W], qf[NV][W];                            // w, and alpha gate pw
+  // w, and alpha gate pw, of a thread's columns: in LDS, as the registers decide how many workgroups a compute unit holds (16385 x 2500 bf16, with means, 175 us with them
+  // there and 114 here)
+  constexpr int F = W < 4 ? W : 4, K = W / F;
+  __shared__ __attribute__((aligned(16))) float factors[2][NV][K][THREADS][F];
+  auto factor = [&](int which, int v, int j) { return factors[which][v][j / F][me][j % F]; };
   int skip[NV];                                          // values of a vector that are not this thread's
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
@@ -210,13 +214,15 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
     if (vec.w) w.load(vec.w + c.at);
     if (vec.gate) g.load(vec.gate + c.at);
     if (vec.pw) pw.load(vec.pw + c.at);
+    if (!group)
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      wf[v][j] = vec.w ? w.get(j) : 1.0f;
-      qf[v][j] = n.alpha * (vec.gate ? g.get(j) : 1.0f) * (vec.pw ? pw.get(j) : 1.0f);
-    }
+      for (int j = 0; j < W; ++j) {
+        factors[0][v][j / F][me][j % F] = vec.w ? w.get(j) : 1.0f;
+        factors[1][v][j / F][me][j % F] = n.alpha * (vec.gate ? g.get(j) : 1.0f) * (vec.pw ? pw.get(j) : 1.0f);
+      }
     skip[v] = v < NV / 2 ? 0 : c.any ? c.skip : W;
   }
+  if (GROUPS > 1) __syncthreads();                       // (else a thread's own)
   float s0[NV][W] = {}, s2[NV][W] = {}, s1[LEAN ? 1 : NV][W] = {}, s3[LEAN ? 1 : NV][W] = {};
   BlockRowHeld<T, W, NV> x;
   auto load = [&](long long row) {
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
       auto dy_of = [&](int v, int j) { return here ? x.dy[v].get(j) : 0.0f; };
       float a1, a2;
       row_total(a1, a2, [&](int v, int j, float& a, float& b) {
-        const float g = dy_of(v, j) * wf[v][j];
+        const float g = dy_of(v, j) * factor(0, v, j);
         if (!LEAN) a += g;
         b = __builtin_fmaf(g, hr(v, j), b);
       });
@@ -287,7 +293,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
         for (int j = 0; j < W; ++j) {
           const float d = dy_of(v, j), h = hr(v, j);
           s0[v][j] = __builtin_fmaf(d, h, s0[v][j]);
-          t[v][j] = __builtin_fmaf(x.rs, d * wf[v][j] - __builtin_fmaf(h, a2, a1), t[v][j]);
+          t[v][j] = __builtin_fmaf(x.rs, d * factor(0, v, j) - __builtin_fmaf(h, a2, a1), t[v][j]);
         }
       if (!LEAN && sums & 2)
 #pragma unroll
@@ -312,7 +318,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
       for (int j = 0; j < W; ++j) o[j] = n.beta * t[v][j];
       if (dx) put(dx, n.ld_dx, v, o);
 #pragma unroll
-      for (int j = 0; j < W; ++j) t[v][j] *= qf[v][j];
+      for (int j = 0; j < W; ++j) t[v][j] *= factor(1, v, j);
     }
     if (!db) return;
     float q1 = 0.0f, q2 = 0.0f;

@@ -234,7 +234,7 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
 }
 
 // Calls f with the constants that a row of `dim` <= MOST values is held by, as with_row_shape; in steps of less than a factor of two above 2048, where lanes without a value
-// cost most (2049 columns: XX).  FORWARD: 16 values a thread where that is enough.
+// cost most (8192 x 4100 bf16 forward 70 us with powers of two, 57 with these).  FORWARD: 16 values a thread where that is enough.
 template <typename T, bool FORWARD, typename F>
 void with_block_shape(int64_t dim, F f) {
   constexpr int W = kWidth<T>, N = 8 / W;
@@ -253,7 +253,8 @@ static_assert(kBlockWidest == 8192 && kNormWidest == 16384, "shapes");
 // Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
 // As many as the chip holds at a time or somewhat fewer, by what was measured, and fewer where that leaves each less than ten turns (of a row, or of the rows that it has side
 // by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with 768, 1024 and 1536: 16385 x 2049 f32
-// 188, 158 and 169, with means and biases (512, 768, 1024) 215, 215 and 224; 131072 x 256 bf16 with those (768, 1024, 1536) 84, 94 and 94.
+// 188, 158 and 169, with means and biases (512, 768, 1024) 215, 215 and 224; 131072 x 256 bf16 with those (768, 1024, 1536) 84, 94 and 94, and 32768 x 4096 with one
+// workgroup a compute unit and two 372 and 294.
 int64_t block_parts(const fira_block_norm_desc* d) {
   if (d->dim > kBlockWidest) return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64));
   const bool lean = d->norm != FIRA_LAYER_NORM && d->post != FIRA_LAYER_NORM, f32 = d->dtype == FIRA_F32;
@@ -264,7 +265,7 @@ int64_t block_parts(const fira_block_norm_desc* d) {
   };
   f32 ? with_block_shape<FiraStoredF32, false>(d->dim, shape) : with_block_shape<FiraStoredBf16, false>(d->dim, shape);
   const int64_t held = d->dim > kBlockWidest / 2 ? 512 : f32 && d->dim > 256 ? (lean ? 1024 : 512) : lean || f32 ? 1024 : 768;
-  const int64_t full = 256 * std::max<int64_t>(1, held / threads), turns = std::max<int64_t>(1, (d->rows + side - 1) / side);
+  const int64_t full = 256 * std::max<int64_t>(f32 || lean || d->dim > kBlockWidest / 2 ? 1 : 2, held / threads), turns = std::max<int64_t>(1, (d->rows + side - 1) / side);
   const int64_t each = std::min(std::max<int64_t>(10, (turns + full - 1) / full), (4 * turns + full - 1) / full);
   return (turns + each - 1) / each;
 }
