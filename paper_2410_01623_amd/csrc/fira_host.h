@@ -1,4 +1,4 @@
-// What the host sides of the operators around the step share: refusals, checks of pointers and sizes, types and row shapes as constants.
+// What the host sides of the operators around the step share: refusals, checks of pointers and sizes, types as constants.
 // No state, no allocation, nothing that throws.
 #pragma once
 #include "../../include/fira.h"
@@ -12,7 +12,7 @@
 #include <type_traits>
 
 #include "fira_error.h"
-#include "fira_layer_norm.h"
+#include "fira_rows.h"
 
 namespace {
 
@@ -72,24 +72,6 @@ template <typename F>
 void with_flag(bool flag, F f) {
   if (flag) f(std::true_type{});
   else f(std::false_type{});
-}
-
-// Calls f with the constants that a row of `dim` <= kNormWidest values of type T is held by: values of a vector, threads, vectors of a thread.
-// EACH: values of a thread where a row takes more than a wavefront, 8 or 16.
-template <typename T, int EACH, typename F>
-void with_row_shape(int64_t dim, F f) {
-  constexpr int W = kWidth<T>, N = 8 / W, D = EACH / 8;
-  if (dim < kMostWidth) f(Int<1>{}, Int<8>{}, Int<1>{});
-  else if (dim <= 8 * W) f(Int<W>{}, Int<8>{}, Int<1>{});
-  else if (dim <= 16 * W) f(Int<W>{}, Int<16>{}, Int<1>{});
-  else if (dim <= 32 * W) f(Int<W>{}, Int<32>{}, Int<1>{});
-  else if (dim <= 64 * W) f(Int<W>{}, Int<64>{}, Int<1>{});
-  else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
-  else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
-  else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
-  else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
-  else if (dim <= 8192) f(Int<W>{}, Int<1024 / D>{}, Int<D * N>{});
-  else f(Int<W>{}, Int<1024>{}, Int<2 * N>{});
 }
 
 }  // namespace

@@ -233,15 +233,23 @@ FiraBlockVectors<P> block_vectors(const fira_block_norm_desc* d, const fira_bloc
   return v;
 }
 
-// Calls f with the constants that a row of `dim` <= MOST values is held by, as with_row_shape; in steps of less than a factor of two above 2048, where lanes without a value
-// cost most (8192 x 4100 bf16 forward 70 us with powers of two, 57 with these).  FORWARD: 16 values a thread where that is enough.
+// Calls f with the constants that a row is held by: values of a vector, threads, vectors of a thread.  FORWARD: up to kNormWidest values, 16 a thread where a row takes more
+// than a wavefront; else up to kBlockWidest, 8 a thread and 16 from 4097 on.  Steps above 2048 are less than a factor of two, since lanes without a value cost most there
+// (8192 x 4100 bf16 forward 70 us with powers of two, 57 with these).
 template <typename T, bool FORWARD, typename F>
 void with_block_shape(int64_t dim, F f) {
-  constexpr int W = kWidth<T>, N = 8 / W;
-  if (dim <= 2048) with_row_shape<T, FORWARD ? 16 : 8>(dim, f);
+  constexpr int W = kWidth<T>, N = 8 / W, D = FORWARD ? 2 : 1;
+  if (dim < kMostWidth) f(Int<1>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 8 * W) f(Int<W>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 16 * W) f(Int<W>{}, Int<16>{}, Int<1>{});
+  else if (dim <= 32 * W) f(Int<W>{}, Int<32>{}, Int<1>{});
+  else if (dim <= 64 * W) f(Int<W>{}, Int<64>{}, Int<1>{});
+  else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
+  else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
+  else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
   else if (dim <= 2560) f(Int<W>{}, Int<320>{}, Int<N>{});
   else if (dim <= 3584) f(Int<W>{}, Int<448>{}, Int<N>{});
-  else if (dim <= 4096) f(Int<W>{}, Int<FORWARD ? 256 : 512>{}, Int<FORWARD ? 2 * N : N>{});
+  else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
   else if (dim <= 5120) f(Int<W>{}, Int<320>{}, Int<2 * N>{});
   else if (dim <= 6144) f(Int<W>{}, Int<384>{}, Int<2 * N>{});
   else if (dim <= 7168) f(Int<W>{}, Int<448>{}, Int<2 * N>{});

@@ -61,6 +61,23 @@ fira_status check_norm(const fira_layer_norm_desc* d) {
   return FIRA_OK;
 }
 
+// Calls f with the constants that a row of `dim` <= kNormWidest values of type T is held by: values of a vector, threads, vectors of a thread.
+// EACH: values of a thread where a row takes more than a wavefront, 8 or 16.
+template <typename T, int EACH, typename F>
+void with_row_shape(int64_t dim, F f) {
+  constexpr int W = kWidth<T>, N = 8 / W, D = EACH / 8;
+  if (dim < kMostWidth) f(Int<1>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 8 * W) f(Int<W>{}, Int<8>{}, Int<1>{});
+  else if (dim <= 16 * W) f(Int<W>{}, Int<16>{}, Int<1>{});
+  else if (dim <= 32 * W) f(Int<W>{}, Int<32>{}, Int<1>{});
+  else if (dim <= 64 * W) f(Int<W>{}, Int<64>{}, Int<1>{});
+  else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
+  else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
+  else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
+  else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
+  else if (dim <= 8192) f(Int<W>{}, Int<1024 / D>{}, Int<D * N>{});
+  else f(Int<W>{}, Int<1024>{}, Int<2 * N>{});
+}
 // Workgroups of the norm's gradient, each of which leaves its sums over rows: as many as the chip holds, but fewer where that leaves each less than ten
 // turns (of a row, or of the rows that it has side by side), and a quarter of that at least.  2048 rows x 2048 f32: 16.5 us with 256 workgroups, 17.6
 // with 512, 24.7 with 1024; 5840 x 1680 f32: 34, 29.6 and 33.7; 16384 x 2048 bf16: 57, 49.7 and 49.3.
