@@ -247,8 +247,8 @@ void with_block_shape(int64_t dim, F f) {
   else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
   else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
   else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
-  else if (dim <= 2560) f(Int<W>{}, Int<320>{}, Int<N>{});
-  else if (dim <= 3584) f(Int<W>{}, Int<448>{}, Int<N>{});
+  else if (dim <= 2560) f(Int<W>{}, Int<FORWARD ? 192 : 320>{}, Int<D * N>{});
+  else if (!FORWARD && dim <= 3584) f(Int<W>{}, Int<448>{}, Int<N>{});
   else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
   else if (dim <= 5120) f(Int<W>{}, Int<320>{}, Int<2 * N>{});
   else if (dim <= 6144) f(Int<W>{}, Int<384>{}, Int<2 * N>{});
@@ -384,7 +384,7 @@ fira_status fira_block_norm(const fira_block_norm_desc* d, const void* dev_x, in
     }
     with_block_shape<T, true>(d->dim, [&](auto width, auto threads, auto nv) {
       constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value, GROUPS = std::max(1, 256 / THREADS);
-      hipLaunchKernelGGL((fira_block_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)), dim3(std::max(256, THREADS)), 0, q, n,
+      hipLaunchKernelGGL((fira_block_norm_kernel<T, P, W, THREADS, NV>), dim3(std::min<int64_t>((d->rows + GROUPS - 1) / GROUPS, 1 << 20)), dim3(GROUPS * THREADS), 0, q, n,
                          (const raw*)dev_x, (const raw*)dev_block, v, (raw*)dev_residual, (raw*)dev_y, to);
     });
   });

@@ -668,6 +668,10 @@ class AdamWList:
         self.m_scale, self.v_scale = ([self._state(x, i, scales[i], torch.float32, name) if states[i] is not torch.float32 else None
                                        for i, x in enumerate(given or [None] * n)] for given, name in ((m_scale, "m_scale"), (v_scale, "v_scale")))
         self.t = self._state(t, 0, 2, torch.int64, "t")
+        for given, name in ((params, "tensor"), (self.m, "state m"), (self.v, "state v")):
+            places = [x.data_ptr() for x in given if x.numel()]
+            if len(set(places)) < len(places):
+                _refuse(FIRA_ERR_INVALID_ARG, f"a {name} is listed twice")
         pointers = ctypes.c_void_p * n
         self.W, self.G = pointers(*[p.data_ptr() for p in params]), pointers(*[g.data_ptr() for g in grads])
         at = lambda x: None if x is None else x.data_ptr()  # noqa: E731

@@ -353,3 +353,23 @@ def test_beyond_32_bit_offsets():
     most = np.repeat(np.abs(full.reshape(-1, 256)).max(1), 256)[(n - last) % 256:][:last]
     got = np.abs(ref.e4m3(lst.m[0][-last:]))
     assert np.mean((got >= ref.held(want["m"][0], most, random, False, -32 * U)) & (got <= ref.held(want["m"][0], most, random, False, 32 * U))) > 0.999
+
+
+def test_lists_that_are_refused():
+    w, g = torch.zeros(4, 300, device=DEV), torch.zeros(4, 300, device=DEV)
+    f, c = torch.zeros(1200, device=DEV), torch.zeros(1200, dtype=torch.uint8, device=DEV).view(E4M3)
+    scale = torch.zeros(5, device=DEV)
+    held = dict(m=[c], v=[c.clone()], m_scale=[scale], v_scale=[scale.clone()])
+    training.AdamWList([w], [g], **held)
+    bad = [([w, w], [g, g], {}), ([w], [g[:, :299]], {}), ([w], [g.half()], {}), ([w.t()], [g.t()], {}), ([w], [g], dict(m=[f[:-1]], v=[f])), ([w], [g], dict(m=[f], v=[c])), ([w], [g], dict(m=[f], v=[f.cpu()])),
+           ([w], [g], dict(m=[c], v=[c.clone()])), ([w], [g], dict(held, m_scale=[scale[:4]])), ([w], [g], dict(t=torch.zeros(1, dtype=torch.int64, device=DEV))), ([w], [g], dict(weight_decay=-1.0)),
+           ([w, g], [g.clone(), w.clone()], dict(m=[f, f], v=[f.clone(), f.clone()])), ([w], [g], dict(seeds=[1, 2])), ([w], [w], {})]
+    for params, grads, kw in bad:
+        with pytest.raises(fira.FiraError):
+            training.AdamWList(params, grads, **kw).fira_adamw_step(1e-3)
+    lst = training.AdamWList([w], [g])
+    for args, kw in (((math.nan,), {}), ((1e-3, 1.0), {}), ((1e-3, 0.9, 1.5), {}), ((1e-3, 0.9, 0.99, 0.0), {}), ((torch.zeros(2, device=DEV),), {}), ((torch.tensor(1e-3),), {}),
+                     ((1e-3,), dict(norm=torch.tensor(1.0, device=DEV, dtype=BF16))), ((1e-3,), dict(norm=torch.tensor(1.0, device=DEV), max_norm=-1.0))):
+        with pytest.raises(fira.FiraError):
+            lst.fira_adamw_step(*args, **kw)
+    assert lst.t.tolist() == [0, 0] and not w.any()
