@@ -20,11 +20,12 @@ struct FiraAdamSpan {
 };
 constexpr int kAdamSpans = 36;        // (a lane for each.)  A launch's pieces travel as kernel arguments, of which there are 4 KB
 // Vectors of a thread that are on their way together, and workgroups of a launch at most: with states in 8 bits a value has five times the arithmetic a byte.
-// us with one vector and 4096 workgroups, two and 16384: 60m 298 and 269, embeddings in 8 bits 276 and 288, 511 x 1377 and the like in 8 bits with rows apart 60 and 72.
+// us with one vector and 4096 workgroups, two and 16384: 60m 298 and 269, embeddings in 8 bits 276 and 288.  One vector in 8 bits with 4096, 8192, 16384 workgroups: embeddings 277,
+// 278, 276, 33 m values fp32 103, 100, 101, 62 m values bf16 with fp32 gradients 240, 231, 224, 511 x 1377 and the like fp32 with rows apart 59, 58, 61.
 template <bool EIGHT>
 constexpr int kAdamUnroll = EIGHT ? 1 : 2;
 template <bool EIGHT>
-constexpr int kAdamWorkgroups = EIGHT ? 4096 : 16384;
+constexpr int kAdamWorkgroups = EIGHT ? 8192 : 16384;
 struct FiraAdamSpans {
   FiraAdamSpan s[kAdamSpans];
   int count, tiles;
@@ -130,18 +131,20 @@ __device__ __forceinline__ void adam_joined(Raw<T, W>& a, const Raw<T, W>& b, in
   }
 }
 
-// Largest over the lanes that share a block, of floats that are not negative, as bits: what is not finite is larger than all that is.
+// The larger one, no number if one of the two is none; and over the lanes that share a block.
+__device__ __forceinline__ float adam_larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 template <int OFF>
-__device__ __forceinline__ unsigned max_xor(unsigned x) {
+__device__ __forceinline__ float max_xor(float x) {
   if constexpr (OFF < 16) {
-    return max(x, __float_as_uint(lane_xor<OFF>(__uint_as_float(x))));
+    return adam_larger(x, lane_xor<OFF>(x));
   } else {
-    const u32x2_s s = OFF == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return max((unsigned)s[0], (unsigned)s[1]);
+    const unsigned u = __float_as_uint(x);
+    const u32x2_s s = OFF == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return adam_larger(__uint_as_float((unsigned)s[0]), __uint_as_float((unsigned)s[1]));
   }
 }
 template <int LANES>
-__device__ __forceinline__ unsigned adam_most(unsigned x) {
+__device__ __forceinline__ float adam_most(float x) {
   x = max_xor<1>(max_xor<2>(max_xor<4>(max_xor<8>(max_xor<16>(x)))));
   if constexpr (LANES == 64) x = max_xor<32>(x);
   return x;
@@ -155,8 +158,16 @@ __device__ __forceinline__ float adam_quotient(float a, float b) {
   return __builtin_amdgcn_div_fixupf(q, b, a);
 }
 
-// The same with states in 8 bits, S times the moment m and root of v (and by S less what they are multiplied with).  The root instruction is off by at most 2 u and has
-// subnormals as zero.
+// Root of x in [2^-126, 2^127], correctly rounded but for one in millions: the rest that the estimate leaves is exact.  (Of less it is too small, of 0 it is 0, of what is
+// not finite no number.)  The root instruction, which is off by an ulp, is 1 % faster at embeddings in 8 bits (274 us and 277); an ulp more or less now and then rounds a code
+// to the other side, whose block has another largest size from the next step on.
+__device__ __forceinline__ float adam_root(float x) {
+  const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f)), q = x * y;
+  return __builtin_fmaf(__builtin_fmaf(-q, q, x), 0.5f * y, q);
+}
+
+// The same with states in 8 bits, S times the moment m and root of v (and by S less what they are multiplied with).
+template <bool FINITE>
 struct AdamScaled {
   float cut, fm, fv;
   __device__ __forceinline__ AdamScaled(const FiraAdamFactors& f, float S) : cut(f.cut * S), fm(f.m / S), fv(f.v / S) {}
@@ -164,7 +175,8 @@ struct AdamScaled {
 #pragma clang fp contract(off)
     g *= cut;
     m = m * hp.b1 + g * hp.omb1;
-    root = __builtin_amdgcn_sqrtf(root * root * hp.b2 + g * g * hp.omb2);
+    root = root * root * hp.b2 + g * g * hp.omb2;
+    root = FINITE ? adam_root(root) : sqrtf(root);
     w = w * decay - adam_quotient(m * fm, root * fv + hp.eps);
   }
 };
@@ -334,15 +346,15 @@ struct AdamVector {
     }
   }
 
-  // All that is of the gradients' size is held times 2^32, so that small squares stay above what the root instruction has as zero; where a product leaves fp32's range
+  // All that is of the gradients' size is held times 2^32, so that small squares stay above 2^-126; where a product leaves fp32's range
   // for that, the value is worked out again without.
   __device__ __forceinline__ void step_e4m3(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, unsigned key) {
     constexpr int LANES = kAdamBlock / W;
     constexpr float kMost = 0x1p120f;
     float S = 0x1p32f;
-    const AdamScaled scaled(f, S);
+    const AdamScaled<true> scaled(f, S);
     float ow[W], om[W], root[W];
-    unsigned bm = 0, bv = 0;
+    float mm = 0.0f, mv = 0.0f;                            // the block's largest
     const float sm = ms * S, sv = vs * S;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
@@ -350,15 +362,15 @@ struct AdamVector {
       om[k] = adam_value(m8[k / 4], k % 4) * sm;
       root[k] = adam_value(v8[k / 4], k % 4) * sv;
       scaled.update(hp, decay, g.get(k), ow[k], om[k], root[k]);
-      bm = max(bm, __float_as_uint(om[k]) & 0x7fffffffu);
-      bv = max(bv, __float_as_uint(root[k]));
+      mm = adam_larger(mm, fabsf(om[k]));
+      mv = adam_larger(mv, root[k]);
     }
-    bm = adam_most<LANES>(bm);
-    bv = adam_most<LANES>(bv);
+    mm = adam_most<LANES>(mm);
+    mv = adam_most<LANES>(mv);
     bool lost_m[W] = {}, lost_v[W] = {};                   // what is not finite
-    if (__any(max(bm, bv) >= __float_as_uint(kMost))) {
-      const AdamScaled plain(f, 1.0f);
-      bm = bv = 0;
+    if (__any(!(adam_larger(mm, mv) < kMost))) {
+      const AdamScaled<false> plain(f, 1.0f);
+      mm = mv = 0.0f;
 #pragma unroll
       for (int k = 0; k < W; ++k) {
         const bool fine = fabsf(om[k]) < INFINITY && root[k] < INFINITY;
@@ -369,25 +381,24 @@ struct AdamVector {
         root[k] = fine ? root[k] * (1.0f / S) : r1;
         lost_m[k] = !(fabsf(om[k]) < INFINITY);
         lost_v[k] = !(root[k] < INFINITY);
-        bm = max(bm, lost_m[k] ? 0u : __float_as_uint(om[k]) & 0x7fffffffu);
-        bv = max(bv, lost_v[k] ? 0u : __float_as_uint(root[k]));
+        mm = adam_larger(mm, lost_m[k] ? 0.0f : fabsf(om[k]));
+        mv = adam_larger(mv, lost_v[k] ? 0.0f : root[k]);
       }
-      bm = adam_most<LANES>(bm);
-      bv = adam_most<LANES>(bv);
+      mm = adam_most<LANES>(mm);
+      mv = adam_most<LANES>(mv);
       S = 1.0f;
     }
-    const float mm = __uint_as_float(bm), mv = __uint_as_float(bv);
     const bool none_m = mm < 0x1p-100f * S, none_v = mv < 0x1p-100f * S;
     // (the reciprocal instruction has results below 2^-126 as zero)
     const float down_m = mm < kMost ? 1.0f : 0x1p-32f, down_v = mv < kMost ? 1.0f : 0x1p-32f;
-    const float up_m = none_m ? 0.0f : adam_quotient(448.0f, mm * down_m) * down_m, up_v = none_v ? 0.0f : adam_quotient(448.0f, mv * down_v) * down_v;
+    const float up_m = none_m ? 0.0f : adam_quotient(1.0f, mm * down_m) * 448.0f * down_m, up_v = none_v ? 0.0f : adam_quotient(1.0f, mv * down_v) * 448.0f * down_v;
     unsigned cm[W / 4] = {}, cv[W / 4] = {};
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       const unsigned random = adam_mix(s.first + j + k + key);
       const float a = __builtin_amdgcn_fmed3f(om[k] * up_m, -448.0f, 448.0f);
-      float b = fminf(root[k] * up_v, 448.0f);
-      b = b > 0.0f ? fmaxf(b, 0x1p-9f) : b;              // the smallest code, which is not rounded down
+      float b = root[k] * up_v;
+      b = b > 0.0f ? __builtin_amdgcn_fmed3f(b, 0x1p-9f, 448.0f) : 0.0f;   // (at least the smallest code, which is not rounded down)
       cm[k / 4] = adam_put(cm[k / 4], a, random << 16 | 0x8000u, k % 4);
       cv[k / 4] = adam_put(cv[k / 4], b, (random & 0xffff0000u) | 0x8000u, k % 4);
       if (lost_m[k]) cm[k / 4] |= 127u << 8 * (k % 4);
@@ -408,8 +419,8 @@ struct AdamVector {
       });
     }
     if (here && j % kAdamBlock == 0) {
-      *as_global(s.m_scale + j / kAdamBlock) = none_m ? 0.0f : adam_quotient(mm, 448.0f) / S;
-      *as_global(s.v_scale + j / kAdamBlock) = none_v ? 0.0f : adam_quotient(mv, 448.0f) / S;
+      *as_global(s.m_scale + j / kAdamBlock) = none_m ? 0.0f : mm * (1.0f / 448.0f) / S;
+      *as_global(s.v_scale + j / kAdamBlock) = none_v ? 0.0f : mv * (1.0f / 448.0f) / S;
     }
   }
 };

@@ -110,6 +110,36 @@ def test_steps(dtype, grads, state):
             g.copy_((1e-3 * (3.0 if k == 1 else 1.0) * torch.randn(shape, device=DEV, generator=gen)).to(grads))
 
 
+def test_codes_are_those_of_elementary_operations():
+    """In 8 bits, too, every product, sum, root and quotient is rounded to nearest by itself, but for one in millions; and a value that is off by an ulp has another code by one chance in
+    2^17 (2^20 ulp to a step, of which a code takes its part down to 2^3).  So 50000 values have the same codes and scales as in numpy, step after step."""
+    one = np.float32
+    _, params, _, gs, _, lst, gen = problem(BF16, F32, E4M3, 8, [((50, 1000), 0)])
+    m, v = np.zeros(50000, one), np.zeros(50000, one)
+    place = np.arange(50000) // 256
+    for k in range(4):
+        lst.fira_adamw_step(1e-3, **HYPER)
+        g = gs[0].cpu().numpy().reshape(-1)
+        m = m * one(0.9) + g * one(1.0 - 0.9)
+        v = v * one(0.999) + g * g * one(1.0 - 0.999)
+        random = ref.rounding(50000, 0, k + 1)
+        held = []
+        for x, r, codes, scales in ((m, random[0], lst.m[0], lst.m_scale[0]), (np.sqrt(v), random[1], lst.v[0], lst.v_scale[0])):
+            most = np.pad(np.abs(x), (0, -len(x) % 256)).reshape(-1, 256).max(1)
+            scale = most * (one(1.0) / one(448.0))
+            y = np.minimum(np.abs(x) * (one(1.0) / most * one(448.0))[place], one(448.0)).astype(np.float64)
+            step = 2.0 ** (np.floor(np.log2(np.maximum(y, 2.0 ** -6))) - 3.0)
+            c = np.minimum(np.floor(y / step + (r.astype(np.float64) + 0.5) / 65536.0) * step, 448.0)
+            c = np.copysign(np.where(x > 0, np.maximum(c, 2.0 ** -9), c) if codes is lst.v[0] else c, x)
+            # (sizes below 2^-6 are added to that before they are rounded, in fp32)
+            got, plain = ref.e4m3(codes), y >= 2.0 ** -6
+            assert np.array_equal(got[plain], c[plain]) and (got != c).sum() <= 2
+            assert np.array_equal(scales.cpu().numpy(), scale)
+            held.append(got.astype(one) * scale[place])
+        m, v = held[0], held[1] * held[1]
+        gs[0].copy_(1e-3 * (k + 1) * torch.randn(50, 1000, device=DEV, generator=gen))
+
+
 @pytest.mark.parametrize("taken", [0, 9, 1000, 10 ** 6, (1 << 32) + 5])
 def test_step_counts(taken):
     for state in (F32, E4M3):
