@@ -634,7 +634,8 @@ class AdamWList:
     are rounded at random by seeds (default: the place in the list).
 
     m, v, m_scale, v_scale (lists; the scales of a float32 state are None) and t (two int64: the steps taken, and a value of the call's) are a
-    checkpoint.  Those that are not given begin at zero, on the stream that is current then."""
+    checkpoint.  Those that are not given begin at zero, on the stream that is current then.  The states may be dropped with the list while its calls are still at
+    work, on whatever stream that is; parameters and gradients are kept by their owner, and everything by that of a captured step."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, weight_decay=0.0, state=torch.float32,
                  m: Optional[Sequence[torch.Tensor]] = None, v: Optional[Sequence[torch.Tensor]] = None, m_scale: Optional[Sequence[Optional[torch.Tensor]]] = None,
@@ -644,10 +645,13 @@ class AdamWList:
         params, grads = list(params), list(grads)
         if not params and device is None:
             _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
+        if (m is None) != (v is None) or (m_scale is None) != (v_scale is None) or (m is None and m_scale is not None):
+            _refuse(FIRA_ERR_INVALID_ARG, "states that are given in part")
         n = self.count = len(params)
         each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
         decays, states, seeds = each(weight_decay), each(state) if m is None else [x.dtype for x in m], list(range(n)) if seeds is None else list(seeds)
-        for given, name in ((grads, "gradients"), (decays, "weight decays"), (states, "states"), (seeds, "seeds"), (v if m is not None else states, "states v")):
+        for given, name in ((grads, "gradients"), (decays, "weight decays"), (states, "states"), (seeds, "seeds"), (states if v is None else v, "states v"),
+                            (states if m_scale is None else m_scale, "scales of m"), (states if v_scale is None else v_scale, "scales of v")):
             if given is None or len(given) != n:
                 _refuse(FIRA_ERR_INVALID_ARG, f"{None if given is None else len(given)} {name} for {n} tensors")
         for i, x in enumerate(states):
@@ -677,6 +681,7 @@ class AdamWList:
         at = lambda x: None if x is None else x.data_ptr()  # noqa: E731
         self.states = (fira.fira_adamw_state * n)(*[fira.fira_adamw_state(*map(at, x)) for x in zip(self.m, self.v, self.m_scale, self.v_scale)])
         self._keep = (params, grads)
+        self._streams = set()                              # on which the states are known to be in use
 
     def _state(self, given, i: int, size: int, dtype, name: str) -> torch.Tensor:
         if given is None:
@@ -699,6 +704,12 @@ class AdamWList:
         if elsewhere is not None:
             with elsewhere:
                 return self.fira_adamw_step(lr, beta1, beta2, eps, norm=norm, max_norm=max_norm)
+        q = _stream(self.device)
+        if q not in self._streams and not torch.cuda.is_current_stream_capturing():
+            for x in (*self.m, *self.v, *self.m_scale, *self.v_scale, self.t):
+                if x is not None:
+                    x.record_stream(torch.cuda.current_stream())
+            self._streams.add(q)
         hp = fira.fira_adamw_hparams(0.0 if given is not None else lr, beta1, beta2, eps, max_norm)
         _check(self.lib.fira_adamw_step(self.descs, self.count, hp, self.W, self.G, self.states, self.t.data_ptr(), None if given is None else given.data_ptr(),
-                                        None if norm is None else norm.data_ptr(), _stream(self.device)))
+                                        None if norm is None else norm.data_ptr(), q))

@@ -346,6 +346,26 @@ def test_two_lists_on_two_streams():
         assert same([p.contiguous() for p in params] + lst.m, [p.contiguous() for p in want] + alone.m) and lst.t.tolist() == [5, 0]
 
 
+@pytest.mark.parametrize("state", [F32, E4M3])
+def test_a_list_dropped_while_its_step_waits(state):
+    """States that only the list holds, a step on a stream that is busy, and the list dropped: memory that the first stream hands out next is not the step's."""
+    gen = generator(16)
+    w, g = 0.02 * torch.randn(300, 1000, device=DEV, generator=gen), 1e-3 * torch.randn(300, 1000, device=DEV, generator=gen)
+    want = w.clone()
+    training.AdamWList([want], [g], state=state).fira_adamw_step(1e-3, **HYPER)
+    side = torch.cuda.Stream()
+    lst = training.AdamWList([w], [g], state=state)
+    sizes = [x.numel() * x.element_size() for x in (*lst.m, *lst.v, *lst.m_scale, *lst.v_scale, lst.t) if x is not None]
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    lst.fira_adamw_step(1e-3, **HYPER, stream=side)
+    del lst
+    others = [torch.full((n,), 77, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(8)]
+    torch.cuda.synchronize()
+    assert all(bool((x == 77).all()) for x in others) and torch.equal(w, want)
+
+
 def test_a_run_goes_on_from_its_states():
     """Saved and put into a new list, the states go on as if nothing had happened."""
     _, params, _, gs, _, lst, _ = problem(BF16, BF16, E4M3, 15)

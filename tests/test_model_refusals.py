@@ -55,6 +55,14 @@ def test_adamw_lists_of_cpu_tensors():
             training.AdamWList(*args, **kwargs)
 
 
+def test_adamw_states_that_are_given_in_part():
+    w, c, scale = torch.zeros(300), torch.zeros(300, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(2)
+    for kwargs in ({"m": [w]}, {"v": [w]}, {"m": [c], "v": [c], "m_scale": [scale]}, {"m_scale": [scale], "v_scale": [scale]}, {"m": [c], "v": [c, c], "m_scale": [scale], "v_scale": [scale]},
+                   {"m": [c], "v": [c], "m_scale": [scale, scale], "v_scale": [scale]}, {"m": [c], "v": [c], "m_scale": [scale], "v_scale": []}):
+        with pytest.raises(fira.FiraError, match="in part|for 1 tensors"):
+            training.AdamWList([w], [w], **kwargs)
+
+
 def test_rotary(lib):
     desc = lambda batch=2, length=3, dim=16, rotated=8, dtype=0, layout=0, position_type=1, position_stride=3, scale=1.0: fira.fira_rotary_desc(  # noqa: E731
         batch, length, dim, rotated, dtype, layout, position_type, position_stride, scale)
