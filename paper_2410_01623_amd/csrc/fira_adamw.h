@@ -31,9 +31,11 @@ struct FiraAdamSpans {
   int count, tiles;
   int counts;              // the call's last launch, of few workgroups: counts the step
 };
-// Values of a thread's vector and of a tile: 16 bytes of the widest type that is streamed.
-template <typename T, typename R, bool EIGHT>
-constexpr int kAdamWidth = EIGHT ? kWidth<T, R> : 4;
+// Values of a thread's vector: 16 bytes of the widest type that is streamed, but with states in 8 bits 32 bytes of fp32 weights or gradients beside bf16 (us so and with 16: 512 x 1376 and
+// the like, bf16 with fp32 gradients 40 and 51, fp32 with bf16 ones 44 and 55; all fp32 50 and 45).  APART: 16 bytes, since the joining of rows' ends takes registers (the
+// former two, 511 x 1377 with rows apart, 83 and 65, 85 and 70).
+template <typename T, typename R, bool EIGHT, bool APART>
+constexpr int kAdamWidth = !EIGHT ? 4 : APART || sizeof(typename T::raw) + sizeof(typename R::raw) == 8 ? kWidth<T, R> : 8;
 
 struct FiraAdamHp {
   double lr, log_beta1, log_beta2, max_norm;
@@ -83,13 +85,13 @@ __device__ __forceinline__ void adam_update(const FiraAdamHp& hp, const FiraAdam
   w = w * decay - (m * f.m) / (sqrtf(v) * f.v + hp.eps);
 }
 
-enum { kStreamed, kWhole, kEnd, kApart };
+enum { kStreamed, kWhole, kEnd, kRows, kApart };
 
 // Calls f with whether to stream as a constant, which where rows are apart is known at run time only.  What the compiler finds twice, with and without
 // streaming, it makes one of plain stores: the empty statements keep it from that.
 template <int PLACE, typename F>
 __device__ __forceinline__ void either_way(bool stream, F f) {
-  if (PLACE == kStreamed || (PLACE == kApart && stream)) {
+  if (PLACE == kStreamed || ((PLACE == kApart || PLACE == kRows) && stream)) {
     asm volatile("" ::: "memory");
     f(std::true_type{});
     asm volatile("" ::: "memory");
@@ -202,10 +204,10 @@ __device__ __forceinline__ unsigned adam_put(unsigned codes, float x, unsigned r
 
 // A thread's values on their way: weights and gradients as they are stored, and the states, which have no gaps.
 // PLACE: whole vectors of a piece without gaps, whose results go past the caches (kStreamed) or not (kWhole); such vectors or a part of one at the piece's end (kEnd); of a piece
-// whose rows are apart (kApart).
+// whose rows are apart and whole vectors wide (kRows), or of any width (kApart).
 template <typename T, typename R, bool EIGHT, int W, int PLACE>
 struct AdamVector {
-  static constexpr bool APART = PLACE == kApart, FULL = PLACE == kStreamed || PLACE == kWhole;
+  static constexpr bool JOIN = PLACE == kApart, APART = JOIN || PLACE == kRows, FULL = PLACE == kStreamed || PLACE == kWhole;
   Raw<T, W> w;
   Raw<R, W> g;
   unsigned m8[W / 4], v8[W / 4];
@@ -232,7 +234,7 @@ struct AdamVector {
       row = (unsigned)(((double)c + 0.5) * s.per_col);
       col = c - row * s.cols;
     }
-    whole = here == W && (!APART || s.cols - col >= W);
+    whole = here == W && (!JOIN || s.cols - col >= W);
     const typename T::raw* const pw = (const typename T::raw*)s.w + row * s.ld_w + col;
     const typename R::raw* const pg = (const typename R::raw*)s.g + row * s.ld_g + col;
     auto vectors = [&] {
@@ -245,7 +247,7 @@ struct AdamVector {
       return;
     }
     if (whole) vectors();
-    if (APART && !whole && here == W && s.cols >= W) {
+    if (JOIN && !whole && here == W && s.cols >= W) {
       // the end of a row and the beginning of the next
       const int back = (int)(col + W - s.cols);
       Raw<T, W> w2;
@@ -258,12 +260,12 @@ struct AdamVector {
       adam_joined<T, W>(w, w2, back);
       adam_joined<R, W>(g, g2, back);
     }
-    if (here < W || (APART && !whole && s.cols < W)) {
+    if (here < W || (JOIN && !whole && s.cols < W)) {
       // value by value, zeros where there are none
 #pragma unroll
       for (int k = 0; k < W; ++k) {
-        const bool is = k < here;
-        const unsigned down = APART && is ? (col + k) / s.cols : 0u;
+        const bool is = PLACE != kRows && k < here;        // (there, all are or none is)
+        const unsigned down = JOIN && is ? (col + k) / s.cols : 0u;
         adam_set<T, W>(w, k, is ? *as_global(pw + k + down * (s.ld_w - s.cols)) : (typename T::raw)0);
         adam_set<R, W>(g, k, is ? *as_global(pg + k + down * (s.ld_g - s.cols)) : (typename R::raw)0);
         if constexpr (EIGHT) {
@@ -294,19 +296,16 @@ struct AdamVector {
     }
   }
 
-  // Calls f(k, place of value k of the weights) for the values that are there.
-  template <typename F>
-  __device__ __forceinline__ void each(const FiraAdamSpan& s, F f) const {
+  __device__ __forceinline__ void put_weights(const FiraAdamSpan& s, const float (&x)[W]) const {
     typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
+    if (FULL || whole) {
+      either_way<PLACE>(s.stream & 1, [&](auto stream) { store_w<T, W, decltype(stream)::value>(pw, x); });
+      return;
+    }
     const bool one = s.cols >= W;                          // (no second end of a row then)
 #pragma unroll
     for (int k = 0; k < W; ++k)
-      if (k < here) f(k, pw + k + (!APART ? 0u : one ? (unsigned)(col + k >= s.cols) : (col + k) / s.cols) * (s.ld_w - s.cols));
-  }
-
-  __device__ __forceinline__ void put_weights(const FiraAdamSpan& s, const float (&x)[W]) const {
-    typename T::raw* const pw = (typename T::raw*)s.w + row * s.ld_w + col;
-    either_way<PLACE>(s.stream & 1, [&](auto stream) { store_w<T, W, decltype(stream)::value>(pw, x); });
+      if (PLACE != kRows && k < here) store1<T>(pw + k + (!JOIN ? 0u : one ? (unsigned)(col + k >= s.cols) : (col + k) / s.cols) * (s.ld_w - s.cols), x[k]);
   }
   static __device__ __forceinline__ void put_bytes(unsigned char* p, const unsigned (&x)[W / 4], bool stream) {
     typedef unsigned __attribute__((aligned(1))) u32_a1;
@@ -328,21 +327,19 @@ struct AdamVector {
       ov[k] = v[k];
       adam_update(hp, f, decay, g.get(k), ow[k], om[k], ov[k]);
     }
-    auto vectors = [&] {
-      put_weights(s, ow);
+    put_weights(s, ow);
+    if (FULL || here == W) {
       either_way<PLACE>(s.stream & 2, [&](auto stream) {
         store_w<FiraStoredF32, W, decltype(stream)::value>((float*)s.m + j, om);
         store_w<FiraStoredF32, W, decltype(stream)::value>((float*)s.v + j, ov);
       });
-    };
-    if (FULL || whole) {
-      vectors();
     } else {
-      each(s, [&](int k, typename T::raw* to) {
-        store1<T>(to, ow[k]);
-        *as_global((float*)s.m + j + k) = om[k];
-        *as_global((float*)s.v + j + k) = ov[k];
-      });
+#pragma unroll
+      for (int k = 0; k < W - 1; ++k)
+        if (PLACE != kRows && k < here) {
+          *as_global((float*)s.m + j + k) = om[k];
+          *as_global((float*)s.v + j + k) = ov[k];
+        }
     }
   }
 
@@ -404,19 +401,17 @@ struct AdamVector {
       if (lost_m[k]) cm[k / 4] |= 127u << 8 * (k % 4);
       if (lost_v[k]) cv[k / 4] |= 127u << 8 * (k % 4);
     }
-    auto vectors = [&] {
-      put_weights(s, ow);
+    put_weights(s, ow);
+    if (FULL || here == W) {
       put_bytes((unsigned char*)s.m + j, cm, s.stream & 2);
       put_bytes((unsigned char*)s.v + j, cv, s.stream & 2);
-    };
-    if (FULL || whole) {
-      vectors();
     } else {
-      each(s, [&](int k, typename T::raw* to) {
-        store1<T>(to, ow[k]);
-        *as_global((unsigned char*)s.m + j + k) = (unsigned char)(cm[k / 4] >> 8 * (k % 4));
-        *as_global((unsigned char*)s.v + j + k) = (unsigned char)(cv[k / 4] >> 8 * (k % 4));
-      });
+#pragma unroll
+      for (int k = 0; k < W - 1; ++k)
+        if (PLACE != kRows && k < here) {
+          *as_global((unsigned char*)s.m + j + k) = (unsigned char)(cm[k / 4] >> 8 * (k % 4));
+          *as_global((unsigned char*)s.v + j + k) = (unsigned char)(cv[k / 4] >> 8 * (k % 4));
+        }
     }
     if (here && j % kAdamBlock == 0) {
       *as_global(s.m_scale + j / kAdamBlock) = none_m ? 0.0f : mm * (1.0f / 448.0f) / S;
@@ -426,9 +421,10 @@ struct AdamVector {
 };
 
 // A workgroup takes every gridDim.x-th tile of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
-template <typename T, typename R, bool EIGHT>
+// APART: some pieces' rows are, and not whole vectors wide.
+template <typename T, typename R, bool EIGHT, bool APART>
 __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {
-  constexpr int W = kAdamWidth<T, R, EIGHT>, TILE = 256 * W * kAdamUnroll<EIGHT>;
+  constexpr int W = kAdamWidth<T, R, EIGHT, APART>, TILE = 256 * W * kAdamUnroll<EIGHT>;
   __shared__ FiraAdamFactors shared;
   // (the other wavefronts' first loads are on their way meanwhile)
   if (threadIdx.x < 2) adam_factors(shared, hp, lr, norm, *as_global(counter));
@@ -470,7 +466,12 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
     };
     typedef std::integral_constant<int, kAdamUnroll<EIGHT>> All;
     typedef std::integral_constant<int, 1> One;
-    if (s.cols) work(std::integral_constant<int, kApart>{}, One{});
+    if constexpr (APART)
+      if (s.cols % kMostWidth) {
+        work(std::integral_constant<int, kApart>{}, One{});
+        continue;
+      }
+    if (s.cols) work(std::integral_constant<int, kRows>{}, One{});
     else if (s.n - first < (unsigned)TILE) work(std::integral_constant<int, kEnd>{}, One{});
     else if (s.stream == 3) work(std::integral_constant<int, kStreamed>{}, All{});
     else work(std::integral_constant<int, kWhole>{}, All{});

@@ -28,12 +28,14 @@ fira_status check_adamw_hparams(const fira_adamw_hparams* hp, bool norm) {
   return FIRA_OK;
 }
 
+bool adamw_apart(const fira_adamw_desc& d) { return d.rows > 1 && d.cols && (d.ld_w != d.cols || d.ld_g != d.cols); }
+
 // Cuts a tensor into pieces that the kernel takes: from a whole block on, up to 2^30 values.
 constexpr int64_t kAdamPiece = 1 << 30;
 template <typename F>
 void cut_adamw(const fira_adamw_desc& d, void* w, const void* g, const fira_adamw_state& s, F piece) {
   const int64_t n = d.rows * d.cols;
-  const bool dense = d.rows == 1 || (d.ld_w == d.cols && d.ld_g == d.cols);
+  const bool dense = !adamw_apart(d);
   const bool eight = d.state_type == FIRA_STATE_E4M3;
   for (int64_t i = 0; i < n; i += kAdamPiece) {
     const int64_t row = dense ? 0 : i / d.cols, col = dense ? 0 : i % d.cols, b = i / kAdamBlock;
@@ -49,29 +51,34 @@ void cut_adamw(const fira_adamw_desc& d, void* w, const void* g, const fira_adam
   }
 }
 
-// Calls f(types, states in 8 bits, pieces) for every launch that the list takes, types by types.
+// Calls f(types, states in 8 bits, whether rows are apart and not whole vectors wide, pieces) for every launch that the list takes, types by types.
 template <typename F>
 void for_each_adamw_launch(const fira_adamw_desc* d, int count, void* const* W, const void* const* G, const fira_adamw_state* state, F f) {
   for (int kind = 0; kind < 8; ++kind) {
     const int in = kind & 1, grad = kind >> 1 & 1, eight = kind >> 2;
+    auto of_kind = [&](const fira_adamw_desc& x) { return x.dtype == in && x.grad_dtype == grad && (x.state_type == FIRA_STATE_E4M3) == (eight != 0); };
+    bool any = false;                                      // (one launch more for those that are not apart would cost more than they lose)
+    for (int i = 0; i < count; ++i) any = any || (of_kind(d[i]) && adamw_apart(d[i]) && d[i].cols % kMostWidth);
     with_types(in, grad, [&](auto t, auto r) {
       with_flag(eight, [&](auto e) {
-        constexpr int64_t tile = 256 * kAdamUnroll<decltype(e)::value> * kAdamWidth<decltype(t), decltype(r), decltype(e)::value>;
-        FiraAdamSpans l{};
-        auto flush = [&] {
-          if (l.count) f(t, r, e, l);
-          l.count = l.tiles = 0;
-        };
-        for (int i = 0; i < count; ++i) {
-          if (d[i].dtype != in || d[i].grad_dtype != grad || (d[i].state_type == FIRA_STATE_E4M3) != (eight != 0)) continue;
-          cut_adamw(d[i], W[i], G[i], state[i], [&](FiraAdamSpan s) {
-            s.tile0 = l.tiles;
-            l.s[l.count++] = s;
-            l.tiles += (int)((s.n + tile - 1) / tile);     // (2^30 values are 2^20 tiles at most)
-            if (l.count == kAdamSpans) flush();
-          });
-        }
-        flush();
+        with_flag(any, [&](auto apart) {
+          constexpr int64_t tile = 256 * kAdamUnroll<decltype(e)::value> * kAdamWidth<decltype(t), decltype(r), decltype(e)::value, decltype(apart)::value>;
+          FiraAdamSpans l{};
+          auto flush = [&] {
+            if (l.count) f(t, r, e, apart, l);
+            l.count = l.tiles = 0;
+          };
+          for (int i = 0; i < count; ++i) {
+            if (!of_kind(d[i])) continue;
+            cut_adamw(d[i], W[i], G[i], state[i], [&](FiraAdamSpan s) {
+              s.tile0 = l.tiles;
+              l.s[l.count++] = s;
+              l.tiles += (int)((s.n + tile - 1) / tile);   // (2^30 values are 2^20 tiles at most)
+              if (l.count == kAdamSpans) flush();
+            });
+          }
+          flush();
+        });
       });
     });
   }
@@ -310,11 +317,11 @@ fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adam
                      (float)hp->eps};
   int launches = 0, at = 0;
   bool counted = false;
-  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto, auto, auto, FiraAdamSpans&) { ++launches; });
-  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, FiraAdamSpans& l) {
+  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto, auto, auto, auto, FiraAdamSpans&) { ++launches; });
+  for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, auto apart, FiraAdamSpans& l) {
     const int workgroups = std::min(l.tiles, kAdamWorkgroups<decltype(eight)::value>);
     l.counts = counted = ++at == launches && workgroups <= kAdamCounting;
-    hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value>), dim3(workgroups), dim3(256), 0, q, l, h, dev_lr, dev_norm, (long long*)dev_t);
+    hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value, decltype(apart)::value>), dim3(workgroups), dim3(256), 0, q, l, h, dev_lr, dev_norm, (long long*)dev_t);
   });
   if (!counted) hipLaunchKernelGGL(fira_adamw_count_kernel<>, dim3(1), dim3(1), 0, q, (long long*)dev_t);
   return launched("AdamW step");

@@ -57,14 +57,15 @@ int64_t pick(int64_t lo, int64_t hi) { return lo + (int64_t)(rng() % (uint64_t)(
 
 struct Seen { FiraAdamSpan s; int dtype, grad, eight; };
 
-template <typename T, typename R, bool EIGHT>
-bool adamw_launch(const void* f, dim3 grid, void** args, std::vector<Seen>& seen, int& counts, int dtype, int grad) {
-  if (f != (const void*)fira_adamw_kernel<T, R, EIGHT>) return false;
+template <typename T, typename R, bool EIGHT, bool APART>
+bool adamw_launch_of(const void* f, dim3 grid, void** args, std::vector<Seen>& seen, int& counts, int dtype, int grad) {
+  if (f != (const void*)fira_adamw_kernel<T, R, EIGHT, APART>) return false;
   const FiraAdamSpans& l = *(const FiraAdamSpans*)args[0];
-  constexpr int64_t tile = 256 * kAdamUnroll<EIGHT> * kAdamWidth<T, R, EIGHT>;
+  constexpr int64_t tile = 256 * kAdamUnroll<EIGHT> * kAdamWidth<T, R, EIGHT, APART>;
   CHECK(l.count >= 1 && l.count <= kAdamSpans && (int)grid.x == std::min(l.tiles, kAdamWorkgroups<EIGHT>) && pushed_block.x == 256);
   int64_t tiles = 0;
   for (int i = 0; i < l.count; ++i) {
+    CHECK(APART || l.s[i].cols % kMostWidth == 0);
     CHECK(l.s[i].tile0 == tiles && l.s[i].n >= 1 && (int64_t)l.s[i].n <= kAdamPiece);
     // (a thread's place in a piece, and in the columns, beyond its last vector)
     CHECK((int64_t)l.s[i].n + tile < (int64_t)1 << 32 && (int64_t)l.s[i].col0 + l.s[i].n + tile < (int64_t)1 << 32);
@@ -75,6 +76,11 @@ bool adamw_launch(const void* f, dim3 grid, void** args, std::vector<Seen>& seen
   CHECK(!l.counts || (int)grid.x <= kAdamCounting);
   counts += l.counts != 0;
   return true;
+}
+
+template <typename T, typename R, bool EIGHT>
+bool adamw_launch(const void* f, dim3 grid, void** args, std::vector<Seen>& seen, int& counts, int dtype, int grad) {
+  return adamw_launch_of<T, R, EIGHT, false>(f, grid, args, seen, counts, dtype, grad) || adamw_launch_of<T, R, EIGHT, true>(f, grid, args, seen, counts, dtype, grad);
 }
 
 void check_adamw_lists() {
