@@ -2,6 +2,8 @@
 #pragma once
 #include "fira_rows.h"
 
+#include <algorithm>
+
 constexpr int kAdamBlock = 256;       // values that share a scale
 
 // A piece of a tensor: n values, of the tensor's rows one after the other, from a whole block on.
@@ -19,13 +21,14 @@ struct FiraAdamSpan {
   int stream;              // results that begin at whole lines, and go past the caches: 1 weights, 2 states
 };
 constexpr int kAdamSpans = 36;        // (a lane for each.)  A launch's pieces travel as kernel arguments, of which there are 4 KB
-// Vectors of a thread that are on their way together, and workgroups of a launch at most: with states in 8 bits a value has five times the arithmetic a byte.
-// us with one vector and 4096 workgroups, two and 16384: 60m 298 and 269, embeddings in 8 bits 276 and 288.  One vector in 8 bits with 4096, 8192, 16384 workgroups: embeddings 277,
-// 278, 276, 33 m values fp32 103, 100, 101, 62 m values bf16 with fp32 gradients 240, 231, 224, 511 x 1377 and the like fp32 with rows apart 59, 58, 61.
-template <bool EIGHT>
-constexpr int kAdamUnroll = EIGHT ? 1 : 2;
-template <bool EIGHT>
-constexpr int kAdamWorkgroups = EIGHT ? 8192 : 16384;
+// Vectors of a thread that are on their way together, and workgroups of a launch of `tiles`: with states in 8 bits and rows apart that are not whole vectors wide (APART), where code and
+// registers are many, one and those of two tiles each, else two and nearly all that there could be.  us with one vector and two: 60m bf16 265 and 235, embeddings in 8 bits 280 and 260, 62 m
+// values bf16 with fp32 gradients in 8 bits 195 and 177; 511 x 1377 and the like in 8 bits with rows apart 58 and 64.  With 8192, 16384 and 65536 workgroups: 60m 244, 235 and 230, those 62 m
+// values 184, 177 and 175; with rows apart and 8192, two tiles each and one tile each: 62 m values fp32 in 8 bits 341, 288 and 315, bf16 231, 237 and 245.
+template <bool EIGHT, bool APART>
+constexpr int kAdamUnroll = EIGHT && APART ? 1 : 2;
+template <bool EIGHT, bool APART>
+int adam_workgroups(int tiles) { return std::min(tiles, EIGHT && APART ? std::max(8192, (tiles + 1) / 2) : 65536); }
 struct FiraAdamSpans {
   FiraAdamSpan s[kAdamSpans];
   int count, tiles;
@@ -424,7 +427,7 @@ struct AdamVector {
 // APART: some pieces' rows are, and not whole vectors wide.
 template <typename T, typename R, bool EIGHT, bool APART>
 __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {
-  constexpr int W = kAdamWidth<T, R, EIGHT, APART>, TILE = 256 * W * kAdamUnroll<EIGHT>;
+  constexpr int W = kAdamWidth<T, R, EIGHT, APART>, TILE = 256 * W * kAdamUnroll<EIGHT, APART>;
   __shared__ FiraAdamFactors shared;
   // (the other wavefronts' first loads are on their way meanwhile)
   if (threadIdx.x < 2) adam_factors(shared, hp, lr, norm, *as_global(counter));
@@ -440,7 +443,7 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
     auto work = [&](auto place, auto together) {
       constexpr int N = decltype(together)::value;
 #pragma unroll 1
-      for (int u0 = 0; u0 < kAdamUnroll<EIGHT>; u0 += N) {
+      for (int u0 = 0; u0 < kAdamUnroll<EIGHT, APART>; u0 += N) {
         AdamVector<T, R, EIGHT, W, decltype(place)::value> x[N];
 #pragma unroll
         for (int u = 0; u < N; ++u) x[u].load(s, first + ((u0 + u) * 256 + threadIdx.x) * W);
@@ -464,7 +467,7 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
         }
       }
     };
-    typedef std::integral_constant<int, kAdamUnroll<EIGHT>> All;
+    typedef std::integral_constant<int, kAdamUnroll<EIGHT, APART>> All;
     typedef std::integral_constant<int, 1> One;
     if constexpr (APART)
       if (s.cols % kMostWidth) {
@@ -478,7 +481,7 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
   }
 }
 
-// Counting the step in the last launch saves a launch (17 vectors 10.3 us with that, 8.8 without); of many workgroups it would be a queue at one address.
+// Counting the step in the last launch saves a launch (of 17 vectors, 1.5 us); of many workgroups it would be a queue at one address.
 constexpr int kAdamCounting = 512;
 template <typename = void>
 __global__ void fira_adamw_count_kernel(long long* taken) { *as_global(taken) += 1; }

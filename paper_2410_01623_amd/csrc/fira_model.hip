@@ -62,7 +62,7 @@ void for_each_adamw_launch(const fira_adamw_desc* d, int count, void* const* W, 
     with_types(in, grad, [&](auto t, auto r) {
       with_flag(eight, [&](auto e) {
         with_flag(any, [&](auto apart) {
-          constexpr int64_t tile = 256 * kAdamUnroll<decltype(e)::value> * kAdamWidth<decltype(t), decltype(r), decltype(e)::value, decltype(apart)::value>;
+          constexpr int64_t tile = 256 * kAdamUnroll<decltype(e)::value, decltype(apart)::value> * kAdamWidth<decltype(t), decltype(r), decltype(e)::value, decltype(apart)::value>;
           FiraAdamSpans l{};
           auto flush = [&] {
             if (l.count) f(t, r, e, apart, l);
@@ -319,7 +319,7 @@ fira_status fira_adamw_step(const fira_adamw_desc* d, int count, const fira_adam
   bool counted = false;
   for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto, auto, auto, auto, FiraAdamSpans&) { ++launches; });
   for_each_adamw_launch(d, count, dev_W, dev_G, dev_state, [&](auto t, auto r, auto eight, auto apart, FiraAdamSpans& l) {
-    const int workgroups = std::min(l.tiles, kAdamWorkgroups<decltype(eight)::value>);
+    const int workgroups = adam_workgroups<decltype(eight)::value, decltype(apart)::value>(l.tiles);
     l.counts = counted = ++at == launches && workgroups <= kAdamCounting;
     hipLaunchKernelGGL((fira_adamw_kernel<decltype(t), decltype(r), decltype(eight)::value, decltype(apart)::value>), dim3(workgroups), dim3(256), 0, q, l, h, dev_lr, dev_norm, (long long*)dev_t);
   });

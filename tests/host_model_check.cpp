@@ -61,8 +61,8 @@ template <typename T, typename R, bool EIGHT, bool APART>
 bool adamw_launch_of(const void* f, dim3 grid, void** args, std::vector<Seen>& seen, int& counts, int dtype, int grad) {
   if (f != (const void*)fira_adamw_kernel<T, R, EIGHT, APART>) return false;
   const FiraAdamSpans& l = *(const FiraAdamSpans*)args[0];
-  constexpr int64_t tile = 256 * kAdamUnroll<EIGHT> * kAdamWidth<T, R, EIGHT, APART>;
-  CHECK(l.count >= 1 && l.count <= kAdamSpans && (int)grid.x == std::min(l.tiles, kAdamWorkgroups<EIGHT>) && pushed_block.x == 256);
+  constexpr int64_t tile = 256 * kAdamUnroll<EIGHT, APART> * kAdamWidth<T, R, EIGHT, APART>;
+  CHECK(l.count >= 1 && l.count <= kAdamSpans && ((int)grid.x == adam_workgroups<EIGHT, APART>(l.tiles)) && (int)grid.x <= l.tiles && (int64_t)grid.x * 256 < (int64_t)1 << 32 && pushed_block.x == 256);
   int64_t tiles = 0;
   for (int i = 0; i < l.count; ++i) {
     CHECK(APART || l.s[i].cols % kMostWidth == 0);
