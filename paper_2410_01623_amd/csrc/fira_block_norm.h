@@ -190,9 +190,12 @@ struct BlockRowHeld {
 // every gridDim.x-th row, or set of rows side by side, and adds up its columns of dy h, dy, t h' and t, of which the vectors' gradients are
 // made (block_vector_gradients): gate and post norm need no sums of their own.  partial: [4][gridDim.x][dim], of which `sums` (bits) are wanted.  Bound by memory.
 constexpr int kBlockWidest = 8192;      // of the gradient's rows in registers, 16 values a thread
+// Ten wavefronts, in fp32 up to 2560 columns: two such workgroups fit a compute unit wherever they begin if six wavefronts fit a SIMD (with five, 16385 x 2049 with means and
+// biases took 213 us, alone 203, so 175).
+constexpr int kBlockTwo = 640;
 // LEAN: no means and no sums of dy and t, as for root-mean-square norms without biases, which leaves registers for more wavefronts.
 template <typename T, typename P, int W, int THREADS, int NV, bool LEAN>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm_gradient_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == kBlockTwo ? 6 : 1) void fira_block_norm_gradient_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
                                                                                                  const typename T::raw* b, FiraBlockVectors<P> vec, FiraBlockStats stats,
                                                                                                  typename T::raw* dx, typename T::raw* db, float* partial, int sums) {
   constexpr int GROUPS = THREADS < 256 ? 256 / THREADS : 1;
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
 #pragma unroll
     for (int v = 0; v < NV; ++v) put(db, n.ld_db, v, t[v]);
   };
-  // (the next row on its way takes registers that more wavefronts can use: 32768 x 4096 bf16 279 us and 283 with it, 16385 x 2049 f32 189 and 224)
+  // (the next row on its way takes registers that more wavefronts can use: 32768 x 4096 bf16 279 us and 283 with it)
   for (long long row0 = (long long)blockIdx.x * GROUPS; row0 < n.rows; row0 += (long long)gridDim.x * GROUPS) {
     load(row0 + group);
     work(row0);

@@ -254,7 +254,7 @@ void with_block_shape(int64_t dim, F f) {
   else if (dim <= 512) f(Int<W>{}, Int<64>{}, Int<N>{});
   else if (dim <= 1024) f(Int<W>{}, Int<128 / D>{}, Int<D * N>{});
   else if (dim <= 2048) f(Int<W>{}, Int<256 / D>{}, Int<D * N>{});
-  else if (dim <= 2560) f(Int<W>{}, Int<FORWARD ? 192 : 320>{}, Int<D * N>{});
+  else if (dim <= 2560) f(Int<W>{}, Int<FORWARD ? 192 : 320 * N>{}, Int<FORWARD ? D * N : 1>{});   // (kBlockTwo with fp32)
   else if (!FORWARD && dim <= 3584) f(Int<W>{}, Int<448>{}, Int<N>{});
   else if (dim <= 4096) f(Int<W>{}, Int<512 / D>{}, Int<D * N>{});
   else if (dim <= 5120) f(Int<W>{}, Int<320>{}, Int<2 * N>{});
@@ -267,8 +267,8 @@ static_assert(kBlockWidest == 8192 && kNormWidest == 16384, "shapes");
 
 // Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
 // As many as the chip holds at a time or somewhat fewer, by what was measured, and fewer where that leaves each less than ten turns (of a row, or of the rows that it has side
-// by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with 768, 1024 and 1536: 16385 x 2049 f32
-// 188, 158 and 169, with means and biases (512, 768, 1024) 215, 215 and 224; 131072 x 256 bf16 with those (768, 1024, 1536) 84, 94 and 94, and 32768 x 4096 with one
+// by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with one workgroup a compute unit and two:
+// 16385 x 2049 f32 165 and 147, with means and biases 203 and 175; 131072 x 256 bf16 with those (768 threads, 1024, 1536) 84, 94 and 94, and 32768 x 4096 with one
 // workgroup a compute unit and two 372 and 294.
 int64_t block_parts(const fira_block_norm_desc* d) {
   if (d->dim > kBlockWidest) return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64));
@@ -279,7 +279,7 @@ int64_t block_parts(const fira_block_norm_desc* d) {
     side = std::max(1, 256 / decltype(t)::value);
   };
   f32 ? with_block_shape<FiraStoredF32, false>(d->dim, shape) : with_block_shape<FiraStoredBf16, false>(d->dim, shape);
-  const int64_t held = d->dim > kBlockWidest / 2 ? 512 : f32 && d->dim > 256 ? (lean ? 1024 : 512) : lean || f32 ? 1024 : 768;
+  const int64_t held = d->dim > kBlockWidest / 2 ? 512 : f32 && d->dim > 256 ? (threads == kBlockTwo ? 2 * kBlockTwo : lean ? 1024 : 512) : lean || f32 ? 1024 : 768;
   const int64_t full = 256 * std::max<int64_t>(f32 || lean || d->dim > kBlockWidest / 2 ? 1 : 2, held / threads), turns = std::max<int64_t>(1, (d->rows + side - 1) / side);
   const int64_t each = std::min(std::max<int64_t>(10, (turns + full - 1) / full), (4 * turns + full - 1) / full);
   return (turns + each - 1) / each;
