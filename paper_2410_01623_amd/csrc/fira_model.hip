@@ -130,12 +130,12 @@ fira_status check_rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, 
   return FIRA_OK;
 }
 
-// How the kernel cuts its work up, in units of `pairs` or `width` values, at most `most` units a workgroup.
-void cut_rotary(FiraRotary& r, int64_t heads, int64_t copied, int pairs, int width, unsigned most) {
-  r.turned = r.half / pairs;
-  r.units = r.turned + (unsigned)(copied / width);
+// How the kernel cuts its work up, in units of `pairs` or `width` values, at most `most` units a workgroup; whole: those of whole heads.
+void cut_rotary(FiraRotary& r, int64_t heads, int pairs, int width, unsigned most, bool whole) {
+  r.turned = (unsigned)(r.half + pairs - 1) / pairs;
+  r.units = r.turned + (unsigned)(r.copied + width - 1) / width;
   r.all = (unsigned)heads * r.units;
-  r.chunk = std::min(r.all, most);
+  r.chunk = std::min(r.all, whole ? most / r.units * r.units : most);
   r.chunks = (r.all + r.chunk - 1) / r.chunk;
   r.tile = std::max(1u, std::min({most / r.chunk, kRotaryTile, kRotaryTable / (unsigned)r.half}));
   r.per_chunk = (unsigned)((((uint64_t)1 << 32) + r.chunk - 1) / r.chunk);
@@ -167,7 +167,8 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
     in_place = in_place && h[i].dev_x == h[i].dev_y;
   }
   if (!heads) return FIRA_OK;
-  const int64_t copied = in_place ? 0 : d->dim - d->rotated, total = (int64_t)r.tokens * heads * (r.half + copied);
+  r.copied = in_place ? 0 : (int)(d->dim - d->rotated);
+  const int64_t copied = r.copied, total = (int64_t)r.tokens * heads * (r.half + copied);
   const hipStream_t q = (hipStream_t)hip_stream;
   with_types(d->dtype, d->dtype, [&](auto t, auto) {
     typedef decltype(t) T;
@@ -180,32 +181,37 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
       }
       return;
     }
-    auto launch = [&](auto width, auto each, auto inter) {
+    auto launch = [&](auto width, auto each, auto inter, bool whole) {
       constexpr int W = decltype(width)::value, N = decltype(each)::value;
       constexpr bool INTER = decltype(inter)::value;
-      cut_rotary(r, heads, copied, INTER && W > 1 ? W / 2 : W, W, 256 * N);
+      cut_rotary(r, heads, INTER && W > 1 ? W / 2 : W, W, 256 * N, whole);
       // (a launch has less than 2^32 threads)
       const int64_t step = (int64_t)((1 << 24) - 1) / r.chunks * r.tile;
       for (int64_t at = 0; at < r.tokens; at += step) {
         r.token0 = (unsigned)at;
-        with_flag(INTER || r.half * size_of(d->dtype) >= 128, [&](auto stream) {
-          hipLaunchKernelGGL((fira_rotary_kernel<T, W, N, INTER, INTER || decltype(stream)::value>), dim3((std::min<int64_t>(step, r.tokens - at) + r.tile - 1) / r.tile * r.chunks),
+        with_flag(!whole && (INTER || r.half * size_of(d->dtype) % 128 == 0), [&](auto stream) {
+          hipLaunchKernelGGL((fira_rotary_kernel<T, W, N, INTER, decltype(stream)::value>), dim3((std::min<int64_t>(step, r.tokens - at) + r.tile - 1) / r.tile * r.chunks),
                              dim3(256), 0, q, r, frequencies, positions);
         });
       }
     };
     // (few units are spread over more workgroups)
-    auto many = [&](auto width) {
+    auto many = [&](auto width, bool whole) {
       with_flag(interleaved, [&](auto inter) {
-        if (total / decltype(width)::value > 1 << 19) launch(width, Int<4>{}, inter);
-        else launch(width, Int<1>{}, inter);
+        if (total / decltype(width)::value > 1 << 19) launch(width, Int<4>{}, inter, whole);
+        else launch(width, Int<1>{}, inter, whole);
       });
     };
     constexpr int W = kWidth<T>;
     const int64_t turned = interleaved ? d->rotated : r.half;
-    if (turned % W == 0 && copied % W == 0) many(Int<W>{});
-    else if (turned % 4 == 0 && copied % 4 == 0) many(Int<4>{});
-    else many(Int<1>{});
+    auto vectors = [&](int w) { return turned % w == 0 && copied % w == 0; };
+    // (vectors may overlap where there are some and a workgroup takes a whole head)
+    auto overlapping = [&](int w) { return turned >= w && (turned + w - 1) / w + (copied + w - 1) / w <= 256; };
+    if (vectors(W)) many(Int<W>{}, false);
+    else if (overlapping(W)) many(Int<W>{}, true);
+    else if (vectors(4)) many(Int<4>{}, false);
+    else if (overlapping(4)) many(Int<4>{}, true);
+    else many(Int<1>{}, false);
   });
   return launched("rotary positions");
 }

@@ -15,12 +15,14 @@ struct FiraRotary {
   unsigned token0, tokens;       // first token of a launch, and tokens of all sequences
   unsigned length;               // of a sequence
   long long position_stride;
-  int half, rotated;
+  int half, rotated, copied;     // copied: values of a head that are not turned, none in place
   float scale, sign;             // sign: -1 for the gradient
   int wide;                      // positions of 64 bits
   // A unit is what a thread turns or copies at a time: W pairs as two vectors of W values, where pairs are interleaved one vector of W values (two with W = 1), or one that is
   // copied.  (Two neighbouring vectors a lane leave every load half a line: 65536 tokens of 32 heads of 128, bf16, interleaved 254 us so and 184 with one.)  A workgroup
-  // takes `tile` tokens and of each `chunk` of the units of all heads.
+  // takes `tile` tokens and of each `chunk` of the units of all heads.  Where a part of a head is no whole number of vectors, its last vector starts earlier and turns values that its neighbour
+  // turns as well; a workgroup takes whole heads then, and has loaded all that it takes before it stores, so that this holds in place too (16384 tokens of 20 heads of 50, bf16, 32 us value
+  // by value and 16 so; heads of 130 149 and 38).
   unsigned units, turned;        // of a head, and those of them that are turned
   unsigned all, tile, chunk, chunks;
   unsigned per_chunk, per_units; // 2^32 / chunk and 2^32 / units, rounded up
@@ -39,13 +41,20 @@ __device__ __forceinline__ void rotary_turn(long long position, double frequency
 // x / d for x d < 2^32
 __device__ __forceinline__ unsigned rotary_quotient(unsigned x, unsigned d, unsigned per_d) { return d == 1 ? x : __umulhi(x, per_d); }
 
+// First value of a unit that is turned.
+template <int W, bool INTERLEAVED>
+__host__ __device__ __forceinline__ unsigned rotary_place(const FiraRotary& r, unsigned unit) {
+  if (INTERLEAVED && W == 1) return 2 * unit;
+  const unsigned last = (unsigned)((INTERLEAVED ? r.rotated : r.half) - W);
+  return unit * W < last ? unit * W : last;
+}
+
 // The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  STREAM: past the caches, but for halves
-// of less than a line, which the caches put together (131072 tokens of 64 heads of 64, bf16: 438 us and 392 with them; heads of 128: 184 and 199).  Bound by memory.
+// that are no whole lines, which the caches put together (131072 tokens of 64 heads of 64, bf16: 438 us and 392 with them; heads of 128: 184 and 199).  Bound by memory.
 template <typename T, int W, int N, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const double* frequencies, const void* positions) {
   typedef typename T::raw raw;
   constexpr bool TWO = !INTERLEAVED || W == 1;             // a unit has two vectors
-  constexpr int PAIRS = TWO ? W : W / 2;
   __shared__ long long place[kRotaryTile];
   __shared__ unsigned long long from[kRotaryTensors][kRotaryTile], to[kRotaryTensors][kRotaryTile];
   __shared__ __attribute__((aligned(16))) float cosines[kRotaryTable], sines[kRotaryTable];
@@ -86,12 +95,12 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     const raw* const in = (const raw*)from[k][t] + h * xh;
     out[n] = (raw*)to[k][t] + h * yh;
     if (unit[n] < r.turned) {
-      const unsigned at = unit[n] * W * (INTERLEAVED && TWO ? 2 : 1);
+      const unsigned at = rotary_place<W, INTERLEAVED>(r, unit[n]);
       fetch(a[n], in + at);
       if (TWO) fetch(b[n], in + at + (INTERLEAVED ? 1 : r.half));
       out[n] += at;
     } else {
-      const unsigned at = r.rotated + (unit[n] - r.turned) * W;
+      const int at = r.rotated + min((int)(unit[n] - r.turned) * W, r.copied - W);
       fetch(a[n], in + at);
       out[n] += at;
     }
@@ -108,10 +117,18 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     if (unit[n] >= r.turned) {
 #pragma unroll
       for (int j = 0; j < W; ++j) p[j] = a[n].get(j);
-      store_w<T, W, STREAM>(out[n], p);
+      if (r.copied >= W) {
+        store_w<T, W, STREAM>(out[n], p);
+      } else {
+        // (the vector begins among the values that are turned)
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          if (j >= W - r.copied) store1<T>(out[n] + j, p[j]);
+      }
       continue;
     }
-    const float *const c = cosines + row[n] * r.half + unit[n] * PAIRS, *const s = sines + row[n] * r.half + unit[n] * PAIRS;
+    const unsigned pair = row[n] * r.half + rotary_place<W, INTERLEAVED>(r, unit[n]) / (INTERLEAVED ? 2 : 1);
+    const float *const c = cosines + pair, *const s = sines + pair;
     if constexpr (!TWO) {
 #pragma unroll
       for (int j = 0; j < W; j += 2) {

@@ -156,9 +156,8 @@ void check_adamw_lists() {
 unsigned quotient(unsigned x, unsigned d, unsigned per_d) { return d == 1 ? x : (unsigned)((uint64_t)x * per_d >> 32); }
 
 // Turns one launch's arguments into counts: touched[tensor][token][head][value].
-void count_rotary(const FiraRotary& r, dim3 grid, int W, int N, bool inter, int64_t dim, std::vector<std::vector<int>>& touched, const std::vector<int64_t>& heads) {
+void count_rotary(const FiraRotary& r, dim3 grid, int W, int N, bool inter, int64_t dim, std::vector<std::vector<int>>& touched, std::vector<std::vector<int>>& owner, const std::vector<int64_t>& heads) {
   const bool two = !inter || W == 1;
-  const int pairs = two ? W : W / 2;
   CHECK(r.tile >= 1 && r.tile <= kRotaryTile && (int64_t)r.tile * r.half <= kRotaryTable);
   CHECK((int64_t)r.tile * r.chunk <= 256 * N && r.chunk >= 1 && (int64_t)r.chunks * r.chunk >= r.all);
   for (unsigned b = 0; b < grid.x; ++b) {
@@ -179,15 +178,24 @@ void count_rotary(const FiraRotary& r, dim3 grid, int W, int N, bool inter, int6
       CHECK(h < heads[k]);
       auto touch = [&](int64_t at, int n) {
         CHECK(at >= 0 && at + n <= dim);
-        for (int v = 0; v < n; ++v) ++touched[k][((int64_t)(t0 + t) * heads[k] + h) * dim + at + v];
+        for (int v = 0; v < n; ++v) {
+          const int64_t place = ((int64_t)(t0 + t) * heads[k] + h) * dim + at + v;
+          ++touched[k][place];
+          // (what is turned twice is turned by one workgroup)
+          CHECK(!owner[k][place] || owner[k][place] == (int)b + 1);
+          owner[k][place] = (int)b + 1;
+        }
       };
       if (unit < r.turned) {
-        CHECK((int64_t)(t * r.half + unit * pairs + pairs) <= kRotaryTable);
-        const unsigned at = unit * W * (inter && two ? 2 : 1);
+        const unsigned at = W == 8 ? (inter ? rotary_place<8, true>(r, unit) : rotary_place<8, false>(r, unit)) : W == 4 ? (inter ? rotary_place<4, true>(r, unit) : rotary_place<4, false>(r, unit)) :
+                            (inter ? rotary_place<1, true>(r, unit) : rotary_place<1, false>(r, unit));
+        CHECK((int64_t)t * r.half + at / (inter ? 2 : 1) + (two ? W : W / 2) <= kRotaryTable && at / (inter ? 2 : 1) + (two ? W : W / 2) <= (unsigned)r.half);
         touch(at, W);
         if (two) touch(at + (inter ? 1 : r.half), W);
       } else {
-        touch(r.rotated + (int64_t)(unit - r.turned) * W, W);
+        const int64_t at = r.rotated + std::min<int64_t>((int64_t)(unit - r.turned) * W, r.copied - W), skip = std::max(0, W - r.copied);
+        CHECK(at >= 0);
+        touch(at + skip, W - skip);
       }
     }
   }
@@ -195,7 +203,7 @@ void count_rotary(const FiraRotary& r, dim3 grid, int W, int N, bool inter, int6
 
 template <typename T, int W, int N>
 bool rotary_launch(const void* f, int& w, int& n, bool& inter) {
-  const bool a = f == (const void*)fira_rotary_kernel<T, W, N, false, false> || f == (const void*)fira_rotary_kernel<T, W, N, false, true>, b = f == (const void*)fira_rotary_kernel<T, W, N, true, true>;
+  const bool a = f == (const void*)fira_rotary_kernel<T, W, N, false, false> || f == (const void*)fira_rotary_kernel<T, W, N, false, true>, b = f == (const void*)fira_rotary_kernel<T, W, N, true, false> || f == (const void*)fira_rotary_kernel<T, W, N, true, true>;
   if (!a && !b) return false;
   w = W;
   n = N;
@@ -214,7 +222,7 @@ void check_rotary_units() {
     fira_rotary_desc d{batch, length, dim, rotated, (int32_t)pick(0, 1), (int32_t)pick(0, 1), (int32_t)pick(0, 1), length, 1.0};
     fira_rotary_heads h[4];
     std::vector<int64_t> heads;
-    std::vector<std::vector<int>> touched;
+    std::vector<std::vector<int>> touched, owner;
     const bool in_place = pick(0, 3) == 0;
     for (int i = 0; i < count; ++i) {
       const int64_t n = pick(0, 9) ? pick(1, big ? 40 : 12) : 0;
@@ -222,6 +230,7 @@ void check_rotary_units() {
       if (!n) continue;
       heads.push_back(n);
       touched.emplace_back((size_t)(batch * length * n * dim));
+      owner.emplace_back((size_t)(batch * length * n * dim));
     }
     int wide = 0;
     look = [&](const void* f, dim3 grid, void** args) {
@@ -232,7 +241,7 @@ void check_rotary_units() {
           rotary_launch<B, 8, 4>(f, w, n, inter) || rotary_launch<B, 8, 1>(f, w, n, inter) || rotary_launch<B, 4, 4>(f, w, n, inter) || rotary_launch<B, 4, 1>(f, w, n, inter) ||
           rotary_launch<B, 1, 4>(f, w, n, inter) || rotary_launch<B, 1, 1>(f, w, n, inter)) {
         CHECK(inter == (d.layout == FIRA_ROTARY_INTERLEAVED) && r.count == (int)heads.size());
-        count_rotary(r, grid, w, n, inter, dim, touched, heads);
+        count_rotary(r, grid, w, n, inter, dim, touched, owner, heads);
       } else {
         ++wide;
         CHECK(rotated / 2 > kRotaryTable);
@@ -242,8 +251,8 @@ void check_rotary_units() {
     if (wide) { CHECK(wide == (int)heads.size()); continue; }
     for (const auto& t : touched)
       for (size_t i = 0; i < t.size(); ++i) {
-        const int want = in_place && (int64_t)(i % dim) >= rotated ? 0 : 1;
-        if (t[i] != want) { CHECK(t[i] == want); break; }
+        const bool want = !in_place || (int64_t)(i % dim) < rotated;
+        if ((t[i] != 0) != want || t[i] > 2) { CHECK((t[i] != 0) == want && t[i] <= 2); break; }
       }
   }
   // the same with more tokens than one launch has threads for: launches adjoin

@@ -56,6 +56,29 @@ def test_shapes(batch, length, heads, kv_heads, dim, rotated, dtype, interleaved
                 assert torch.isnan(buffers[1][:, :, heads + kv_heads:].float()).all() and torch.isnan(buffers[1][..., dim:].float()).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim,rotated", [(50, 50), (98, 98), (130, 130), (130, 26), (256, 254), (64, 10), (72, 18), (27, 16), (35, 34), (254, 254), (1030, 1026)])
+def test_heads_that_are_no_whole_vectors(dim, rotated, dtype, interleaved):
+    """Vectors overlap at the end of a half and of what is copied: many heads and tokens, more than a workgroup has, into other tensors and in place; the same bits both ways."""
+    gen = generator(dim + rotated)
+    f, _ = training.fira_rotary_frequencies(rotated)
+    for tokens, heads in ((3, 5), (700, 9)):
+        q, k = (torch.randn(2, tokens, h, dim, device=DEV, generator=gen).to(dtype) for h in (heads, 2))
+        where = np.arange(tokens)[None].repeat(2, 0)
+        for call in CALLS:
+            got = call(q, k, None, f, interleaved=interleaved, scale=0.9)
+            check(call, got[0], q, where, f, interleaved, 0.9)
+            check(call, got[1], k, where, f, interleaved, 0.9)
+            for _ in range(3):
+                a, b = q.clone(), k.clone()
+                call(a, b, None, f, interleaved=interleaved, scale=0.9, q_out=a, k_out=b)
+                assert torch.equal(a, got[0]) and torch.equal(b, got[1])
+            a, b = q.clone(), torch.empty_like(k)
+            call(a, k, None, f, interleaved=interleaved, scale=0.9, q_out=a, k_out=b)
+            assert torch.equal(a, got[0]) and torch.equal(b, got[1])
+
+
 @pytest.mark.parametrize("far", [10 ** 6, (1 << 31) - 5, 1 << 36, -10 ** 7])
 def test_far_positions(far):
     gen = generator(1)
