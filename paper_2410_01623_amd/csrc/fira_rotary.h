@@ -41,15 +41,16 @@ __device__ __forceinline__ void rotary_turn(long long position, double frequency
 // x / d for x d < 2^32
 __device__ __forceinline__ unsigned rotary_quotient(unsigned x, unsigned d, unsigned per_d) { return d == 1 ? x : __umulhi(x, per_d); }
 
-// First value of a unit that is turned.
-template <int W, bool INTERLEAVED>
+// First value of a unit that is turned.  OVERLAP: vectors may.
+template <int W, bool INTERLEAVED, bool OVERLAP = true>
 __host__ __device__ __forceinline__ unsigned rotary_place(const FiraRotary& r, unsigned unit) {
   if (INTERLEAVED && W == 1) return 2 * unit;
+  if (!OVERLAP) return unit * W;
   const unsigned last = (unsigned)((INTERLEAVED ? r.rotated : r.half) - W);
   return unit * W < last ? unit * W : last;
 }
 
-// The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  STREAM: past the caches, but for halves
+// The sines and cosines of a workgroup's tokens are worked out once, for all heads, into LDS, while the values are on their way.  N: units of a thread.  STREAM: past the caches, and no vectors that overlap; but for halves
 // that are no whole lines, which the caches put together (131072 tokens of 64 heads of 64, bf16: 438 us and 392 with them; heads of 128: 184 and 199).  Bound by memory.
 template <typename T, int W, int N, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const double* frequencies, const void* positions) {
@@ -95,12 +96,12 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     const raw* const in = (const raw*)from[k][t] + h * xh;
     out[n] = (raw*)to[k][t] + h * yh;
     if (unit[n] < r.turned) {
-      const unsigned at = rotary_place<W, INTERLEAVED>(r, unit[n]);
+      const unsigned at = rotary_place<W, INTERLEAVED, !STREAM>(r, unit[n]);
       fetch(a[n], in + at);
       if (TWO) fetch(b[n], in + at + (INTERLEAVED ? 1 : r.half));
       out[n] += at;
     } else {
-      const int at = r.rotated + min((int)(unit[n] - r.turned) * W, r.copied - W);
+      const int c = (int)(unit[n] - r.turned) * W, at = r.rotated + (STREAM ? c : min(c, r.copied - W));
       fetch(a[n], in + at);
       out[n] += at;
     }
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
     if (unit[n] >= r.turned) {
 #pragma unroll
       for (int j = 0; j < W; ++j) p[j] = a[n].get(j);
-      if (r.copied >= W) {
+      if (STREAM || r.copied >= W) {
         store_w<T, W, STREAM>(out[n], p);
       } else {
         // (the vector begins among the values that are turned)
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(256) void fira_rotary_kernel(FiraRotary r, const do
       }
       continue;
     }
-    const unsigned pair = row[n] * r.half + rotary_place<W, INTERLEAVED>(r, unit[n]) / (INTERLEAVED ? 2 : 1);
+    const unsigned pair = row[n] * r.half + rotary_place<W, INTERLEAVED, !STREAM>(r, unit[n]) / (INTERLEAVED ? 2 : 1);
     const float *const c = cosines + pair, *const s = sines + pair;
     if constexpr (!TWO) {
 #pragma unroll
