@@ -155,14 +155,14 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
   r.sign = sign;
   const bool interleaved = d->layout == FIRA_ROTARY_INTERLEAVED;
   r.wide = d->position_type == FIRA_I64;
-  int64_t heads = 0;
+  int64_t heads = 0, of[kRotaryTensors] = {};              // all tensors', which may be 2^31 and more, and each one's
   bool in_place = true;
   for (int i = 0; i < count; ++i) {
     if (!h[i].heads) continue;
     FiraRotaryTensor& t = r.t[r.count];
     t = {h[i].dev_x, h[i].dev_y, {}, {}};
     for (int k = 0; k < 3; ++k) { t.xs[k] = h[i].x_stride[k]; t.ys[k] = h[i].y_stride[k]; }
-    r.first[r.count++] = (int)heads;
+    of[r.count++] = h[i].heads;
     heads += h[i].heads;
     in_place = in_place && h[i].dev_x == h[i].dev_y;
   }
@@ -174,13 +174,12 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
     typedef decltype(t) T;
     // (a head's units are below 2^15, and those of all heads below 2^21, so that their products stay in 32 bits)
     if ((unsigned)r.half > kRotaryTable || r.half + copied > 1 << 15 || heads * (r.half + copied) > 1 << 21) {
-      for (int k = 0; k < r.count; ++k) {
-        const int64_t n = (k + 1 < r.count ? r.first[k + 1] : heads) - r.first[k];
-        hipLaunchKernelGGL(fira_rotary_wide_kernel<T>, dim3(std::min<int64_t>((r.tokens * n * (r.half + copied) + 255) / 256, 1 << 20)), dim3(256), 0, q, r, k, (unsigned)n, (unsigned)copied,
-                           interleaved, frequencies, positions);
-      }
+      for (int k = 0; k < r.count; ++k)
+        hipLaunchKernelGGL(fira_rotary_wide_kernel<T>, dim3(std::min<int64_t>((r.tokens * of[k] * (r.half + copied) + 255) / 256, 1 << 20)), dim3(256), 0, q, r, k, (unsigned)of[k],
+                           (unsigned)copied, interleaved, frequencies, positions);
       return;
     }
+    for (int k = 1; k < r.count; ++k) r.first[k] = r.first[k - 1] + (int)of[k - 1];
     auto launch = [&](auto width, auto each, auto inter, bool whole) {
       constexpr int W = decltype(width)::value, N = decltype(each)::value;
       constexpr bool INTER = decltype(inter)::value;

@@ -10,7 +10,7 @@ struct FiraRotaryTensor {
 };
 struct FiraRotary {
   FiraRotaryTensor t[kRotaryTensors];
-  int first[kRotaryTensors];     // first head of each tensor, of all tensors' heads one after the other
+  int first[kRotaryTensors];     // first head of each tensor, of all tensors' heads one after the other (not for the wide kernel, which takes one tensor)
   int count;
   unsigned token0, tokens;       // first token of a launch, and tokens of all sequences
   unsigned length;               // of a sequence

@@ -1,0 +1,82 @@
+// Host-only check of the largest calls that include/fira.h allows of rotary positions: their host code (csrc/fira_model.hip) over a stand-in for the HIP runtime
+// (host_hip.h), which hands every launch to this program.  Built and run on the CPU by tests/test_host_model_limits.py.
+#include "../paper_2410_01623_amd/csrc/fira_model.hip"
+
+#include <cstring>
+#include <functional>
+#include <string>
+#include <vector>
+
+// (the stand-in leaves launch shapes out: kept here, as launches are made of a shape pushed and popped)
+#define __hipPushCallConfiguration stand_in_push
+#define __hipPopCallConfiguration stand_in_pop
+#include "host_hip.h"
+#undef __hipPushCallConfiguration
+#undef __hipPopCallConfiguration
+namespace {
+dim3 pushed_grid, pushed_block;
+std::string message;
+std::function<void(const void*, dim3, void**)> look;
+void launched_here(const void* f, dim3 grid, void** args) {
+  CHECK(grid.x >= 1 && pushed_block.x >= 1 && pushed_block.x <= 1024 && (int64_t)grid.x * grid.y * grid.z * pushed_block.x < (int64_t)1 << 32);
+  look(f, grid, args);
+}
+}  // namespace
+extern "C" hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t, hipStream_t) {
+  pushed_grid = grid;
+  pushed_block = block;
+  return hipSuccess;
+}
+extern "C" hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* q) {
+  *grid = pushed_grid;
+  *block = pushed_block;
+  *lds = 0;
+  *q = nullptr;
+  return hipSuccess;
+}
+fira_status fira_fail_without_context(fira_status st, const char* msg) noexcept {
+  message = msg;
+  return st;
+}
+
+namespace {
+
+// Up to four tensors of any heads below 2^31, more than that together: each is turned by a launch of its own heads.
+void check_rotary_heads() {
+  const int64_t most = 0x7fffffff;
+  const std::vector<std::vector<int64_t>> lists = {{most}, {most, most}, {most, most, most}, {most, most, most, most}, {most, 5, most, 7}, {1, most, 0, most}, {1 << 30, 1 << 30, 1 << 30, 1 << 30}};
+  for (const auto& heads : lists)
+    for (int layout = 0; layout < 2; ++layout)
+      for (int64_t dim : {2, 6}) {
+        std::vector<fira_rotary_heads> h;
+        for (size_t i = 0; i < heads.size(); ++i)
+          h.push_back({(void*)((1ll << 44) * (int64_t)(i + 1)), (void*)((1ll << 44) * (int64_t)(i + 9)), heads[i], {0, 0, 0}, {0, heads[i] * dim, dim}});
+        const fira_rotary_desc d{1, 3, dim, 2, FIRA_BF16, layout, FIRA_I64, 0, 1.0};
+        std::vector<int64_t> seen;
+        look = [&](const void* f, dim3 grid, void** args) {
+          CHECK(f == (const void*)fira_rotary_wide_kernel<FiraStoredBf16>);
+          const FiraRotary& r = *(const FiraRotary*)args[0];
+          const int k = *(const int*)args[1];
+          const unsigned n = *(const unsigned*)args[2];
+          CHECK(k == (int)seen.size() && k < r.count && (int64_t)grid.x <= 1 << 20);
+          size_t i = 0;                                    // the k-th tensor that has heads
+          for (int j = k; i < heads.size(); ++i)
+            if (heads[i] && j-- == 0) break;
+          CHECK(i < heads.size() && (int64_t)n == heads[i] && r.t[k].x == h[i].dev_x && r.t[k].y == h[i].dev_y);
+          seen.push_back(n);
+        };
+        CHECK(fira_rotary(&d, h.data(), (int)h.size(), (const double*)4096, nullptr, nullptr) == FIRA_OK);
+        size_t some = 0;
+        for (int64_t n : heads) some += n != 0;
+        CHECK(seen.size() == some);
+      }
+}
+
+}  // namespace
+
+int main() {
+  on_launch = launched_here;
+  check_rotary_heads();
+  std::printf("%d failure(s)\n", failures);
+  return failures != 0;
+}
