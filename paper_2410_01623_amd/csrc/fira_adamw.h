@@ -28,7 +28,7 @@ constexpr int kAdamSpans = 36;        // (a lane for each.)  A launch's pieces t
 template <bool EIGHT, bool APART>
 constexpr int kAdamUnroll = EIGHT && APART ? 1 : 2;
 template <bool EIGHT, bool APART>
-int adam_workgroups(int tiles) { return std::min(tiles, EIGHT && APART ? std::max(8192, (tiles + 1) / 2) : 65536); }
+int adam_workgroups(int tiles) { return std::min(tiles, EIGHT && APART ? std::min(std::max(8192, (tiles + 1) / 2), (1 << 24) - 1) : 65536); }   // (a launch has less than 2^32 threads)
 struct FiraAdamSpans {
   FiraAdamSpan s[kAdamSpans];
   int count, tiles;

@@ -1,4 +1,4 @@
-// Host-only check of the largest calls that include/fira.h allows of rotary positions: their host code (csrc/fira_model.hip) over a stand-in for the HIP runtime
+// Host-only check of the largest calls that include/fira.h allows of AdamW and of rotary positions: their host code (csrc/fira_model.hip) over a stand-in for the HIP runtime
 // (host_hip.h), which hands every launch to this program.  Built and run on the CPU by tests/test_host_model_limits.py.
 #include "../paper_2410_01623_amd/csrc/fira_model.hip"
 
@@ -72,10 +72,43 @@ void check_rotary_heads() {
       }
 }
 
+// 2^35 values and more in one list, rows apart and not whole vectors wide, states in 8 bits: each launch has a grid that it may have, and covers its pieces.
+void check_adamw_threads() {
+  typedef FiraStoredF32 F;
+  typedef FiraStoredBf16 B;
+  const int64_t rows = 1047552, cols = 1025;               // nearly a whole piece, so that a launch has 36 of them
+  for (int n : {33, 36, 40})
+    for (int kind = 0; kind < 4; ++kind) {
+      std::vector<fira_adamw_desc> d((size_t)n, fira_adamw_desc{rows, cols, cols + 3, cols + 3, kind & 1, kind >> 1, FIRA_STATE_E4M3, 0, 0.0});
+      std::vector<void*> W;
+      std::vector<const void*> G;
+      std::vector<fira_adamw_state> S;
+      for (int64_t i = 0; i < n; ++i) {
+        char* const at = (char*)((i + 1) << 36);
+        W.push_back(at);
+        G.push_back(at + (1ll << 33));
+        S.push_back({at + (2ll << 33), at + (3ll << 33), (float*)(at + (4ll << 33)), (float*)(at + (5ll << 33))});
+      }
+      int64_t values = 0;
+      look = [&](const void* f, dim3 grid, void** args) {
+        if (f == (const void*)fira_adamw_count_kernel<>) return;
+        CHECK(f == (kind == 0 ? (const void*)fira_adamw_kernel<F, F, true, true> : kind == 1 ? (const void*)fira_adamw_kernel<B, F, true, true> :
+                    kind == 2 ? (const void*)fira_adamw_kernel<F, B, true, true> : (const void*)fira_adamw_kernel<B, B, true, true>));
+        const FiraAdamSpans& l = *(const FiraAdamSpans*)args[0];
+        CHECK((int)grid.x <= l.tiles);
+        for (int i = 0; i < l.count; ++i) values += l.s[i].n;
+      };
+      const fira_adamw_hparams hp{1e-3, 0.9, 0.999, 1e-8, 1.0};
+      CHECK(fira_adamw_step(d.data(), n, &hp, W.data(), G.data(), S.data(), (int64_t*)4096, nullptr, nullptr, nullptr) == FIRA_OK);
+      CHECK(values == n * rows * cols);
+    }
+}
+
 }  // namespace
 
 int main() {
   on_launch = launched_here;
+  check_adamw_threads();
   check_rotary_heads();
   std::printf("%d failure(s)\n", failures);
   return failures != 0;
