@@ -1,4 +1,4 @@
-// Host-only check of the largest calls that include/fira.h allows of AdamW and of rotary positions: their host code (csrc/fira_model.hip) over a stand-in for the HIP runtime
+// Host-only check of the largest calls that include/fira.h allows of AdamW and of rotary positions, and of every width of the block norm: their host code (csrc/fira_model.hip) over a stand-in for the HIP runtime
 // (host_hip.h), which hands every launch to this program.  Built and run on the CPU by tests/test_host_model_limits.py.
 #include "../paper_2410_01623_amd/csrc/fira_model.hip"
 
@@ -104,10 +104,37 @@ void check_adamw_threads() {
     }
 }
 
+// Every width that a row of the block norm is held by: a row's vectors cover it, none begins before it, and the first half of a thread's vectors, which the kernels take
+// as wholly its own, lie wholly inside; a column is one thread's own.
+template <typename T, bool FORWARD>
+void check_block_shapes() {
+  for (int64_t dim = 1; dim <= (FORWARD ? kNormWidest : kBlockWidest); ++dim)
+    with_block_shape<T, FORWARD>(dim, [&](auto width, auto threads, auto nv) {
+      constexpr int W = decltype(width)::value, THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+      CHECK((int64_t)THREADS * W * NV >= dim && (int64_t)THREADS * W * (NV / 2) <= dim && dim >= W);
+      CHECK(THREADS <= 1024 && (THREADS >= 64 ? THREADS % 64 == 0 : 64 % THREADS == 0));
+      if (dim % 97 && dim % 64 > 1) return;
+      std::vector<int> own((size_t)dim, 0);
+      for (int v = 0; v < NV; ++v)
+        for (int me = 0; me < THREADS; ++me) {
+          // (as Columns has it)
+          const int64_t c = ((int64_t)v * THREADS + me) * W, at = std::min(c, dim - W), skip = v < NV / 2 ? 0 : c < dim ? c - at : W;
+          CHECK(at >= 0 && (v >= NV / 2 || at == c));
+          for (int64_t j = skip; j < W; ++j) ++own[(size_t)(at + j)];
+        }
+      for (int n : own)
+        if (n != 1) { CHECK(n == 1); break; }
+    });
+}
+
 }  // namespace
 
 int main() {
   on_launch = launched_here;
+  check_block_shapes<FiraStoredF32, true>();
+  check_block_shapes<FiraStoredF32, false>();
+  check_block_shapes<FiraStoredBf16, true>();
+  check_block_shapes<FiraStoredBf16, false>();
   check_adamw_threads();
   check_rotary_heads();
   std::printf("%d failure(s)\n", failures);
