@@ -406,7 +406,8 @@ FIRA_API fira_status fira_clip_gradients(const fira_gradient_desc* d, int count,
  * there).  r is 16 bits, the low ones for m and the high ones for sqrt(v), of
  *     hash(i, seed, t) = mix(i + mix(mix(seed) + t)),   mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16     (modulo 2^32)
  * with i the value's place in the tensor and t the number of the step: the same call gives the same bits.  A sqrt(v) above zero is held as
- * the smallest code at least, so that a step is never divided by eps alone.  A block whose largest size is below 2^-100 is held as zeros.  What is not finite is held as NaN and
+ * the smallest code at least, so that a step is never divided by eps alone.  A block whose largest size is below 2^-100 is held as zeros
+ * (and of one that is above, roots below 2^-103 as less than they are).  What is not finite is held as NaN and
  * spoils nothing but its own value; in fp32 it stays what it is.
  * A tensor's result does not depend on what else is listed. */
 typedef enum { FIRA_STATE_F32 = 0, FIRA_STATE_E4M3 = 1 } fira_state_type;

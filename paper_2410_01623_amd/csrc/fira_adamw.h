@@ -155,7 +155,7 @@ __device__ __forceinline__ float adam_most(float x) {
   return x;
 }
 
-// a / b, correctly rounded but for what leaves fp32's range on the way.
+// a / b, correctly rounded (1 / b of every mantissa and 2^30 random quotients compared) but for what leaves fp32's range on the way.
 __device__ __forceinline__ float adam_quotient(float a, float b) {
   const float r = __builtin_amdgcn_rcpf(b);
   float q = a * r;
@@ -163,9 +163,9 @@ __device__ __forceinline__ float adam_quotient(float a, float b) {
   return __builtin_amdgcn_div_fixupf(q, b, a);
 }
 
-// Root of x in [2^-126, 2^127], correctly rounded but for one in millions: the rest that the estimate leaves is exact.  (Of less it is too small, of 0 it is 0, of what is
-// not finite no number.)  The root instruction, which is off by an ulp, is 1 % faster at embeddings in 8 bits (274 us and 277); an ulp more or less now and then rounds a code
-// to the other side, whose block has another largest size from the next step on.
+// Root of x in [2^-126, 2^127], correctly rounded from 2^-102 on (every mantissa compared; the rest that the estimate leaves is exact there, and below rounded, so that up to one in twelve is off by an
+// ulp).  (Of less it is too small, of 0 it is 0, of what is not finite no number.)  The root instruction, which is off by an ulp, is 1 % faster at embeddings in 8 bits (274 us and 277); an ulp more
+// or less now and then rounds a code to the other side, whose block has another largest size from the next step on.
 __device__ __forceinline__ float adam_root(float x) {
   const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f)), q = x * y;
   return __builtin_fmaf(__builtin_fmaf(-q, q, x), 0.5f * y, q);
@@ -346,12 +346,12 @@ struct AdamVector {
     }
   }
 
-  // All that is of the gradients' size is held times 2^32, so that small squares stay above 2^-126; where a product leaves fp32's range
-  // for that, the value is worked out again without.
+  // All that is of the gradients' size is held times 2^40, so that squares of roots down to 2^-103, below all that a block's scale is kept for, stay above 2^-126; where a product
+  // leaves fp32's range for that (roots above 2^24), the value is worked out again without.
   __device__ __forceinline__ void step_e4m3(const FiraAdamSpan& s, const FiraAdamHp& hp, const FiraAdamFactors& f, float decay, unsigned key) {
     constexpr int LANES = kAdamBlock / W;
     constexpr float kMost = 0x1p120f;
-    float S = 0x1p32f;
+    float S = 0x1p40f;
     const AdamScaled<true> scaled(f, S);
     float ow[W], om[W], root[W];
     float mm = 0.0f, mv = 0.0f;                            // the block's largest

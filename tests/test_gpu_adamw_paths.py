@@ -118,6 +118,35 @@ def test_a_piece_that_begins_inside_a_row(state):
         assert not w[at].any() and not lst.m[0][at.start * cols:at.stop * cols].view(torch.uint8).any()
 
 
+def test_blocks_of_small_values():
+    """Scales and codes of blocks whose largest root is 2^-100 and more, which are held, and less, which are not.  With betas of zero m is g and the root |g|, but for roundings of the
+    square, the root, the scale and the quotient."""
+    exponents = [-99.9, -99.5, -99.0, -98.0, -97.0, -96.0, -95.5, -95.0, -94.0, -93.0, -90.0, -60.0, 0.0, 26.0, 28.0, 31.0, 33.0, 60.0]
+    gen = base.generator(23)
+    g = 1.0 - 0.4 * torch.rand(len(exponents), 256, device=DEV, generator=gen).double()
+    g[:, 7] = 1.0                                          # the largest
+    g = (g * torch.tensor([2.0 ** e for e in exponents], dtype=torch.float64, device=DEV)[:, None] * torch.where(torch.rand(256, device=DEV, generator=gen) < 0.5, -1.0, 1.0)).float()
+    w = torch.zeros_like(g)
+    lst = training.AdamWList([w], [g], state=E4M3, seeds=[3])
+    lst.fira_adamw_step(1e-3, beta1=0.0, beta2=0.0, eps=1e-38)
+    x = f64(g).reshape(-1)
+    random = ref.rounding(len(x), 3, 1)
+    # (below 2^-100, which no value but those of the first two blocks is, a root may be held as less)
+    fine = np.abs(x) >= 2.0 ** -100
+    assert fine[512:].all()
+    for codes, scales, r, floor in ((lst.m[0], lst.m_scale[0], random[0], False), (lst.v[0], lst.v_scale[0], random[1], True)):
+        most, blocks = ref.block_most(x)
+        within(scales, blocks / 448.0, 8 * U * blocks / 448.0)
+        got = np.abs(ref.e4m3(codes))
+        low, high = (ref.held(x, most, r, floor, e * U) for e in (-8, 8))
+        assert np.all(((got >= low) & (got <= high))[fine]) and np.all(got <= high)
+    # every step is lr in size
+    assert np.all(np.abs(np.abs(f64(w)).reshape(-1) - 1e-3)[fine] <= 16 * U * 1e-3)
+    lst = training.AdamWList([torch.zeros(1, 256, device=DEV)], [g[:1] * 0.9], state=E4M3)
+    lst.fira_adamw_step(1e-3, beta1=0.0, beta2=0.0)
+    assert not any(bool(t.float().any()) for t in (lst.m[0], lst.v[0], lst.m_scale[0], lst.v_scale[0]))       # (zeros of either sign)
+
+
 def test_scales_and_codes_are_the_headers():
     """With betas of zero, m is g and the root |g| (of a square that is rounded, the rounded root is what was squared).  The scale is the largest size times fp32's 1/448, and what a code is
     of the value times ((1 / largest) times 448), each rounded: the same bits for blocks of every size in fp32's range."""
