@@ -672,8 +672,8 @@ class AdamWList:
         self.m_scale, self.v_scale = ([self._state(x, i, scales[i], torch.float32, name) if states[i] is not torch.float32 else None
                                        for i, x in enumerate(given or [None] * n)] for given, name in ((m_scale, "m_scale"), (v_scale, "v_scale")))
         self.t = self._state(t, 0, 2, torch.int64, "t")
-        for given, name in ((params, "tensor"), (self.m, "state m"), (self.v, "state v")):
-            places = [x.data_ptr() for x in given if x.numel()]
+        for given, name in ((params, "tensor"), ((*self.m, *self.v, *self.m_scale, *self.v_scale, self.t), "state or scale")):
+            places = [x.data_ptr() for x in given if x is not None and x.numel()]
             if len(set(places)) < len(places):
                 _refuse(FIRA_ERR_INVALID_ARG, f"a {name} is listed twice")
         pointers = ctypes.c_void_p * n

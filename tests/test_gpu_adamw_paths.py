@@ -168,3 +168,21 @@ def test_scales_and_codes_are_the_headers():
         assert np.array_equal(scales.cpu().numpy(), most * (one(1.0) / one(448.0)))
         c = np.minimum(np.floor(y / step + (r.astype(np.float64) + 0.5) / 65536.0) * step, 448.0)
         assert np.array_equal(np.abs(ref.e4m3(codes))[plain], c[plain])
+
+
+@pytest.mark.parametrize("state", [F32, E4M3])
+def test_one_buffer_for_two_states_is_refused(state):
+    """m of one tensor that is v of another, scales that are listed twice."""
+    from paper_2410_01623_amd import fira
+    p, g = [torch.zeros(2, 256, device=DEV) for _ in range(2)], [torch.zeros(2, 256, device=DEV) for _ in range(2)]
+    held = lambda: [torch.zeros(512, dtype=torch.uint8, device=DEV).view(E4M3) if state is E4M3 else torch.zeros(512, device=DEV) for _ in range(2)]  # noqa: E731
+    scale = lambda: [torch.zeros(2, device=DEV) for _ in range(2)]  # noqa: E731
+    m, v, ms, vs = held(), held(), scale(), scale()
+    scales = dict(m_scale=ms, v_scale=vs) if state is E4M3 else {}
+    training.AdamWList(p, g, m=m, v=v, **scales)
+    bad = [dict(m=m, v=[v[0], m[0]], **scales)]
+    if state is E4M3:
+        bad += [dict(m=m, v=v, m_scale=[ms[0], ms[0]], v_scale=vs), dict(m=m, v=v, m_scale=ms, v_scale=[vs[0], ms[0]]), dict(m=m, v=v, m_scale=ms, v_scale=ms)]
+    for kw in bad:
+        with pytest.raises(fira.FiraError, match="twice"):
+            training.AdamWList(p, g, **kw)
