@@ -458,7 +458,7 @@ def fira_rotary_frequencies(rotated: int, base: float = 10000.0, *, context: int
     """-> (angles of one position, rotated / 2 fp64 values on `device`, and the scale that goes with them) for fira_rotary; context: FIRA_ROTARY_PLAIN, or
     FIRA_ROTARY_LINEAR or FIRA_ROTARY_BY_PARTS for one `factor` times as long as the trained one."""
     lib = fira.load_library()
-    f, scale = (ctypes.c_double * max(1, rotated // 2))(), ctypes.c_double()
+    f, scale = (ctypes.c_double * min(max(1, rotated // 2), 1 << 15))(), ctypes.c_double()       # (more is refused)
     _check(lib.fira_rotary_frequencies(rotated, base, context, factor, trained, low, high, f, scale))
     return torch.tensor(list(f), dtype=torch.float64, device=device), scale.value
 
