@@ -482,7 +482,8 @@ __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAd
   }
 }
 
-// Counting the step in the last launch saves a launch (of 17 vectors, 1.5 us); of many workgroups it would be a queue at one address.
-constexpr int kAdamCounting = 512;
+// Counting the step in the last launch saves a launch, but its workgroups queue at one address.  us in a graph so and with a launch for it: 17 vectors 4.6 and 5.4, 64 workgroups 5.2 and 5.1 (states
+// in 8 bits 6.2 and 6.2), 128 6.6 and 5.3, 256 9.5 and 5.8, 512 19.9 and 6.9; call by call, 17 vectors 7.6 and 9.3.
+constexpr int kAdamCounting = 64;
 template <typename = void>
 __global__ void fira_adamw_count_kernel(long long* taken) { *as_global(taken) += 1; }
