@@ -399,11 +399,14 @@ FIRA_API fira_status fira_clip_gradients(const fira_gradient_desc* d, int count,
  * (eps stands beside the corrected root; fira_step's Adam has it beside the root alone, as Eq. 4 does.)  W is rounded once, to nearest even.
  *
  * States of FIRA_STATE_F32 are m and v, in fp32.  Those of FIRA_STATE_E4M3 are m and sqrt(v), of which the step works with the new values before
- * they are rounded: 256 neighbouring values (of the tensor's rows one after the other; the last such block may be shorter) share an fp32 scale, their
- * largest size / 448, and each value is held as the OCP e4m3 code (1 sign, 4 exponent, 3 mantissa bits) of value / scale.  It is rounded up
+ * they are rounded: 256 neighbouring values (of the tensor's rows one after the other; the last such block may be shorter) share an fp32 scale.  With `most` the
+ * largest size among them,
+ *     scale = most * s,  s = 1/448 rounded to fp32,       y = value * ((1 / most) * 448)
+ * where every product and quotient is rounded to fp32, and a value is held as the OCP e4m3 code (1 sign, 4 exponent, 3 mantissa bits) of y, whose size is at most 448;
+ * what is held is code * scale.  y is rounded up
  * or down at random, with the chances that keep its mean: to nearest, changes below a sixteenth would be lost, and an average over a
- * thousand steps changes by a thousandth in each.  With u = (r + 1/2) / 2^16 the code is the one at or below |value| / scale + u steps (a step: the distance of codes
- * there).  r is 16 bits, the low ones for m and the high ones for sqrt(v), of
+ * thousand steps changes by a thousandth in each.  With u = (r + 1/2) / 2^16 the code is the one at or below |y| + u steps (a step: the distance of codes
+ * there; sizes below 2^-6 are added to 2^-6 for that, in fp32, which loses what they have below 2^-30).  r is 16 bits, the low ones for m and the high ones for sqrt(v), of
  *     hash(i, seed, t) = mix(i + mix(mix(seed) + t)),   mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16     (modulo 2^32)
  * with i the value's place in the tensor and t the number of the step: the same call gives the same bits.  A sqrt(v) above zero is held as
  * the smallest code at least, so that a step is never divided by eps alone.  A block whose largest size is below 2^-100 is held as zeros
