@@ -481,7 +481,8 @@ FIRA_API fira_status fira_rotary_gradient(const fira_rotary_desc* d, const fira_
 
 /* Frequencies f_j = base^(-2j/rotated) in host memory, for contexts longer than the `trained` one.  FIRA_ROTARY_LINEAR: f_j / factor.  FIRA_ROTARY_BY_PARTS: what turns fewer
  * than `low` times over the trained context is divided by factor, what turns more than `high` times is kept, in between it goes over linearly in the
- * number of turns; *scale is then 0.1 ln(factor) + 1, else 1. */
+ * number of turns; *scale is then 0.1 ln(factor) + 1, else 1.  That scale is the one that models trained with it expect; one whose frequencies go by parts and whose scores are
+ * left as they are takes the frequencies and a scale of 1. */
 typedef enum { FIRA_ROTARY_PLAIN = 0, FIRA_ROTARY_LINEAR = 1, FIRA_ROTARY_BY_PARTS = 2 } fira_rotary_context;
 FIRA_API fira_status fira_rotary_frequencies(int64_t rotated, double base, int32_t context, double factor, double trained, double low, double high,
                                              double* host_frequencies, double* scale);

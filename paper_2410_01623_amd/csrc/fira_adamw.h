@@ -424,7 +424,9 @@ struct AdamVector {
 };
 
 // A workgroup takes every gridDim.x-th tile of 256 threads times kAdamUnroll vectors; the lanes that hold a block of 256 values find its scale between them.
-// Bound by memory: 60m bf16 with fp32 gradients and states 232 us (6.0 TB/s), embeddings bf16 in 8 bits 266 (4.9); in 8 bits with rows apart by their ends (511 x 1377 and the like 58, dense 47).
+// With fp32 states bound by memory: 60m bf16 with fp32 gradients 232 us (6.0 TB/s).  With states in 8 bits by vector instructions, about 70 a value, which at four cycles each take all cycles of the SIMDs at
+// embeddings bf16 (270 us, 4.9 TB/s; 330 and more in the first passes after a pause, until the clock is up), 0.93 of them at 62 m values bf16 with fp32 gradients (176) and, with rows apart, whose ends are joined,
+// 0.93 at 511 x 1377 and the like f32 (58, dense 47) and 0.89 at bf16 (57, dense 41).
 // APART: some pieces' rows are, and not whole vectors wide.
 template <typename T, typename R, bool EIGHT, bool APART>
 __global__ __launch_bounds__(256) void fira_adamw_kernel(FiraAdamSpans l, FiraAdamHp hp, const float* lr, const float* norm, long long* counter) {

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void fira_block_norm
   }
 }
 
-// Rows wider than kNormWidest: a workgroup for a row, which it reads again for every sum.
+// Rows wider than kNormWidest: a workgroup for a row, which it reads again for every sum, value by value (4096 x 32768 bf16 1702 us, where 8192 x 16384 above take 215).
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void fira_block_norm_wide_kernel(FiraBlockNorm n, const typename T::raw* x, const typename T::raw* b, FiraBlockVectors<P> v, typename T::raw* r,
                                                                     typename T::raw* y, FiraBlockStats to) {
@@ -193,7 +193,7 @@ struct BlockRowHeld {
 // 312 us (5.2 TB/s), 16385 x 2049 f32 with means and biases 167 (4.8); with few rows by the latency of those of a workgroup (4097 x 2049 so 55, 3.6).
 constexpr int kBlockWidest = 8192;      // of the gradient's rows in registers, 16 values a thread
 // Ten wavefronts, in fp32 up to 2560 columns: two such workgroups fit a compute unit wherever they begin if six wavefronts fit a SIMD (with five, 16385 x 2049 with means and
-// biases took 213 us, alone 203, so 175).
+// biases took 213 us, alone 203, so 175; with five wavefronts of two vectors 210, and without means 165 for 147; 16385 x 2560 224 for 188 and 195 for 178).
 constexpr int kBlockTwo = 640;
 // LEAN: no means and no sums of dy and t, as for root-mean-square norms without biases, which leaves registers for more wavefronts.
 template <typename T, typename P, int W, int THREADS, int NV, bool LEAN>
@@ -397,7 +397,8 @@ struct BlockRow {
   __device__ __forceinline__ float hb(long long c) const { return b ? (load1<T>(b + c) - pm) * ps : 0.0f; }
 };
 
-// Rows wider than kBlockWidest: a workgroup for a row, which it reads again for every sum.  means: of g and g h of every row, for the sums over rows.
+// Rows wider than kBlockWidest: a workgroup for a row, which it reads again for every sum, value by value.  means: of g and g h of every row, for the sums over rows, which read all of it once more (8192 x 16384
+// bf16 2814 us and 637).
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void fira_block_norm_wide_rows_kernel(FiraBlockNorm n, const typename T::raw* dr, const typename T::raw* dy, const typename T::raw* r,
                                                                          const typename T::raw* b, FiraBlockVectors<P> v, FiraBlockStats stats, typename T::raw* dx,

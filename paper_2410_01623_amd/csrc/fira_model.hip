@@ -57,7 +57,9 @@ void for_each_adamw_launch(const fira_adamw_desc* d, int count, void* const* W, 
   for (int kind = 0; kind < 8; ++kind) {
     const int in = kind & 1, grad = kind >> 1 & 1, eight = kind >> 2;
     auto of_kind = [&](const fira_adamw_desc& x) { return x.dtype == in && x.grad_dtype == grad && (x.state_type == FIRA_STATE_E4M3) == (eight != 0); };
-    bool any = false;                                      // (one launch more for those that are not apart would cost more than they lose)
+    // All of a kind go through that kernel then.  A launch more for the others would cost about 1 us, which short lists save; long ones lose more: one such tensor beside 60m bf16 267 us and
+    // without it 232, beside 62 m values bf16 with fp32 gradients in 8 bits 217 and 185.
+    bool any = false;
     for (int i = 0; i < count; ++i) any = any || (of_kind(d[i]) && adamw_apart(d[i]) && d[i].cols % kMostWidth);
     with_types(in, grad, [&](auto t, auto r) {
       with_flag(eight, [&](auto e) {
@@ -194,7 +196,8 @@ fira_status rotary(const fira_rotary_desc* d, const fira_rotary_heads* h, int co
         });
       }
     };
-    // (few units are spread over more workgroups)
+    // Few units are spread over more workgroups.  us with one unit a thread and with four, in a graph, 40 heads of 128: bf16 512 tokens (0.3 of the limit) 4.3 and 5.9, 1024 7.1 and 6.5, 2048 12.0
+    // and 8.4; fp32 512 tokens (0.6) 4.9 and 5.5, 1024 8.8 and 7.5.
     auto many = [&](auto width, bool whole) {
       with_flag(interleaved, [&](auto inter) {
         if (total / decltype(width)::value > 1 << 19) launch(width, Int<4>{}, inter, whole);
@@ -273,8 +276,8 @@ static_assert(kBlockWidest == 8192 && kNormWidest == 16384, "shapes");
 // Workgroups of the gradient, each of which leaves its sums over rows; the workspace: the sums, then two means of every row where rows are read again.
 // As many as the chip holds at a time or somewhat fewer, by what was measured, and fewer where that leaves each less than ten turns (of a row, or of the rows that it has side
 // by side), with a quarter of that at least.  us with 1024 threads a compute unit, 1280 and 2048: 65536 x 2048 bf16 323, 354 and 327; with one workgroup a compute unit and two:
-// 16385 x 2049 f32 165 and 147, with means and biases 203 and 175; 131072 x 256 bf16 with those (768 threads, 1024, 1536) 84, 94 and 94, and 32768 x 4096 with one
-// workgroup a compute unit and two 372 and 294.
+// 16385 x 2049 f32 165 and 147, with means and biases 203 and 175; 131072 x 256 bf16 with those (768 threads, 1024, 1536) 84, 94 and 94, 16385 x 2049 (two workgroups of 320 threads,
+// three, four) 120, 142 and 182, x 2560 109, 133 and 152, and 32768 x 4096 with one workgroup a compute unit and two 372 and 294.
 int64_t block_parts(const fira_block_norm_desc* d) {
   if (d->dim > kBlockWidest) return std::max<int64_t>(1, std::min<int64_t>(d->rows, 64));
   const bool lean = d->norm != FIRA_LAYER_NORM && d->post != FIRA_LAYER_NORM, f32 = d->dtype == FIRA_F32;

@@ -455,8 +455,9 @@ def fira_block_norm_gradient(dresidual: Optional[torch.Tensor], dy: Optional[tor
 
 def fira_rotary_frequencies(rotated: int, base: float = 10000.0, *, context: int = fira.FIRA_ROTARY_PLAIN, factor: float = 1.0, trained: float = 4096.0,
                             low: float = 1.0, high: float = 32.0, device="cuda") -> Tuple[torch.Tensor, float]:
-    """-> (angles of one position, rotated / 2 fp64 values on `device`, and the scale that goes with them) for fira_rotary; context: FIRA_ROTARY_PLAIN, or
-    FIRA_ROTARY_LINEAR or FIRA_ROTARY_BY_PARTS for one `factor` times as long as the trained one."""
+    """-> (angles of one position, rotated / 2 fp64 values on `device`, and a scale) for fira_rotary; context: FIRA_ROTARY_PLAIN, or
+    FIRA_ROTARY_LINEAR or FIRA_ROTARY_BY_PARTS for one `factor` times as long as the trained one.  The scale is 0.1 ln(factor) + 1 by parts, else 1: queries and keys times
+    it make the scores larger, as models expect that were trained so; for one that was not, take the frequencies alone."""
     lib = fira.load_library()
     f, scale = (ctypes.c_double * min(max(1, rotated // 2), 1 << 15))(), ctypes.c_double()       # (more is refused)
     _check(lib.fira_rotary_frequencies(rotated, base, context, factor, trained, low, high, f, scale))
