@@ -635,8 +635,9 @@ class AdamWList:
     are rounded at random by seeds (default: the place in the list).
 
     m, v, m_scale, v_scale (lists; the scales of a float32 state are None) and t (two int64: the steps taken, and a value of the call's) are a
-    checkpoint.  Those that are not given begin at zero, on the stream that is current then.  The states may be dropped with the list while its calls are still at
-    work, on whatever stream that is; parameters and gradients are kept by their owner, and everything by that of a captured step."""
+    checkpoint.  Lists that are not given begin at zero, on the stream that is current then; states that are given have the type that they have,
+    whatever `state` says.  The states may be dropped with the list while its calls are still at work, on whatever stream that is; parameters and
+    gradients are kept by their owner, and everything by that of a captured step."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, weight_decay=0.0, state=torch.float32,
                  m: Optional[Sequence[torch.Tensor]] = None, v: Optional[Sequence[torch.Tensor]] = None, m_scale: Optional[Sequence[Optional[torch.Tensor]]] = None,
@@ -646,7 +647,7 @@ class AdamWList:
         params, grads = list(params), list(grads)
         if not params and device is None:
             _refuse(FIRA_ERR_INVALID_ARG, "an empty list needs a device")
-        if (m is None) != (v is None) or (m_scale is None) != (v_scale is None) or (m is None and m_scale is not None):
+        if (m is None) != (v is None) or (m_scale is None) != (v_scale is None) or (m is None and m_scale is not None) or (m is not None and any(x is None for x in (*m, *v))):
             _refuse(FIRA_ERR_INVALID_ARG, "states that are given in part")
         n = self.count = len(params)
         each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
@@ -658,6 +659,8 @@ class AdamWList:
         for i, x in enumerate(states):
             if x not in _STATES:
                 _refuse(FIRA_ERR_DTYPE, f"state {i} is neither float32 nor float8_e4m3fn")
+        if m_scale is not None and any(x is torch.float8_e4m3fn and None in (a, b) for x, a, b in zip(states, map(_pointer, m_scale), map(_pointer, v_scale))):
+            _refuse(FIRA_ERR_INVALID_ARG, "8-bit states that are given in part, without a scale")
         self.device = dev = _device(*(params or [torch.empty(0, device=device)]), *grads)
         self.descs = (fira.fira_adamw_desc * n)()
         for i, (p, g) in enumerate(zip(params, grads)):
